@@ -248,6 +248,34 @@ vcnn_status vcnn_sgd_update(size_t count, float lr, float* w, const float* dw, v
  * variant).  Tensors with count 0 are skipped. */
 vcnn_status vcnn_sgd_update_multi(int32_t tensors, const size_t* counts, float* const* w, const float* const* dw,
                                   void* const* w_bf16, float lr, void* stream);
+/* Root-mean-square norm of the rows of a [rows][cols] matrix (the activations of a mini-batch, one sample per row), with
+ * the residual's addition before it:
+ *     h = x + residual (rounded to dtype),   rstd[r] = 1 / sqrt(mean_c h[r][c]^2 + eps),   y[r][c] = h[r][c] * rstd[r] * gain[c]
+ * x, residual, h, y follow dtype; gain [cols] and rstd [rows] are float; sums are float (double where the squares leave its
+ * range).  residual may be NULL: then h is x, and the argument h is not used.  rstd may be NULL; vcnn_rmsnorm_bwd needs it.
+ * eps must be positive and finite, cols at most 2^30.  h may be x or residual itself (an update of the residual stream in place), y may be x
+ * where h is not; nothing else may overlap.  A row with an infinity or NaN gives what the formula gives, in that row alone. */
+vcnn_status vcnn_rmsnorm_fwd(int32_t dtype, int32_t rows, int32_t cols, float eps, const void* x, const void* residual,
+                             const float* gain, void* h, void* y, float* rstd, void* stream);
+/* The same with an 8-bit output for vcnn_fc_fwd_i8: with u = h*gain (rounded to float) and a[r] the largest |u| of the row,
+ *     q[r][c] = 127 u / a[r] rounded to the nearest integer (ties to even),   scale[r] = a[r] * rstd[r] / 127
+ * so that q * scale is y within half a step of 1/127 of the row's largest |y|; q is the rounding of the exact quotient.  A row of
+ * zeros gives q = 0 and scale = 0.  A row with a u that is not finite gives q = 0 and scale = NaN. */
+vcnn_status vcnn_rmsnorm_fwd_i8(int32_t dtype, int32_t rows, int32_t cols, float eps, const void* x, const void* residual,
+                                const float* gain, void* h, int8_t* q, float* scale, void* stream);
+/* Gradients of vcnn_rmsnorm_fwd from h (x without a residual), its rstd and dy = dL/dy: with z = h*rstd, t = dy*gain,
+ *     dh[r][c] = dh_above[r][c] + rstd[r] * (t[r][c] - z[r][c] * mean_c(t*z)),   dgain[c] = sum_r dy[r][c] * z[r][c]
+ * dh is the gradient of x and of residual alike; dh_above, the gradient that reaches h beside the norm, may be NULL (zero).
+ * Each of dh, dgain may be NULL and is then not computed.  dh may be dy or dh_above itself.  workspace: at least
+ * vcnn_rmsnorm_workspace_bytes (partial sums of dgain; not needed without dgain). */
+vcnn_status vcnn_rmsnorm_workspace_bytes(int32_t rows, int32_t cols, size_t* bytes);
+vcnn_status vcnn_rmsnorm_bwd(int32_t dtype, int32_t rows, int32_t cols, const void* h, const float* gain, const float* rstd,
+                             const void* dy, const void* dh_above, void* dh, float* dgain, void* workspace,
+                             size_t workspace_bytes, void* stream);
+/* Rows in 8 bits: vcnn_rmsnorm_fwd_i8 with u = x and scale[r] = a[r] / 127.  For the weights [out_f][in_f] of
+ * vcnn_fc_fwd_i8 (one scale per output), and for activations (one per sample). */
+vcnn_status vcnn_quant_rows_i8(int32_t dtype, int32_t rows, int32_t cols, const void* x, int8_t* q, float* scale,
+                               void* stream);
 /* Rounds a float tensor to bfloat16 (nearest even) and back: dst_bf16[i] = bf16(src[i]);  src_f32[i] = float(bf16). */
 vcnn_status vcnn_f32_to_bf16(size_t count, const float* src, void* dst, void* stream);
 vcnn_status vcnn_bf16_to_f32(size_t count, const void* src, float* dst, void* stream);

@@ -1227,6 +1227,57 @@ vcnn_status vcnn_sgd_update_multi(int32_t tensors, const size_t* counts, float* 
   return VCNN_OK;
 }
 
+static vcnn_status check_norm(const char* what, int32_t dtype, int32_t rows, int32_t cols) {
+  if (rows <= 0 || cols <= 0) return fail(VCNN_ERR_SHAPE, "%s: non-positive dimension (rows=%d cols=%d)", what, rows, cols);
+  if (cols > 1 << 30) return fail(VCNN_ERR_UNSUPPORTED, "%s: rows of more than 2^30 elements", what);
+  return check_dtype(dtype, what);
+}
+static vcnn_status check_norm_fwd(const char* what, int32_t dtype, int32_t rows, int32_t cols, float eps, const void* x,
+                                  const void* residual, const float* gain, const void* h, const void* y) {
+  if (vcnn_status s = check_norm(what, dtype, rows, cols)) return s;
+  if (!(eps > 0.f) || !std::isfinite(eps)) return fail(VCNN_ERR_UNSUPPORTED, "%s: eps must be positive and finite", what);
+  if (!x || !gain || !y || (residual && !h)) return fail(VCNN_ERR_NULL, "%s: NULL tensor", what);
+  return VCNN_OK;
+}
+
+vcnn_status vcnn_rmsnorm_fwd(int32_t dtype, int32_t rows, int32_t cols, float eps, const void* x, const void* residual,
+                             const float* gain, void* h, void* y, float* rstd, void* stream) {
+  if (vcnn_status s = check_norm_fwd("rmsnorm_fwd", dtype, rows, cols, eps, x, residual, gain, h, y)) return s;
+  return launch_rmsnorm(dtype, rows, cols, eps, x, residual, gain, h, y, rstd, (hipStream_t)stream);
+}
+
+vcnn_status vcnn_rmsnorm_fwd_i8(int32_t dtype, int32_t rows, int32_t cols, float eps, const void* x, const void* residual,
+                                const float* gain, void* h, int8_t* q, float* scale, void* stream) {
+  if (vcnn_status s = check_norm_fwd("rmsnorm_fwd_i8", dtype, rows, cols, eps, x, residual, gain, h, q)) return s;
+  if (!scale) return fail(VCNN_ERR_NULL, "rmsnorm_fwd_i8: NULL scale");
+  return launch_rmsnorm_i8(dtype, rows, cols, eps, x, residual, gain, h, q, scale, (hipStream_t)stream);
+}
+
+vcnn_status vcnn_rmsnorm_workspace_bytes(int32_t rows, int32_t cols, size_t* bytes) {
+  if (!bytes) return fail(VCNN_ERR_NULL, "rmsnorm_workspace_bytes: NULL out-parameter");
+  if (vcnn_status s = check_norm("rmsnorm_workspace_bytes", VCNN_F32, rows, cols)) return s;
+  *bytes = rmsnorm_bwd_partial_bytes(rows, cols);
+  return VCNN_OK;
+}
+
+vcnn_status vcnn_rmsnorm_bwd(int32_t dtype, int32_t rows, int32_t cols, const void* h, const float* gain, const float* rstd,
+                             const void* dy, const void* dh_above, void* dh, float* dgain, void* workspace,
+                             size_t workspace_bytes, void* stream) {
+  if (vcnn_status s = check_norm("rmsnorm_bwd", dtype, rows, cols)) return s;
+  if (!h || !gain || !rstd || !dy) return fail(VCNN_ERR_NULL, "rmsnorm_bwd: NULL tensor");
+  if (!dh && !dgain) return VCNN_OK;
+  if (dgain)
+    if (vcnn_status s = check_ws(workspace, workspace_bytes, rmsnorm_bwd_partial_bytes(rows, cols), "rmsnorm_bwd")) return s;
+  return launch_rmsnorm_bwd(dtype, rows, cols, h, gain, rstd, dy, dh_above, dh, dgain, (float*)workspace, (hipStream_t)stream);
+}
+
+vcnn_status vcnn_quant_rows_i8(int32_t dtype, int32_t rows, int32_t cols, const void* x, int8_t* q, float* scale,
+                               void* stream) {
+  if (vcnn_status s = check_norm("quant_rows_i8", dtype, rows, cols)) return s;
+  if (!x || !q || !scale) return fail(VCNN_ERR_NULL, "quant_rows_i8: NULL tensor");
+  return launch_quant_rows_i8(dtype, rows, cols, x, q, scale, (hipStream_t)stream);
+}
+
 vcnn_status vcnn_f32_to_bf16(size_t count, const float* src, void* dst, void* stream) {
   if (count == 0) return VCNN_OK;
   if (!src || !dst) return fail(VCNN_ERR_NULL, "f32_to_bf16: NULL tensor");

@@ -474,4 +474,14 @@ vcnn_status launch_sgd_multi(const SgdBatch& a, hipStream_t st);
 vcnn_status launch_f32_to_bf16(size_t count, const float* src, uint16_t* dst, hipStream_t st);
 vcnn_status launch_bf16_to_f32(size_t count, const uint16_t* src, float* dst, hipStream_t st);
 
+// ---- norm.hip -------------------------------------------------------------------------------------------
+vcnn_status launch_rmsnorm(int dtype, int rows, int cols, float eps, const void* x, const void* residual, const float* gain,
+                           void* h, void* y, float* rstd, hipStream_t st);
+vcnn_status launch_rmsnorm_i8(int dtype, int rows, int cols, float eps, const void* x, const void* residual,
+                              const float* gain, void* h, int8_t* q, float* scale, hipStream_t st);
+vcnn_status launch_quant_rows_i8(int dtype, int rows, int cols, const void* x, int8_t* q, float* scale, hipStream_t st);
+size_t rmsnorm_bwd_partial_bytes(int rows, int cols);
+vcnn_status launch_rmsnorm_bwd(int dtype, int rows, int cols, const void* h, const float* gain, const float* rstd,
+                               const void* dy, const void* above, void* dh, float* dgain, float* partial, hipStream_t st);
+
 }  // namespace vcnn

@@ -74,6 +74,14 @@ _SIGNATURES = {
     "vcnn_l2_loss": (c_int32, [c_int32, c_size_t, c_int32, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]),
     "vcnn_sgd_update": (c_int32, [c_size_t, c_float, c_void_p, c_void_p, c_void_p]),
     "vcnn_sgd_update_multi": (c_int32, [c_int32, c_void_p, c_void_p, c_void_p, c_void_p, c_float, c_void_p]),
+    "vcnn_rmsnorm_fwd": (c_int32, [c_int32, c_int32, c_int32, c_float, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                   c_void_p, c_void_p]),
+    "vcnn_rmsnorm_fwd_i8": (c_int32, [c_int32, c_int32, c_int32, c_float, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                      c_void_p, c_void_p]),
+    "vcnn_rmsnorm_workspace_bytes": (c_int32, [c_int32, c_int32, POINTER(c_size_t)]),
+    "vcnn_rmsnorm_bwd": (c_int32, [c_int32, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                   c_void_p, c_void_p, c_size_t, c_void_p]),
+    "vcnn_quant_rows_i8": (c_int32, [c_int32, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_void_p]),
     "vcnn_f32_to_bf16": (c_int32, [c_size_t, c_void_p, c_void_p, c_void_p]),
     "vcnn_bf16_to_f32": (c_int32, [c_size_t, c_void_p, c_void_p, c_void_p]),
 }
@@ -294,6 +302,32 @@ def sgd_update_multi(lr, ws, dws, w16s=None, stream=None):
     dp = (c_void_p * n)(*[_ptr(g) for g in dws])
     hp = None if w16s is None else (c_void_p * n)(*[_ptr(h) for h in w16s])
     _check(lib().vcnn_sgd_update_multi(n, counts, wp, dp, hp, lr, _stream(stream)))
+
+
+def rmsnorm_fwd(dtype, rows, cols, eps, x, residual, gain, h, y, rstd, stream=None):
+    _check(lib().vcnn_rmsnorm_fwd(dtype, rows, cols, eps, _ptr(x), _ptr(residual), _ptr(gain), _ptr(h), _ptr(y), _ptr(rstd),
+                                  _stream(stream)))
+
+
+def rmsnorm_fwd_i8(dtype, rows, cols, eps, x, residual, gain, h, q, scale, stream=None):
+    _check(lib().vcnn_rmsnorm_fwd_i8(dtype, rows, cols, eps, _ptr(x), _ptr(residual), _ptr(gain), _ptr(h), _ptr(q),
+                                     _ptr(scale), _stream(stream)))
+
+
+def rmsnorm_workspace_bytes(rows, cols) -> int:
+    b = c_size_t()
+    _check(lib().vcnn_rmsnorm_workspace_bytes(rows, cols, byref(b)))
+    return b.value
+
+
+def rmsnorm_bwd(dtype, rows, cols, h, gain, rstd, dy, dh_above, dh, dgain, workspace=None, stream=None):
+    p, nbytes = _ws(workspace)
+    _check(lib().vcnn_rmsnorm_bwd(dtype, rows, cols, _ptr(h), _ptr(gain), _ptr(rstd), _ptr(dy), _ptr(dh_above), _ptr(dh),
+                                  _ptr(dgain), p, nbytes, _stream(stream)))
+
+
+def quant_rows_i8(dtype, rows, cols, x, q, scale, stream=None):
+    _check(lib().vcnn_quant_rows_i8(dtype, rows, cols, _ptr(x), _ptr(q), _ptr(scale), _stream(stream)))
 
 
 def f32_to_bf16(count, src, dst, stream=None):

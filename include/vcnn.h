@@ -276,6 +276,18 @@ vcnn_status vcnn_rmsnorm_bwd(int32_t dtype, int32_t rows, int32_t cols, const vo
  * vcnn_fc_fwd_i8 (one scale per output), and for activations (one per sample). */
 vcnn_status vcnn_quant_rows_i8(int32_t dtype, int32_t rows, int32_t cols, const void* x, int8_t* q, float* scale,
                                void* stream);
+/* The forward pass of a fully connected layer in 8-bit integers, for answering with a trained layer:
+ *     y[b][o] = act(bias[o] + xscale[b] * wscale[o] * sum_i xq[b][i] * wq[o][i])
+ * with xq [batch][in_f], wq [out_f][in_f] int8 and a float scale per row of either (vcnn_rmsnorm_fwd_i8, vcnn_quant_rows_i8, or
+ * the caller's own); bias is float and may be NULL; y [batch][out_f] follows dtype.  The sums are exact; a scale of NaN gives
+ * NaN.  in_f is at most 131071 (sums of 32 bits; VCNN_ERR_UNSUPPORTED).  Rows may start at any byte; in_f a multiple of 16 and
+ * 16-byte aligned operands are faster with more than 64 samples.  workspace: vcnn_fc_i8_workspace_bytes (0 for most
+ * layers) divides the sums of layers with few tiles over more of the chip; with less of it, or none (NULL, 0), the call
+ * gives the same bits more slowly. */
+vcnn_status vcnn_fc_i8_workspace_bytes(int32_t batch, int32_t in_f, int32_t out_f, size_t* bytes);
+vcnn_status vcnn_fc_fwd_i8(int32_t dtype, int32_t batch, int32_t in_f, int32_t out_f, int32_t act, const int8_t* xq,
+                           const float* xscale, const int8_t* wq, const float* wscale, const float* bias, void* y,
+                           void* workspace, size_t workspace_bytes, void* stream);
 /* Rounds a float tensor to bfloat16 (nearest even) and back: dst_bf16[i] = bf16(src[i]);  src_f32[i] = float(bf16). */
 vcnn_status vcnn_f32_to_bf16(size_t count, const float* src, void* dst, void* stream);
 vcnn_status vcnn_bf16_to_f32(size_t count, const void* src, float* dst, void* stream);

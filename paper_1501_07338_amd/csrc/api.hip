@@ -1278,6 +1278,35 @@ vcnn_status vcnn_quant_rows_i8(int32_t dtype, int32_t rows, int32_t cols, const 
   return launch_quant_rows_i8(dtype, rows, cols, x, q, scale, (hipStream_t)stream);
 }
 
+static vcnn_status check_fc_i8(int32_t batch, int32_t in_f, int32_t out_f) {
+  if (vcnn_status s = check_fc(batch, in_f, out_f)) return s;
+  if (in_f > kMaxI8Depth)
+    return fail(VCNN_ERR_UNSUPPORTED, "fc_fwd_i8: sums of %d products do not fit 32 bits (at most %d)", in_f, kMaxI8Depth);
+  if (ceil_div(batch, 128) * ceil_div(out_f, 128) > 0x7fffffffLL)
+    return fail(VCNN_ERR_UNSUPPORTED, "fc_fwd_i8: problem too large (batch=%d out_f=%d)", batch, out_f);
+  return VCNN_OK;
+}
+
+vcnn_status vcnn_fc_i8_workspace_bytes(int32_t batch, int32_t in_f, int32_t out_f, size_t* bytes) {
+  if (!bytes) return fail(VCNN_ERR_NULL, "fc_i8_workspace_bytes: NULL out-parameter");
+  if (vcnn_status s = check_fc_i8(batch, in_f, out_f)) return s;
+  *bytes = fc_i8_workspace(batch, in_f, out_f);
+  return VCNN_OK;
+}
+
+vcnn_status vcnn_fc_fwd_i8(int32_t dtype, int32_t batch, int32_t in_f, int32_t out_f, int32_t act, const int8_t* xq,
+                           const float* xscale, const int8_t* wq, const float* wscale, const float* bias, void* y,
+                           void* workspace, size_t workspace_bytes, void* stream) {
+  if (vcnn_status s = check_fc_i8(batch, in_f, out_f)) return s;
+  if (act < VCNN_ACT_NONE || act > VCNN_ACT_SIGMOID) return fail(VCNN_ERR_UNSUPPORTED, "fc_fwd_i8: unknown activation %d", act);
+  if (vcnn_status s = check_dtype(dtype, "fc_fwd_i8")) return s;
+  if (!xq || !xscale || !wq || !wscale || !y) return fail(VCNN_ERR_NULL, "fc_fwd_i8: NULL tensor");
+  if (!workspace) workspace_bytes = 0;
+  if (vcnn_status s = check_ws(workspace, workspace_bytes, workspace ? 1 : 0, "fc_fwd_i8")) return s;
+  return launch_fc_i8(dtype, batch, in_f, out_f, act, xq, xscale, wq, wscale, bias, y, workspace, workspace_bytes,
+                      (hipStream_t)stream);
+}
+
 vcnn_status vcnn_f32_to_bf16(size_t count, const float* src, void* dst, void* stream) {
   if (count == 0) return VCNN_OK;
   if (!src || !dst) return fail(VCNN_ERR_NULL, "f32_to_bf16: NULL tensor");

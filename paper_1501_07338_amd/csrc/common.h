@@ -484,4 +484,11 @@ size_t rmsnorm_bwd_partial_bytes(int rows, int cols);
 vcnn_status launch_rmsnorm_bwd(int dtype, int rows, int cols, const void* h, const float* gain, const float* rstd,
                                const void* dy, const void* above, void* dh, float* dgain, float* partial, hipStream_t st);
 
+// ---- int8.hip -------------------------------------------------------------------------------------------
+static constexpr int kMaxI8Depth = 131071;  // sums of products of at most 2^14 below 2^31
+size_t fc_i8_workspace(int batch, int in_f, int out_f);
+vcnn_status launch_fc_i8(int dtype, int batch, int in_f, int out_f, int act, const int8_t* xq, const float* xscale,
+                         const int8_t* wq, const float* wscale, const float* bias, void* y, void* workspace, size_t bytes,
+                         hipStream_t st);
+
 }  // namespace vcnn

@@ -82,6 +82,9 @@ _SIGNATURES = {
     "vcnn_rmsnorm_bwd": (c_int32, [c_int32, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
                                    c_void_p, c_void_p, c_size_t, c_void_p]),
     "vcnn_quant_rows_i8": (c_int32, [c_int32, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_void_p]),
+    "vcnn_fc_i8_workspace_bytes": (c_int32, [c_int32, c_int32, c_int32, POINTER(c_size_t)]),
+    "vcnn_fc_fwd_i8": (c_int32, [c_int32, c_int32, c_int32, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_void_p,
+                                 c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
     "vcnn_f32_to_bf16": (c_int32, [c_size_t, c_void_p, c_void_p, c_void_p]),
     "vcnn_bf16_to_f32": (c_int32, [c_size_t, c_void_p, c_void_p, c_void_p]),
 }
@@ -328,6 +331,18 @@ def rmsnorm_bwd(dtype, rows, cols, h, gain, rstd, dy, dh_above, dh, dgain, works
 
 def quant_rows_i8(dtype, rows, cols, x, q, scale, stream=None):
     _check(lib().vcnn_quant_rows_i8(dtype, rows, cols, _ptr(x), _ptr(q), _ptr(scale), _stream(stream)))
+
+
+def fc_i8_workspace_bytes(batch, in_f, out_f) -> int:
+    b = c_size_t()
+    _check(lib().vcnn_fc_i8_workspace_bytes(batch, in_f, out_f, byref(b)))
+    return b.value
+
+
+def fc_fwd_i8(dtype, batch, in_f, out_f, act, xq, xscale, wq, wscale, bias, y, workspace=None, stream=None):
+    p, nbytes = _ws(workspace)
+    _check(lib().vcnn_fc_fwd_i8(dtype, batch, in_f, out_f, act, _ptr(xq), _ptr(xscale), _ptr(wq), _ptr(wscale), _ptr(bias),
+                                _ptr(y), p, nbytes, _stream(stream)))
 
 
 def f32_to_bf16(count, src, dst, stream=None):

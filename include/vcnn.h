@@ -288,6 +288,27 @@ vcnn_status vcnn_fc_i8_workspace_bytes(int32_t batch, int32_t in_f, int32_t out_
 vcnn_status vcnn_fc_fwd_i8(int32_t dtype, int32_t batch, int32_t in_f, int32_t out_f, int32_t act, const int8_t* xq,
                            const float* xscale, const int8_t* wq, const float* wscale, const float* bias, void* y,
                            void* workspace, size_t workspace_bytes, void* stream);
+/* The orthogonal part of a [rows][cols] float matrix by Newton-Schulz products: with X = g / |g| (Frobenius norm), `steps`
+ * times  A = X X^T,  X <- a X + (b A + c A^2) X,  (a, b, c) = (3.4445, -4.7750, 2.0315)  (a tall matrix transposed).  The
+ * singular vectors stay, and the singular values, wherever they were between 0.01 and 1 of the norm, come to lie between
+ * 0.68 and 1.21 in five steps.  The products keep float accuracy.  A matrix of zeros gives zeros, one with an infinity or
+ * NaN gives NaN throughout.  out may be g itself.  steps is 1 to 32; workspace: vcnn_orthogonalize_workspace_bytes. */
+vcnn_status vcnn_orthogonalize_workspace_bytes(int32_t rows, int32_t cols, size_t* bytes);
+vcnn_status vcnn_orthogonalize(int32_t rows, int32_t cols, int32_t steps, const float* g, float* out, void* workspace,
+                               size_t workspace_bytes, void* stream);
+/* The Muon update of `tensors` weight matrices (a convolution's kernels count as [k][c*r*s], the kernel matrix of Eq. 2):
+ *     m[t] = momentum * m[t] + dw[t],   u = nesterov ? dw[t] + momentum * m[t] : m[t]
+ *     w[t] = (1 - lr * weight_decay) * w[t] - lr * sqrt(max(1, rows[t] / cols[t])) * orthogonalize(u)
+ * All matrices go through each of its 2 + 3 steps launches together (sixteen at a time).  rows, cols, w, dw, m and w_bf16
+ * are HOST arrays of length `tensors` holding sizes and DEVICE pointers; they are read before the call returns.  w_bf16 may be
+ * NULL; a non-NULL w_bf16[t] receives the updated tensor rounded to bfloat16.  No two tensors may overlap.  lr, momentum and
+ * weight_decay must be finite, steps 1 to 32.  workspace: vcnn_muon_workspace_bytes, three to five times the bytes of the
+ * (first sixteen) matrices, their sides rounded up to multiples of 128. */
+vcnn_status vcnn_muon_workspace_bytes(int32_t tensors, const int32_t* rows, const int32_t* cols, size_t* bytes);
+vcnn_status vcnn_muon_update_multi(int32_t tensors, const int32_t* rows, const int32_t* cols, float* const* w,
+                                   const float* const* dw, float* const* m, void* const* w_bf16, float lr, float momentum,
+                                   int32_t nesterov, float weight_decay, int32_t steps, void* workspace,
+                                   size_t workspace_bytes, void* stream);
 /* Rounds a float tensor to bfloat16 (nearest even) and back: dst_bf16[i] = bf16(src[i]);  src_f32[i] = float(bf16). */
 vcnn_status vcnn_f32_to_bf16(size_t count, const float* src, void* dst, void* stream);
 vcnn_status vcnn_bf16_to_f32(size_t count, const void* src, float* dst, void* stream);

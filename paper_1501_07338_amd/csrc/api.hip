@@ -1307,6 +1307,78 @@ vcnn_status vcnn_fc_fwd_i8(int32_t dtype, int32_t batch, int32_t in_f, int32_t o
                       (hipStream_t)stream);
 }
 
+static vcnn_status check_matrix(const char* what, int32_t rows, int32_t cols) {
+  if (rows <= 0 || cols <= 0) return fail(VCNN_ERR_SHAPE, "%s: non-positive dimension (rows=%d cols=%d)", what, rows, cols);
+  // (the tiles of a launch, and the squares of the smaller side, stay below 2^31 and 2^41)
+  if (rows > 1 << 24 || cols > 1 << 24 || (int64_t)rows * cols > (int64_t)1 << 34)
+    return fail(VCNN_ERR_UNSUPPORTED, "%s: matrix too large (rows=%d cols=%d)", what, rows, cols);
+  return VCNN_OK;
+}
+static vcnn_status check_steps(const char* what, int32_t steps) {
+  if (steps >= 1 && steps <= 32) return VCNN_OK;
+  return fail(VCNN_ERR_UNSUPPORTED, "%s: %d steps (1 to 32 are built)", what, steps);
+}
+
+vcnn_status vcnn_orthogonalize_workspace_bytes(int32_t rows, int32_t cols, size_t* bytes) {
+  if (!bytes) return fail(VCNN_ERR_NULL, "orthogonalize_workspace_bytes: NULL out-parameter");
+  if (vcnn_status s = check_matrix("orthogonalize_workspace_bytes", rows, cols)) return s;
+  *bytes = muon_workspace(1, &rows, &cols);
+  return VCNN_OK;
+}
+
+vcnn_status vcnn_orthogonalize(int32_t rows, int32_t cols, int32_t steps, const float* g, float* out, void* workspace,
+                               size_t workspace_bytes, void* stream) {
+  if (vcnn_status s = check_matrix("orthogonalize", rows, cols)) return s;
+  if (vcnn_status s = check_steps("orthogonalize", steps)) return s;
+  if (!g || !out) return fail(VCNN_ERR_NULL, "orthogonalize: NULL tensor");
+  if (vcnn_status s = check_ws(workspace, workspace_bytes, muon_workspace(1, &rows, &cols), "orthogonalize")) return s;
+  MuonTensor t{};
+  t.g = g, t.out = out, t.rows = rows, t.cols = cols;
+  return launch_muon(&t, 1, 0.f, 0.f, 0, 0.f, steps, workspace, (hipStream_t)stream);
+}
+
+static vcnn_status check_muon(const char* what, int32_t tensors, const int32_t* rows, const int32_t* cols) {
+  if (tensors < 0) return fail(VCNN_ERR_SHAPE, "%s: negative tensor count", what);
+  if (tensors > 0 && (!rows || !cols)) return fail(VCNN_ERR_NULL, "%s: NULL argument array", what);
+  for (int t = 0; t < tensors; ++t)
+    if (vcnn_status s = check_matrix(what, rows[t], cols[t])) return s;
+  return VCNN_OK;
+}
+
+vcnn_status vcnn_muon_workspace_bytes(int32_t tensors, const int32_t* rows, const int32_t* cols, size_t* bytes) {
+  if (!bytes) return fail(VCNN_ERR_NULL, "muon_workspace_bytes: NULL out-parameter");
+  if (vcnn_status s = check_muon("muon_workspace_bytes", tensors, rows, cols)) return s;
+  *bytes = muon_workspace(tensors, rows, cols);
+  return VCNN_OK;
+}
+
+vcnn_status vcnn_muon_update_multi(int32_t tensors, const int32_t* rows, const int32_t* cols, float* const* w,
+                                   const float* const* dw, float* const* m, void* const* w_bf16, float lr, float momentum,
+                                   int32_t nesterov, float weight_decay, int32_t steps, void* workspace,
+                                   size_t workspace_bytes, void* stream) {
+  if (vcnn_status s = check_muon("muon_update_multi", tensors, rows, cols)) return s;
+  if (vcnn_status s = check_steps("muon_update_multi", steps)) return s;
+  if (!std::isfinite(lr) || !std::isfinite(momentum) || !std::isfinite(weight_decay))
+    return fail(VCNN_ERR_UNSUPPORTED, "muon_update_multi: lr, momentum and weight_decay must be finite");
+  if (tensors == 0) return VCNN_OK;
+  if (!w || !dw || !m) return fail(VCNN_ERR_NULL, "muon_update_multi: NULL argument array");
+  for (int t = 0; t < tensors; ++t)  // all checks before the first launch: an error leaves every tensor as it was
+    if (!w[t] || !dw[t] || !m[t]) return fail(VCNN_ERR_NULL, "muon_update_multi: NULL tensor %d", t);
+  if (vcnn_status s = check_ws(workspace, workspace_bytes, muon_workspace(tensors, rows, cols), "muon_update_multi")) return s;
+  for (int t0 = 0; t0 < tensors; t0 += kMuonBatch) {  // batches follow one another in the same memory
+    MuonTensor batch[kMuonBatch] = {};
+    const int n = std::min(kMuonBatch, tensors - t0);
+    for (int i = 0; i < n; ++i) {
+      const int t = t0 + i;
+      batch[i].g = dw[t], batch[i].m = m[t], batch[i].w = w[t], batch[i].w16 = w_bf16 ? w_bf16[t] : nullptr;
+      batch[i].rows = rows[t], batch[i].cols = cols[t];
+      batch[i].factor = std::sqrt(std::max(1.f, (float)rows[t] / (float)cols[t]));
+    }
+    if (vcnn_status s = launch_muon(batch, n, lr, momentum, nesterov, weight_decay, steps, workspace, (hipStream_t)stream)) return s;
+  }
+  return VCNN_OK;
+}
+
 vcnn_status vcnn_f32_to_bf16(size_t count, const float* src, void* dst, void* stream) {
   if (count == 0) return VCNN_OK;
   if (!src || !dst) return fail(VCNN_ERR_NULL, "f32_to_bf16: NULL tensor");

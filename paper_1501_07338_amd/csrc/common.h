@@ -491,4 +491,23 @@ vcnn_status launch_fc_i8(int dtype, int batch, int in_f, int out_f, int act, con
                          const int8_t* wq, const float* wscale, const float* bias, void* y, void* workspace, size_t bytes,
                          hipStream_t st);
 
+// ---- muon.hip -------------------------------------------------------------------------------------------
+static constexpr int kMuonBatch = 16;  // matrices of a launch
+struct MuonTensor {
+  const float* g;      // [rows][cols]
+  float* m;            // momentum, updated (null: g alone is orthogonalised)
+  float* w;            // weights, updated ...
+  void* w16;           // ... and their bfloat16 copy (nullable)
+  float* out;          // given: the orthogonalised matrix, in place of an update of w
+  float factor;        // of the learning rate
+  int rows, cols;
+  // set by the launch: smaller and larger side, 128-tiles along them, this matrix' part of the workspace
+  int tall, small, large, mt, nt, norm_blocks;
+  uint4* work;
+};
+size_t muon_workspace(int tensors, const int32_t* rows, const int32_t* cols);
+// count: at most kMuonBatch
+vcnn_status launch_muon(const MuonTensor* tensors, int count, float lr, float momentum, int nesterov, float weight_decay,
+                        int steps, void* workspace, hipStream_t st);
+
 }  // namespace vcnn

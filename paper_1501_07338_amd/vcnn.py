@@ -8,6 +8,7 @@ there is no fallback path: a missing library raises.
 from __future__ import annotations
 
 import ctypes
+import math
 from ctypes import POINTER, Structure, byref, c_char_p, c_float, c_int32, c_size_t, c_void_p
 from pathlib import Path
 
@@ -85,6 +86,11 @@ _SIGNATURES = {
     "vcnn_fc_i8_workspace_bytes": (c_int32, [c_int32, c_int32, c_int32, POINTER(c_size_t)]),
     "vcnn_fc_fwd_i8": (c_int32, [c_int32, c_int32, c_int32, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_void_p,
                                  c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
+    "vcnn_orthogonalize_workspace_bytes": (c_int32, [c_int32, c_int32, POINTER(c_size_t)]),
+    "vcnn_orthogonalize": (c_int32, [c_int32, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
+    "vcnn_muon_workspace_bytes": (c_int32, [c_int32, c_void_p, c_void_p, POINTER(c_size_t)]),
+    "vcnn_muon_update_multi": (c_int32, [c_int32, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_float, c_float,
+                                         c_int32, c_float, c_int32, c_void_p, c_size_t, c_void_p]),
     "vcnn_f32_to_bf16": (c_int32, [c_size_t, c_void_p, c_void_p, c_void_p]),
     "vcnn_bf16_to_f32": (c_int32, [c_size_t, c_void_p, c_void_p, c_void_p]),
 }
@@ -343,6 +349,42 @@ def fc_fwd_i8(dtype, batch, in_f, out_f, act, xq, xscale, wq, wscale, bias, y, w
     p, nbytes = _ws(workspace)
     _check(lib().vcnn_fc_fwd_i8(dtype, batch, in_f, out_f, act, _ptr(xq), _ptr(xscale), _ptr(wq), _ptr(wscale), _ptr(bias),
                                 _ptr(y), p, nbytes, _stream(stream)))
+
+
+def orthogonalize_workspace_bytes(rows, cols) -> int:
+    b = c_size_t()
+    _check(lib().vcnn_orthogonalize_workspace_bytes(rows, cols, byref(b)))
+    return b.value
+
+
+def orthogonalize(rows, cols, steps, g, out, workspace, stream=None):
+    p, nbytes = _ws(workspace)
+    _check(lib().vcnn_orthogonalize(rows, cols, steps, _ptr(g), _ptr(out), p, nbytes, _stream(stream)))
+
+
+def _sizes(shapes):
+    """(rows, cols) of each shape as two C arrays; a convolution's kernels are the rows of its kernel matrix."""
+    n = len(shapes)
+    rows = (c_int32 * n)(*[s[0] for s in shapes])
+    cols = (c_int32 * n)(*[math.prod(s[1:]) for s in shapes])
+    return rows, cols
+
+
+def muon_workspace_bytes(shapes) -> int:
+    b = c_size_t()
+    _check(lib().vcnn_muon_workspace_bytes(len(shapes), *_sizes(shapes), byref(b)))
+    return b.value
+
+
+def muon_update_multi(lr, momentum, nesterov, weight_decay, steps, ws, dws, ms, workspace, w16s=None, stream=None):
+    """For a list of weight tensors (2 or more dimensions), their gradients and momenta; w16s (optional) are the weights'
+    bfloat16 working copies."""
+    n = len(ws)
+    wp, dp, mp = ((c_void_p * n)(*[_ptr(t) for t in ts]) for ts in (ws, dws, ms))
+    hp = None if w16s is None else (c_void_p * n)(*[_ptr(h) for h in w16s])
+    p, nbytes = _ws(workspace)
+    _check(lib().vcnn_muon_update_multi(n, *_sizes([w.shape for w in ws]), wp, dp, mp, hp, lr, momentum, int(nesterov),
+                                        weight_decay, steps, p, nbytes, _stream(stream)))
 
 
 def f32_to_bf16(count, src, dst, stream=None):

@@ -1,5 +1,5 @@
 """Sequences the C-ABI layer calls into one training step of a layer chain (forward, cost, backward,
-SGD) on one GPU.  This module only owns buffers (torch device tensors), streams and call order; every
+SGD or Muon) on one GPU.  This module only owns buffers (torch device tensors), streams and call order; every
 arithmetic step runs inside libvcnn's kernels.
 
 The backward pass has two independent strands per layer: the input gradient, which the next layer
@@ -16,17 +16,20 @@ import numpy as np
 import torch
 
 from . import vcnn
-from .workloads import FC, Conv, Net, Pool
+from .workloads import FC, Conv, Net, Norm, Pool
 
 
 class TrainStep:
     """Device-resident state of one network: parameters, activations, gradients, workspace."""
 
     def __init__(self, net: Net, params: list, inputs: dict, device: str = "cuda:0", first_layer_dx: bool = False,
-                 dtype: int = vcnn.F32, overlap: bool = True, algos: Optional[dict] = None, fold_conv_act: bool = True):
+                 dtype: int = vcnn.F32, overlap: bool = True, algos: Optional[dict] = None, fold_conv_act: bool = True,
+                 muon: Optional[dict] = None):
         """algos: {layer index: vcnn.ALGO_*} - convolutions named there are planned and launched under that route
         choice, the others under the process-wide one.  fold_conv_act=False: convolutions store their plain input
-        gradient and the ReLU derivative of the layer below is a pass of its own (for comparisons)."""
+        gradient and the ReLU derivative of the layer below is a pass of its own (for comparisons).
+        muon: the weight matrices (a convolution's kernels as the rows of one) are moved by vcnn.muon_update_multi, biases
+        and gains by SGD with the net's rate; a dict with any of lr, momentum, nesterov, weight_decay, steps."""
         self.net, self.dev, self.dtype = net, torch.device(device), dtype
         self.fold_conv_act = fold_conv_act
         self.algos = dict(algos or {})
@@ -44,11 +47,12 @@ class TrainStep:
         self.target = torch.from_numpy(inputs["target"]).to(self.dev) if "target" in inputs else None
         self.upstream = torch.from_numpy(inputs["upstream"]).to(self.dev) if "upstream" in inputs else None
         self.params: List[Optional[tuple]] = [
-            None if p is None else (torch.from_numpy(p[0]).to(self.dev), torch.from_numpy(p[1]).to(self.dev))
-            for p in params]
-        self.grads = [None if p is None else (torch.empty_like(p[0]), torch.empty_like(p[1])) for p in self.params]
+            None if p is None else tuple(torch.from_numpy(t).to(self.dev) for t in p) for p in params]
+        self.grads = [None if p is None else tuple(torch.empty_like(t) for t in p) for p in self.params]
         # bf16 variant: fp32 master weights plus a bf16 copy refreshed after every update
-        self.params16 = [None if p is None or dtype != vcnn.BF16 else torch.empty(p[0].shape, **act) for p in self.params]
+        self.params16 = [None if p is None or len(p) == 1 or dtype != vcnn.BF16 else torch.empty(p[0].shape, **act)
+                         for p in self.params]  # (a norm's gain is read as float)
+        self.rstd = {li: torch.empty(net.batch, **f32) for li, L in enumerate(net.layers) if isinstance(L, Norm)}
         self.acts = [self.x] + [torch.empty(s, **act) for s in net.shapes]
         self.dacts = [torch.empty_like(a) for a in self.acts]
         self.argmax = {li: torch.empty(net.shapes[li], dtype=torch.int32, device=self.dev)
@@ -69,6 +73,8 @@ class TrainStep:
             elif isinstance(L, Pool):
                 self.descs[li] = vcnn.pool_desc(ishape[0], ishape[1], ishape[2], ishape[3], L.win, L.win, L.stride,
                                                 L.stride, dtype=dtype)
+            elif isinstance(L, Norm):
+                ws_bytes = max(ws_bytes, vcnn.rmsnorm_workspace_bytes(*self._rows_cols(li)))
             if getattr(L, "relu", False):  # gradient w.r.t. the pre-activation, read by both strands
                 self.dpre[li] = torch.empty(net.shapes[li], **act)
             # (a first layer's kernel gradient has no input gradient to overlap with and runs on the main stream)
@@ -80,6 +86,13 @@ class TrainStep:
                 if 2.0 * L.cout * ishape[1] * L.kh * L.kw * oshape[0] * oshape[2] * oshape[3] >= 5e8:
                     self.forked[li] = torch.cuda.Event()
                     ws_side_bytes = max(ws_side_bytes, need[2])
+        self.muon = None
+        if muon is not None:
+            self.muon = dict(dict(lr=0.02, momentum=0.95, nesterov=True, weight_decay=0.0, steps=5), **muon)
+            if len(self.muon) != 5:
+                raise ValueError(f"unknown settings of the Muon update: {sorted(muon)}")
+            self.momenta = {li: torch.zeros_like(p[0]) for li, p in enumerate(self.params) if p is not None and len(p) == 2}
+            ws_bytes = max(ws_bytes, vcnn.muon_workspace_bytes([m.shape for m in self.momenta.values()]))
         self.workspace = torch.empty(max(ws_bytes, 256), dtype=torch.uint8, device=self.dev)
         self.workspace_side = torch.empty(max(ws_side_bytes, 256), dtype=torch.uint8, device=self.dev)
         if dtype == vcnn.BF16 and net.loss == "softmax":  # the cost works on float logits
@@ -94,20 +107,23 @@ class TrainStep:
     def refresh_weights(self, stream=None):
         if self.dtype == vcnn.BF16:
             for p, p16 in zip(self.params, self.params16):
-                if p is not None:
+                if p16 is not None:
                     vcnn.f32_to_bf16(p[0].numel(), p[0], p16, stream)
 
     def snapshot(self):
-        """Keeps a device copy of the current parameters for restore()."""
-        self._saved = [None if p is None else (p[0].clone(), p[1].clone()) for p in self.params]
+        """Keeps a device copy of the current parameters (and momenta) for restore()."""
+        self._saved = [None if p is None else tuple(t.clone() for t in p) for p in self.params]
+        self._saved_momenta = {li: m.clone() for li, m in self.momenta.items()} if self.muon else {}
 
     def restore(self, stream=None):
         """Puts the parameters of the last snapshot() back (device-to-device copies, no arithmetic) and refreshes the
         bf16 working copies, so that the next step starts from the same state again."""
         for p, q in zip(self.params, self._saved):
             if p is not None:
-                p[0].copy_(q[0], non_blocking=True)
-                p[1].copy_(q[1], non_blocking=True)
+                for t, u in zip(p, q):
+                    t.copy_(u, non_blocking=True)
+        for li, m in self._saved_momenta.items():
+            self.momenta[li].copy_(m, non_blocking=True)
         self.refresh_weights(stream)
 
     def folds(self, li):
@@ -116,6 +132,11 @@ class TrainStep:
         L = self.net.layers[li]
         kinds = (Pool, FC, Conv) if self.fold_conv_act else (Pool, FC)
         return li > 0 and getattr(self.net.layers[li - 1], "relu", False) and isinstance(L, kinds)
+
+    def _rows_cols(self, li):
+        """Samples, and features of a sample, at the input of layer li."""
+        shape = self.net.in_shape(li)
+        return shape[0], int(np.prod(shape[1:]))
 
     def _routed(self, li, call):
         """call() under the route choice given for layer li (the process-wide choice is put back afterwards)."""
@@ -141,6 +162,9 @@ class TrainStep:
                 self._routed(li, lambda: vcnn.conv_fwd(self.descs[li], a_in, w, b, a_out, self.workspace, stream))
             elif isinstance(L, Pool):
                 vcnn.pool_fwd(self.descs[li], a_in, a_out, self.argmax[li], stream)
+            elif isinstance(L, Norm):
+                vcnn.rmsnorm_fwd(self.dtype, *self._rows_cols(li), L.eps, a_in, None, self.params[li][0], None, a_out,
+                                 self.rstd[li], stream)
             else:
                 w, b = self.weights(li), self.params[li][1]
                 bsz = a_in.shape[0]
@@ -189,6 +213,10 @@ class TrainStep:
                 if need_dx:
                     vcnn.pool_bwd_act(self.descs[li], act_below, a_in, d, self.argmax[li], dx_out, main)
                 continue
+            if isinstance(L, Norm):
+                vcnn.rmsnorm_bwd(self.dtype, *self._rows_cols(li), a_in, self.params[li][0], self.rstd[li], d, None,
+                                 dx_out if need_dx else None, self.grads[li][0], self.workspace, main)
+                continue
             w = self.weights(li)
             dw, db = self.grads[li]
             if isinstance(L, FC):  # one call: at these sizes both products and the bias gradient share a launch
@@ -218,7 +246,15 @@ class TrainStep:
         gs = [t for g in self.grads if g is not None for t in g]
         w16 = None
         if self.dtype == vcnn.BF16:  # the weights' bf16 working copies are refreshed by the same launch
-            w16 = [t for p, h in zip(self.params, self.params16) if p is not None for t in (h, None)]
+            w16 = [t for p, h in zip(self.params, self.params16) if p is not None for t in (h, None)[:len(p)]]
+        if self.muon is not None:
+            o, at = self.muon, list(self.momenta)
+            vcnn.muon_update_multi(o["lr"], o["momentum"], o["nesterov"], o["weight_decay"], o["steps"],
+                                   [self.params[li][0] for li in at], [self.grads[li][0] for li in at],
+                                   [self.momenta[li] for li in at], self.workspace,
+                                   None if w16 is None else [self.params16[li] for li in at], stream)
+            rest = [p[-1] for p in self.params if p is not None]  # biases, gains
+            ws, gs, w16 = rest, [g[-1] for g in self.grads if g is not None], None
         vcnn.sgd_update_multi(self.net.lr, ws, gs, w16, stream)
 
     def step(self, stream=None):
@@ -229,7 +265,7 @@ class TrainStep:
 
     # ---- HIP graph ---------------------------------------------------------------------------------
     def capture(self):
-        """Records one full step (forward, cost, backward, SGD) into a HIP graph and returns the
+        """Records one full step (forward, cost, backward, update) into a HIP graph and returns the
         graph; `graph.replay()` then re-issues the whole launch sequence with one call.  The step
         is run eagerly once first so that one-time kernel attribute set-up happens outside the capture."""
         self.step()

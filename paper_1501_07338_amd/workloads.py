@@ -38,6 +38,12 @@ class FC:
     relu: bool = False
 
 
+@dataclass(frozen=True)
+class Norm:
+    """Root-mean-square norm of each sample over all its features, with a learned gain per feature."""
+    eps: float = 1e-6
+
+
 @dataclass
 class Net:
     name: str
@@ -170,7 +176,7 @@ def make_inputs(net: Net) -> dict:
 
 def make_params(net: Net) -> list:
     """He-normal weights (variance 2 / fan-in) and constant biases, one (w, b) pair per parametrised
-    layer (None for pooling layers), fp32."""
+    layer (None for pooling layers, a gain of ones for a norm), fp32."""
     params = []
     pl = 0
     for li, L in enumerate(net.layers):
@@ -183,6 +189,10 @@ def make_params(net: Net) -> list:
             fan_in = int(np.prod(ishape[1:]))
             wshape = (L.out, fan_in)
             nout = L.out
+        elif isinstance(L, Norm):
+            params.append((np.ones(int(np.prod(ishape[1:])), dtype=np.float32),))
+            pl += 1
+            continue
         else:
             params.append(None)
             continue

@@ -9,27 +9,34 @@
 // transposed.  A and B are symmetric: only tiles on and above the diagonal are computed, and written to both places.
 //
 // Products.  p multiplies small singular values, and with them the rounding errors beside them, by up to 3.44^steps, so the
-// products are kept to float accuracy: every operand is two f16 terms (split_f16.h, 23 bits), three products on the
-// half-precision matrix cores each (frag_product.h).  Since the entries of X, A and B are bounded by their spectral norms
-// (1.203, 1.45, 2.81), their scales are constants.  (With a I in B the sums of B X would carry a X from their beginning and be
-// rounded at its size throughout: three times the error after one step.)  All three live in fragment order only; X in two of them, by rows (the
-// contraction of X X^T runs along n) and by columns (that of B X along m): the tile that a block has finished goes through
-// LDS and leaves in both.
+// products are kept to float accuracy: every operand v is two f16 terms, hi + lo of v times a power of two, and a product is
+// the three products hi hi + hi lo + lo hi on the half-precision matrix cores, in one float accumulator.  The entries of X, A
+// and B are bounded by their spectral norms (1.203, 1.45, 2.81), so the power is 2^14 for all of them: the terms hold 23
+// bits of an entry down to 2^-16, and 2^-39 below; what is left out, lo lo, is 2^-22 of a product at most.  (With a I in B
+// the sums of B X would carry a X from their beginning and be rounded at its size throughout: three times the error after
+// one step.)  All three live in fragment order only (frag_product.h), the order in which the matrix cores take them; X in
+// two of them, by rows (the contraction of X X^T runs along n) and by columns (that of B X along m): the tile that a block
+// has finished goes through LDS and leaves in both.
+//
+// Tiles.  256 x 256 and 128 x 128 from slabs in LDS; where there are too few of those for the chip, 64 x 64 with the
+// contraction divided over the block's eight waves, which read their fragments straight from the caches.
 //
 // All matrices of an update go through each phase in one launch: two launches and three a step for all of them.
 #include <algorithm>
 
 #include "common.h"
 #include "elem.h"
-#include "frag_product.h"
+#include "bf16_core.h"
+#include "mma_core.h"
 
 namespace vcnn {
 
 static constexpr int kThreads = 256;
-static constexpr int kNormBlocks = 256;  // of a matrix
-static constexpr int kExpX = 14, kExpA = 14, kExpB = 14;  // 2^14 times those is below 65504
+static constexpr int kNormBlocks = 1024;  // of a matrix, at most
+static constexpr int kPad = 128;         // sides in the workspace are multiples of it
+static constexpr float kScale = 16384.f, kUnscale = 1.f / kScale;  // 2^14 * 2.81 < 65504
 static constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
-static constexpr int kTileWords = 2048;  // 16-byte words of a 128 x 128 tile of one term
+static constexpr int kTileWords = kPad * kPad / 8;  // 16-byte words of a 128 x 128 tile of one term
 
 enum { MUON_A = 0, MUON_B = 1 };
 
@@ -66,18 +73,28 @@ __device__ __forceinline__ float direction(const MuonBatch& b, float g, float m)
 // ---- momentum, sum of squares -----------------------------------------------------------------------------------------
 // In double: the squares of floats and their sums leave no range and lose nothing that matters.
 __global__ __launch_bounds__(kThreads) void muon_moment_kernel(MuonBatch b) {
-  const MuonTensor& t = b.t[tensor_of(b)];
-  const int block = blockIdx.x - b.first[tensor_of(b)];
+  const int at_tensor = tensor_of(b);
+  const MuonTensor& t = b.t[at_tensor];
+  const int block = blockIdx.x - b.first[at_tensor];
   const int64_t count = (int64_t)t.rows * t.cols;
   double sum = 0.;
-  for (int64_t i = (int64_t)block * kThreads + threadIdx.x; i < count; i += (int64_t)t.norm_blocks * kThreads) {
-    float u = t.g[i];
-    if (t.m) {
-      const float m = fmaf(b.momentum, t.m[i], u);
-      t.m[i] = m;
-      u = direction(b, u, m);
-    }
-    sum += (double)u * u;
+  const auto one = [&](float g, float m, float* out) {
+    if (t.m) *out = fmaf(b.momentum, m, g), g = direction(b, g, *out);
+    sum += (double)g * g;
+  };
+  const int64_t stride = (int64_t)t.norm_blocks * kThreads * 4;
+#pragma unroll 2
+  for (int64_t i = ((int64_t)block * kThreads + threadIdx.x) * 4; i + 4 <= count; i += stride) {
+    const float4 g = ld4_dword_aligned(t.g + i), m = t.m ? ld4_dword_aligned(t.m + i) : g;
+    float4_dword_aligned u;
+    one(g.x, m.x, &u.x), one(g.y, m.y, &u.y), one(g.z, m.z, &u.z), one(g.w, m.w, &u.w);
+    if (t.m) *reinterpret_cast<float4_dword_aligned*>(t.m + i) = u;
+  }
+  if (block == 0 && threadIdx.x < count % 4) {
+    const int64_t i = count - count % 4 + threadIdx.x;
+    float u;
+    one(t.g[i], t.m ? t.m[i] : 0.f, &u);
+    if (t.m) t.m[i] = u;
   }
   __shared__ double waves[kThreads / 64];
 #pragma unroll
@@ -89,7 +106,8 @@ __global__ __launch_bounds__(kThreads) void muon_moment_kernel(MuonBatch b) {
 // 1 / |U|; zero for a matrix of zeros, NaN where an element is not finite.  Called by whole blocks;
 // `waves`: four doubles of LDS, free again afterwards.
 __device__ __forceinline__ double inverse_norm(const MuonTensor& t, double* waves) {
-  double sum = (int)threadIdx.x < t.norm_blocks ? norms(t)[threadIdx.x] : 0.;
+  double sum = 0.;
+  for (int i = threadIdx.x; i < t.norm_blocks; i += kThreads) sum += norms(t)[i];
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
   if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = sum;
@@ -106,168 +124,360 @@ __device__ __forceinline__ double inverse_norm(const MuonTensor& t, double* wave
 __device__ __forceinline__ int shift_of(int i) { return (i & 7) << 2 ^ (i & 4) << 3; }
 __device__ __forceinline__ int at64(int i, int j) { return i * 64 + (j ^ shift_of(i)); }
 
-// Writes the values as two row tiles by four steps of fragments: rows i and contraction j, or (COLS) rows j and contraction i.
-// change(v, word, row, k): eight values of row `row`, contraction k .. k + 7 (both within the wave's part); word: their place.
-template <bool COLS, typename F>
-__device__ __forceinline__ void put_fragments(const float* v64, uint4* dst, int64_t term, int row_tile, int step, int steps,
-                                              int exponent, F change) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll 2
-  for (int f = 0; f < 8; ++f) {
-    const int row = (f >> 2) * 32 + (lane & 31), k = (f & 3) * 16 + (lane >> 5) * 8;
-    float v[8];
-    if (COLS) {
+// Eight values (times 2^14) as two terms.
+__device__ __forceinline__ void split8(const float (&v)[8], uint4* hi, uint4* lo) {
+  f16x8 h, l;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = v64[at64(k + e, row)];
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; e += 4) {
-        const float4 p = *reinterpret_cast<const float4*>(v64 + at64(row, k + e));
-        v[e] = p.x, v[e + 1] = p.y, v[e + 2] = p.z, v[e + 3] = p.w;
-      }
-    }
-    const int64_t word = ((int64_t)(row_tile + (f >> 2)) * steps + step + (f & 3)) * 64 + lane;
-    change(v, word, row, k);
-    uint32_t s[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) s[e] = split_f16(v[e], exponent);
-    uint4 hi, lo;
-    pack_terms(s, &hi, &lo);
-    dst[word] = hi, dst[term + word] = lo;
+  for (int e = 0; e < 8; ++e) {
+    const float t = v[e] * kScale;
+    h[e] = (_Float16)t;
+    l[e] = (_Float16)(t - (float)h[e]);
   }
+  *hi = __builtin_bit_cast(uint4, h), *lo = __builtin_bit_cast(uint4, l);
+}
+__device__ __forceinline__ void join8(const uint4* src, int64_t term, int64_t word, float (&v)[8]) {
+  const f16x8 hi = __builtin_bit_cast(f16x8, src[word]), lo = __builtin_bit_cast(f16x8, src[term + word]);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = ((float)hi[e] + (float)lo[e]) * kUnscale;
 }
 
+// Fragment f (of two row tiles by four steps) of the 64 x 64 values: rows i and contraction j, or (COLS) rows j and
+// contraction i.  word0: the word of fragment 0; change(v, word): eight values and their place.
+template <bool COLS, typename F>
+__device__ __forceinline__ void put_fragment(const float* v64, uint4* dst, int64_t term, int64_t word0, int steps, int f,
+                                             F change) {
+  const int lane = threadIdx.x & 63;
+  const int row = (f >> 2) * 32 + (lane & 31), k = (f & 3) * 16 + (lane >> 5) * 8;
+  float v[8];
+  if (COLS) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = v64[at64(k + e, row)];
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; e += 4) {
+      const float4 p = *reinterpret_cast<const float4*>(v64 + at64(row, k + e));
+      v[e] = p.x, v[e + 1] = p.y, v[e + 2] = p.z, v[e + 3] = p.w;
+    }
+  }
+  const int64_t word = word0 + ((int64_t)(f >> 2) * steps + (f & 3)) * 64 + lane;
+  change(v, word);
+  uint4 hi, lo;
+  split8(v, &hi, &lo);
+  dst[word] = hi, dst[term + word] = lo;
+}
+// Word (without the lane) of the fragment at row i0, contraction j0.
+__device__ __forceinline__ int64_t word_of(int i0, int j0, int steps) { return ((int64_t)(i0 / 32) * steps + j0 / 16) * 64; }
+struct AsIs {
+  __device__ __forceinline__ void operator()(float (&)[8], int64_t) const {}
+};
+
 // ---- X = U / |U| in both orders ---------------------------------------------------------------------------------------
+// (a block's four waves take neighbouring 64 x 64 parts)
 __global__ __launch_bounds__(kThreads) void muon_begin_kernel(MuonBatch b) {
   __shared__ __attribute__((aligned(16))) float smem[4][64 * 64];
-  const MuonTensor& t = b.t[tensor_of(b)];
-  const int tile = blockIdx.x - b.first[tensor_of(b)], it = tile % t.mt, jt = tile / t.mt;
+  const int at_tensor = tensor_of(b);
+  const MuonTensor& t = b.t[at_tensor];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int i0 = it * kFragTile + (wave & 1) * 64, j0 = jt * kFragTile + (wave >> 1) * 64;
   const double inverse = inverse_norm(t, reinterpret_cast<double*>(smem[0]));
+  const int parts_m = (t.small + 63) / 64, parts_n = (t.large + 63) / 64;
+  const int part = (blockIdx.x - b.first[at_tensor]) * 4 + wave;
+  if (part >= parts_m * parts_n) return;
+  // neighbouring parts lie along the rows as stored
+  const int pi = t.tall ? part % parts_m : part / parts_n, pj = t.tall ? part / parts_m : part % parts_n;
+  const int i0 = pi * 64, j0 = pj * 64;
   float* const v64 = smem[wave];
-#pragma unroll 4
-  for (int r = 0; r < 64; ++r) {  // rows of the matrix as stored: of X, or of a tall matrix its columns
-    const int i = t.tall ? lane : r, j = t.tall ? r : lane;
-    float x = 0.f;
-    if (i0 + i < t.small && j0 + j < t.large) {
-      const int64_t at = t.tall ? (int64_t)(j0 + j) * t.small + i0 + i : (int64_t)(i0 + i) * t.large + j0 + j;
-      const float g = t.g[at];
-      x = (float)((t.m ? direction(b, g, t.m[at]) : g) * inverse);
+  const bool whole = i0 + 64 <= t.small && j0 + 64 <= t.large;
+  const int64_t at0 = t.tall ? (int64_t)j0 * t.small + i0 : (int64_t)i0 * t.large + j0;
+  const int pitch = t.tall ? t.small : t.large;
+  const int rows_left = t.tall ? t.large - j0 : t.small - i0, cols_left = t.tall ? t.small - i0 : t.large - j0;
+#pragma unroll 1
+  for (int r0 = 0; r0 < 64; r0 += 16) {  // rows of the matrix as stored: of X, or of a tall matrix its columns
+    float x[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      x[r] = 0.f;
+      if (whole || (r0 + r < rows_left && lane < cols_left)) {
+        const int64_t at = at0 + (int64_t)(r0 + r) * pitch + lane;
+        x[r] = t.m ? direction(b, t.g[at], t.m[at]) : t.g[at];
+      }
     }
-    v64[at64(i, j)] = x;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) v64[t.tall ? at64(lane, r0 + r) : at64(r0 + r, lane)] = (float)(x[r] * inverse);
   }
-  const auto as_is = [](float (&)[8], int64_t, int, int) {};
-  put_fragments<false>(v64, x_rows(t), x_term(t), i0 / 32, j0 / 16, t.nt * 8, kExpX, as_is);
-  put_fragments<true>(v64, x_cols(t, b.turn), x_term(t), j0 / 32, i0 / 16, t.mt * 8, kExpX, as_is);
+#pragma unroll 2
+  for (int f = 0; f < 8; ++f) {
+    put_fragment<false>(v64, x_rows(t), x_term(t), word_of(i0, j0, t.nt * 8), t.nt * 8, f, AsIs());
+    put_fragment<true>(v64, x_cols(t, b.turn), x_term(t), word_of(j0, i0, t.mt * 8), t.mt * 8, f, AsIs());
+  }
 }
 
 // ---- products -----------------------------------------------------------------------------------------------------------
-// The tile (it, jt) of rows by columns, both along `steps` steps, as this wave's 64 x 64 part in LDS.
-__device__ __forceinline__ float* tile_product(const uint4* rows, int64_t rows_term, const uint4* cols, int64_t cols_term,
-                                               int it, int jt, int steps, float scale, uint4* smem) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const uint4* const a = rows + (int64_t)(4 * it + wave) * steps * 64 + lane;
-  const uint4* const c = cols + (int64_t)(4 * jt + wave) * steps * 64 + lane;
-  constexpr int S = FragSlab<2>::STEPS;
-  f32x16 acc[2][2];
-  frag_product<2>(steps / S, smem, rows_term, cols_term, [&](int sl) { return a + sl * (S * 64); },
-                  [&](int sl) { return c + sl * (S * 64); }, acc);
-  float* const v64 = reinterpret_cast<float*>(smem) + wave * (64 * 64);
-#pragma unroll
-  for (int mi = 0; mi < 2; ++mi)
-#pragma unroll
-    for (int ni = 0; ni < 2; ++ni)
-#pragma unroll
-      for (int q = 0; q < 16; ++q) v64[at64(mi * 32 + acc_row(q, lane), ni * 32 + (lane & 31))] = acc[mi][ni][q] * scale;
-  return v64;
-}
+// A block's tile: C[i][j] = sum over `steps` steps (of 16) of rows i of one operand times rows j of the other, handed out
+// as 64 x 64 parts in LDS.  Row tiles of 32 behind the last one read that one again.
+struct Operand {
+  const uint4* src;
+  int64_t term;
+  int row_tile;   // first of the tile
+  int row_tiles;  // of the operand
+  int pitch;      // steps of a row tile
+  __device__ __forceinline__ const uint4* frag(int row, int t, int step) const {
+    return src + t * term + ((int64_t)min(row_tile + row, row_tiles - 1) * pitch + step) * 64;
+  }
+};
 
-__device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
-// the two terms at `word` of a matrix, joined and scaled back
-__device__ __forceinline__ void join8(const uint4* src, int64_t term, int64_t word, float scale, float (&v)[8]) {
-  const f16x8 hi = __builtin_bit_cast(f16x8, src[word]), lo = __builtin_bit_cast(f16x8, src[term + word]);
+// Tiles of 32 TM WM x 32 TN WN, a wave 32 TM x 32 TN of them.  A slab is two steps; wave w brings two row tiles of it, 1 KB a
+// load, while the slab before is multiplied.
+template <int TM_, int TN_, int WM_, int WN_>
+struct SlabTile {
+  static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, WAVES = WM * WN, THREADS = 64 * WAVES;
+  static constexpr int BM = 32 * TM * WM, BN = 32 * TN * WN;
+  static constexpr int ROWS = TM * WM + TN * WN;  // row tiles of both operands
+  static constexpr int WORDS = ROWS * 256;        // of a slab
+  static constexpr size_t LDS = 2 * WORDS * 16;
+  static_assert(ROWS == 2 * WAVES && TM % 2 == 0 && TN == 2, "two row tiles a wave, parts of 64 x 64");
+  static_assert(LDS >= WAVES * 64 * 64 * 4, "the parts fit the slabs' memory");
+
+  // part(v64, i0, j0, f0, f1): a 64 x 64 part at (i0, j0) within the tile, for one wave: fragments 0 .. 8 are its own
+  template <typename F>
+  __device__ static __forceinline__ void run(const Operand& a, const Operand& b, int steps, uint4* smem, F part) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint4* src[2][2];  // [row tile][term]
 #pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = fmaf((float)lo[e], 1.f / 2048.f, (float)hi[e]) * scale;
-}
+    for (int r = 0; r < 2; ++r)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const int row = 2 * wave + r;
+        src[r][t] = (row < TM * WM ? a.frag(row, t, 0) : b.frag(row - TM * WM, t, 0)) + lane;
+      }
+    auto stage = [&](int sl, uint4* buf) {
+#pragma unroll
+      for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int s = 0; s < 2; ++s)
+            load_to_lds16(src[r][t] + (2 * sl + s) * 64, buf + (((2 * wave + r) * 2 + t) * 2 + s) * 64);
+    };
+    const int ra = (wave % WM) * TM, rb = TM * WM + (wave / WM) * TN;
+    f32x16 acc[TM][TN];
+    zero_acc<TM, TN>(acc);
+    const int slabs = (steps + 1) / 2;
+    stage(0, smem);
+    for (int sl = 0; sl < slabs; ++sl) {
+      const uint4* const buf = smem + (sl & 1) * WORDS + lane;
+      __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): this wave's share of the slab has landed
+      __syncthreads();                     // everyone's has, and the other buffer is free
+      if (sl + 1 < slabs) stage(sl + 1, smem + ((sl + 1) & 1) * WORDS);
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        uint4 fa[2][TM], fb[2][TN];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+#pragma unroll
+          for (int i = 0; i < TM; ++i) fa[t][i] = buf[(((ra + i) * 2 + t) * 2 + s) * 64];
+#pragma unroll
+          for (int j = 0; j < TN; ++j) fb[t][j] = buf[(((rb + j) * 2 + t) * 2 + s) * 64];
+        }
+#pragma unroll
+        for (int p = 0; p < 3; ++p)  // hi hi, hi lo, lo hi: consecutive products go to different accumulators
+#pragma unroll
+          for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[i][j] = mfma_f16(fa[p == 2][i], fb[p == 1][j], acc[i][j]);
+      }
+    }
+    __syncthreads();
+    float* const v64 = reinterpret_cast<float*>(smem) + wave * (64 * 64);
+#pragma unroll
+    for (int h = 0; h < TM / 2; ++h) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+          for (int q = 0; q < 16; ++q)
+            v64[at64(i * 32 + acc_row(q, lane), j * 32 + (lane & 31))] = acc[2 * h + i][j][q] * (kUnscale * kUnscale);
+      part(v64, (ra / 2 + h) * 64, (wave / WM) * 64, 0, 8);
+    }
+  }
+};
+
+// A tile of 64 x 64, every eighth step a wave's; the waves' sums are added in order.
+struct FewTile {
+  static constexpr int WAVES = 8, THREADS = 512, BM = 64, BN = 64;
+  static constexpr size_t LDS = WAVES * 64 * 64 * 4;
+
+  // part(v64, 0, 0, f0, f1): the whole tile for every wave, fragments f0 .. f1 are its own
+  template <typename F>
+  __device__ static __forceinline__ void run(const Operand& a, const Operand& b, int steps, uint4* smem, F part) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint4* src[4][2];  // [row tile of either operand][term]
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) src[r][t] = (r < 2 ? a.frag(r, t, wave) : b.frag(r - 2, t, wave)) + lane;
+    f32x16 acc[2][2];
+    zero_acc<2, 2>(acc);
+    uint4 f[4][2], g[4][2];
+    auto fetch = [&](int s, uint4 (&to)[4][2]) {  // (the last one again behind the last)
+      const int at = min(s, (steps - 1 - wave) / WAVES) * (WAVES * 64);
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) to[r][t] = src[r][t][at];
+    };
+    auto products = [&](const uint4 (&x)[4][2]) {
+#pragma unroll
+      for (int p = 0; p < 3; ++p)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) acc[i][j] = mfma_f16(x[i][p == 2], x[2 + j][p == 1], acc[i][j]);
+    };
+    if (wave < steps) {
+      const int mine = (steps - 1 - wave) / WAVES + 1;
+      fetch(0, f);
+      for (int s = 0; s < mine; s += 2) {
+        fetch(s + 1, g);
+        products(f);
+        if (s + 1 == mine) break;
+        fetch(s + 2, f);
+        products(g);
+      }
+    }
+    float* const all = reinterpret_cast<float*>(smem);
+    float* const v64 = all + wave * (64 * 64);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int q = 0; q < 16; ++q)
+          v64[at64(i * 32 + acc_row(q, lane), j * 32 + (lane & 31))] = acc[i][j][q] * (kUnscale * kUnscale);
+    __syncthreads();
+    float4* const sums = reinterpret_cast<float4*>(all);  // (the waves' parts lie alike: places are added)
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      float4 v = sums[n * 512 + threadIdx.x];
+#pragma unroll
+      for (int w = 1; w < WAVES; ++w) {
+        const float4 u = sums[w * 1024 + n * 512 + threadIdx.x];
+        v.x += u.x, v.y += u.y, v.z += u.z, v.w += u.w;
+      }
+      sums[n * 512 + threadIdx.x] = v;
+    }
+    __syncthreads();
+    part(all, 0, 0, wave, wave + 1);
+  }
+};
 
 // MUON_A: A = X X^T.  MUON_B: B = b A + c A A^T.
-template <int WHAT>
-__global__ __launch_bounds__(kThreads, 2) void muon_square_kernel(MuonBatch b) {
+template <typename TILE, int WHAT>
+__global__ __launch_bounds__(TILE::THREADS, 2) void muon_square_kernel(MuonBatch b) {
   extern __shared__ uint4 smem16[];
-  const MuonTensor& t = b.t[tensor_of(b)];
-  int it = blockIdx.x - b.first[tensor_of(b)], jt = 0;
+  static_assert(TILE::BM == TILE::BN, "the tiles of a symmetric matrix");
+  const int at_tensor = tensor_of(b);
+  const MuonTensor& t = b.t[at_tensor];
+  int it = blockIdx.x - b.first[at_tensor], jt = 0;
   while (it > jt) it -= ++jt;  // column jt of the upper triangle has jt + 1 tiles
-  const int wave = threadIdx.x >> 6;
-  const uint4* const src = WHAT == MUON_A ? x_rows(t) : mat_a(t);
-  const int64_t src_term = WHAT == MUON_A ? x_term(t) : a_term(t);
-  const float* const v64 = tile_product(src, src_term, src, src_term, it, jt, (WHAT == MUON_A ? t.nt : t.mt) * 8,
-                                        pow2(WHAT == MUON_A ? -2 * kExpX : -2 * kExpA), smem16);
-  const int i0 = it * kFragTile + (wave & 1) * 64, j0 = jt * kFragTile + (wave >> 1) * 64;
+  const int pitch = (WHAT == MUON_A ? t.nt : t.mt) * 8, depth = WHAT == MUON_A ? t.large : t.small;
+  Operand x{WHAT == MUON_A ? x_rows(t) : mat_a(t), WHAT == MUON_A ? x_term(t) : a_term(t), it * (TILE::BM / 32), t.mt * 4, pitch};
+  Operand y = x;
+  y.row_tile = jt * (TILE::BM / 32);
   uint4* const dst = WHAT == MUON_A ? mat_a(t) : mat_b(t);
-  const auto polynomial = [&](float (&v)[8], int64_t word, int, int) {
-    if (WHAT == MUON_A) return;
-    float a8[8];
-    join8(mat_a(t), a_term(t), word, pow2(-kExpA), a8);
+  const int steps = t.mt * 8;
+  TILE::run(x, y, (depth + 15) / 16, smem16, [&](const float* v64, int i1, int j1, int f0, int f1) {
+    const int i0 = it * TILE::BM + i1, j0 = jt * TILE::BN + j1;
+    if (max(i0, j0) >= t.mt * kPad) return;
+    const auto polynomial = [&](float (&v)[8], int64_t word) {
+      if (WHAT == MUON_A) return;
+      float a8[8];
+      join8(mat_a(t), a_term(t), word, a8);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = fmaf(kC, v[e], kB * a8[e]);
-  };
-  constexpr int exponent = WHAT == MUON_A ? kExpA : kExpB;
-  put_fragments<false>(v64, dst, a_term(t), i0 / 32, j0 / 16, t.mt * 8, exponent, polynomial);
-  if (it != jt) put_fragments<true>(v64, dst, a_term(t), j0 / 32, i0 / 16, t.mt * 8, exponent, polynomial);
+      for (int e = 0; e < 8; ++e) v[e] = fmaf(kC, v[e], kB * a8[e]);
+    };
+#pragma unroll 2
+    for (int f = f0; f < f1; ++f) {
+      put_fragment<false>(v64, dst, a_term(t), word_of(i0, j0, steps), steps, f, polynomial);
+      if (it != jt) put_fragment<true>(v64, dst, a_term(t), word_of(j0, i0, steps), steps, f, polynomial);
+    }
+  });
 }
 
 // X <- a X + B X; the last one: the result, or the weights moved by it.
-template <bool LAST>
-__global__ __launch_bounds__(kThreads, 2) void muon_apply_kernel(MuonBatch b) {
+template <typename TILE, bool LAST>
+__global__ __launch_bounds__(TILE::THREADS, 2) void muon_apply_kernel(MuonBatch b) {
   extern __shared__ uint4 smem16[];
-  const MuonTensor& t = b.t[tensor_of(b)];
-  const int tile = blockIdx.x - b.first[tensor_of(b)], it = tile % t.mt, jt = tile / t.mt;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  float* const v64 = tile_product(mat_b(t), a_term(t), x_cols(t, b.turn), x_term(t), it, jt, t.mt * 8,
-                                        pow2(-kExpB - kExpX), smem16);
-  const int i0 = it * kFragTile + (wave & 1) * 64, j0 = jt * kFragTile + (wave >> 1) * 64;
+  const int at_tensor = tensor_of(b);
+  const MuonTensor& t = b.t[at_tensor];
+  const int tiles_m = (t.small + TILE::BM - 1) / TILE::BM;
+  const int tile = blockIdx.x - b.first[at_tensor], it = tile % tiles_m, jt = tile / tiles_m;
+  const Operand x{mat_b(t), a_term(t), it * (TILE::BM / 32), t.mt * 4, t.mt * 8};
+  const Operand y{x_cols(t, b.turn), x_term(t), jt * (TILE::BN / 32), t.nt * 4, t.mt * 8};
+  TILE::run(x, y, (t.small + 15) / 16, smem16, [&](float* v64, int i1, int j1, int f0, int f1) {
+    const int i0 = it * TILE::BM + i1, j0 = jt * TILE::BN + j1;
+    const bool inside = i0 < t.mt * kPad && j0 < t.nt * kPad;  // (the same for all waves that share a part)
+    const int lane = threadIdx.x & 63;
+    const int64_t by_rows = word_of(i0, j0, t.nt * 8);
+    if (inside) {
 #pragma unroll 2
-  for (int f = 0; f < 8; ++f) {  // a X, from X by rows (whose place the same lanes write below)
-    const int row = (f >> 2) * 32 + (lane & 31), k = (f & 3) * 16 + (lane >> 5) * 8;
-    float x[8];
-    join8(x_rows(t), x_term(t), ((int64_t)(i0 / 32 + (f >> 2)) * (t.nt * 8) + j0 / 16 + (f & 3)) * 64 + lane, pow2(-kExpX), x);
+      for (int f = f0; f < f1; ++f) {  // a X, from X by rows (whose place the same lanes write below)
+        const int row = (f >> 2) * 32 + (lane & 31), k = (f & 3) * 16 + (lane >> 5) * 8;
+        float v[8];
+        join8(x_rows(t), x_term(t), by_rows + ((int64_t)(f >> 2) * (t.nt * 8) + (f & 3)) * 64 + lane, v);
 #pragma unroll
-    for (int e = 0; e < 8; e += 4) {
-      float4* const p = reinterpret_cast<float4*>(v64 + at64(row, k + e));
-      const float4 v = *p;
-      *p = make_float4(fmaf(kA, x[e], v.x), fmaf(kA, x[e + 1], v.y), fmaf(kA, x[e + 2], v.z), fmaf(kA, x[e + 3], v.w));
-    }
-  }
-  if constexpr (!LAST) {
-    const auto as_is = [](float (&)[8], int64_t, int, int) {};
-    put_fragments<false>(v64, x_rows(t), x_term(t), i0 / 32, j0 / 16, t.nt * 8, kExpX, as_is);
-    put_fragments<true>(v64, x_cols(t, b.turn ^ 1), x_term(t), j0 / 32, i0 / 16, t.mt * 8, kExpX, as_is);
-  } else {
-    const float step = b.lr * t.factor;
-#pragma unroll 4
-    for (int r = 0; r < 64; ++r) {
-      const int i = t.tall ? lane : r, j = t.tall ? r : lane;
-      if (i0 + i >= t.small || j0 + j >= t.large) continue;
-      const int64_t at = t.tall ? (int64_t)(j0 + j) * t.small + i0 + i : (int64_t)(i0 + i) * t.large + j0 + j;
-      const float o = v64[at64(i, j)];
-      if (t.out) {
-        t.out[at] = o;
-      } else {
-        const float w = fmaf(-step, o, b.keep * t.w[at]);
-        t.w[at] = w;
-        if (t.w16) st(reinterpret_cast<bf16*>(t.w16) + at, w);
+        for (int e = 0; e < 8; e += 4) {
+          float4* const p = reinterpret_cast<float4*>(v64 + at64(row, k + e));
+          const float4 u = *p;
+          *p = make_float4(fmaf(kA, v[e], u.x), fmaf(kA, v[e + 1], u.y), fmaf(kA, v[e + 2], u.z), fmaf(kA, v[e + 3], u.w));
+        }
       }
     }
-  }
+    if (f1 - f0 < 8) __syncthreads();  // (a part of several waves)
+    if (!inside) return;
+    if constexpr (!LAST) {
+#pragma unroll 2
+      for (int f = f0; f < f1; ++f) {
+        put_fragment<false>(v64, x_rows(t), x_term(t), by_rows, t.nt * 8, f, AsIs());
+        put_fragment<true>(v64, x_cols(t, b.turn ^ 1), x_term(t), word_of(j0, i0, t.mt * 8), t.mt * 8, f, AsIs());
+      }
+    } else {
+      const float step = b.lr * t.factor;
+      const int64_t at0 = t.tall ? (int64_t)j0 * t.small + i0 : (int64_t)i0 * t.large + j0;
+      const int pitch = t.tall ? t.small : t.large;
+      const int rows_left = t.tall ? t.large - j0 : t.small - i0, cols_left = t.tall ? t.small - i0 : t.large - j0;
+      if (lane >= cols_left) return;
+#pragma unroll 1
+      for (int r0 = f0 * 8; r0 < min(f1 * 8, rows_left); r0 += 8) {  // rows of the matrix as stored
+        float w[8];
+        if (!t.out) {
+#pragma unroll
+          for (int r = 0; r < 8; ++r) w[r] = r0 + r < rows_left ? t.w[at0 + (int64_t)(r0 + r) * pitch + lane] : 0.f;
+        }
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+          if (r0 + r >= rows_left) break;
+          const int64_t at = at0 + (int64_t)(r0 + r) * pitch + lane;
+          const float o = v64[t.tall ? at64(lane, r0 + r) : at64(r0 + r, lane)];
+          if (t.out) {
+            t.out[at] = o;
+          } else {
+            const float v = fmaf(-step, o, b.keep * w[r]);
+            t.w[at] = v;
+            if (t.w16) st(reinterpret_cast<bf16*>(t.w16) + at, v);
+          }
+        }
+      }
+    }
+  });
 }
 
 // ---- launches -----------------------------------------------------------------------------------------------------------
 static void lay_out(MuonTensor* t) {
   t->tall = t->rows > t->cols;
   t->small = std::min(t->rows, t->cols), t->large = std::max(t->rows, t->cols);
-  t->mt = (int)ceil_div(t->small, kFragTile), t->nt = (int)ceil_div(t->large, kFragTile);
-  t->norm_blocks = (int)std::min<int64_t>(kNormBlocks, ceil_div((int64_t)t->rows * t->cols, 4 * kThreads));
+  t->mt = (int)ceil_div(t->small, kPad), t->nt = (int)ceil_div(t->large, kPad);
+  t->norm_blocks = (int)std::min<int64_t>(kNormBlocks, ceil_div((int64_t)t->rows * t->cols, 8 * kThreads));
 }
 
 size_t muon_workspace(int tensors, const int32_t* rows, const int32_t* cols) {
@@ -286,7 +496,7 @@ size_t muon_workspace(int tensors, const int32_t* rows, const int32_t* cols) {
 }
 
 template <typename K, typename N>
-static vcnn_status launch_phase(const char* what, K kernel, MuonBatch* b, size_t lds, hipStream_t st, N blocks_of) {
+static vcnn_status launch_phase(const char* what, K kernel, MuonBatch* b, int threads, size_t lds, hipStream_t st, N blocks_of) {
   int64_t blocks = 0;
   for (int t = 0; t < b->tensors; ++t) {
     b->first[t] = (unsigned)blocks;
@@ -295,36 +505,47 @@ static vcnn_status launch_phase(const char* what, K kernel, MuonBatch* b, size_t
   if (blocks > 0x7fffffffLL) return fail(VCNN_ERR_UNSUPPORTED, "%s: too many tiles", what);
   b->first[b->tensors] = (unsigned)blocks;
   if (lds) (void)hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-  hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kThreads), lds, st, *b);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(threads), lds, st, *b);
   return check_launch(what);
+}
+
+template <typename TILE>
+static vcnn_status launch_steps(MuonBatch b, int steps, hipStream_t st) {
+  const auto tiles = [](const MuonTensor& t) { return ceil_div(t.small, TILE::BM) * ceil_div(t.large, TILE::BN); };
+  const auto triangle = [](const MuonTensor& t) { const int64_t n = ceil_div(t.small, TILE::BM); return n * (n + 1) / 2; };
+  for (int i = 0; i < steps; ++i, b.turn ^= 1) {
+    if (vcnn_status s = launch_phase("muon A", muon_square_kernel<TILE, MUON_A>, &b, TILE::THREADS, TILE::LDS, st, triangle)) return s;
+    if (vcnn_status s = launch_phase("muon B", muon_square_kernel<TILE, MUON_B>, &b, TILE::THREADS, TILE::LDS, st, triangle)) return s;
+    if (vcnn_status s = i + 1 < steps ? launch_phase("muon apply", muon_apply_kernel<TILE, false>, &b, TILE::THREADS, TILE::LDS, st, tiles)
+                                      : launch_phase("muon apply", muon_apply_kernel<TILE, true>, &b, TILE::THREADS, TILE::LDS, st, tiles))
+      return s;
+  }
+  return VCNN_OK;
 }
 
 vcnn_status launch_muon(const MuonTensor* tensors, int count, float lr, float momentum, int nesterov, float weight_decay,
                         int steps, void* workspace, hipStream_t st) {
-  constexpr size_t lds = FragSlab<2>::LDS_BYTES;
-  static_assert(lds >= 4 * 64 * 64 * sizeof(float), "a tile fits the slabs' memory");
   MuonBatch b{};
   b.tensors = count;
   b.lr = lr, b.momentum = momentum, b.nesterov = nesterov, b.keep = 1.f - lr * weight_decay;
   uint4* work = (uint4*)workspace;
+  int64_t tiles128 = 0;
   for (int t = 0; t < b.tensors; ++t) {
     b.t[t] = tensors[t];
     lay_out(&b.t[t]);
     b.t[t].work = work;
     work += work_words(b.t[t]);
+    tiles128 += (int64_t)b.t[t].mt * b.t[t].nt;
   }
-  const auto tiles = [](const MuonTensor& t) { return (int64_t)t.mt * t.nt; };
-  const auto triangle = [](const MuonTensor& t) { return (int64_t)t.mt * (t.mt + 1) / 2; };
-  if (vcnn_status s = launch_phase("muon moment", muon_moment_kernel, &b, 0, st, [](const MuonTensor& t) { return t.norm_blocks; })) return s;
-  if (vcnn_status s = launch_phase("muon begin", muon_begin_kernel, &b, 0, st, tiles)) return s;
-  for (int i = 0; i < steps; ++i, b.turn ^= 1) {
-    if (vcnn_status s = launch_phase("muon A", muon_square_kernel<MUON_A>, &b, lds, st, triangle)) return s;
-    if (vcnn_status s = launch_phase("muon B", muon_square_kernel<MUON_B>, &b, lds, st, triangle)) return s;
-    if (vcnn_status s = i + 1 < steps ? launch_phase("muon apply", muon_apply_kernel<false>, &b, lds, st, tiles)
-                                      : launch_phase("muon apply", muon_apply_kernel<true>, &b, lds, st, tiles))
-      return s;
-  }
-  return VCNN_OK;
+  const auto norm_blocks = [](const MuonTensor& t) { return t.norm_blocks; };
+  const auto parts = [](const MuonTensor& t) { return ceil_div(ceil_div(t.small, 64) * ceil_div(t.large, 64), 4); };
+  if (vcnn_status s = launch_phase("muon moment", muon_moment_kernel, &b, kThreads, 0, st, norm_blocks)) return s;
+  if (vcnn_status s = launch_phase("muon begin", muon_begin_kernel, &b, kThreads, 0, st, parts)) return s;
+  const char* const force = getenv("MUON_TILE");
+  const int tile = force ? atoi(force) : tiles128 <= 128 ? 64 : 128;
+  if (tile == 64) return launch_steps<FewTile>(b, steps, st);
+  if (tile == 256) return launch_steps<SlabTile<4, 2, 2, 4>>(b, steps, st);
+  return launch_steps<SlabTile<2, 2, 2, 2>>(b, steps, st);
 }
 
 }  // namespace vcnn

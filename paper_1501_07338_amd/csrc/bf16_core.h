@@ -23,6 +23,11 @@ __device__ __forceinline__ void load_to_lds16(const uint4* src, uint4* lds_base)
   const unsigned base = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)lds_base);  // low half = LDS offset
   asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(base), "v"(src) : "memory", "m0");
 }
+// The same from a wave-uniform address and a byte offset per lane.
+__device__ __forceinline__ void load_to_lds16(const void* base, uint32_t offset, uint4* lds_base) {
+  const unsigned to = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)lds_base);
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(offset), "s"(base) : "memory", "m0");
+}
 #pragma clang diagnostic pop
 
 // v_mfma_f32_32x32x16_bf16 / v_mfma_f32_16x16x32_bf16: lane l holds A[row l % T][8 k-values of group l / T] and

@@ -58,15 +58,6 @@ __device__ __forceinline__ uint4 load16(const int8_t* row, int c, int k) {
   }
   return make_uint4((uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32));
 }
-// load_to_lds16 (bf16_core.h) from a wave-uniform address and a byte offset per lane.
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-__device__ __forceinline__ void load_to_lds16(const int8_t* base, uint32_t offset, uint4* lds_base) {
-  const unsigned to = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)lds_base);
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(offset), "s"(base) : "memory", "m0");
-}
-#pragma clang diagnostic pop
-
 __device__ __forceinline__ i32x4 mfma_i8(uint4 a, uint4 b, i32x4 c) {
   return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
 }

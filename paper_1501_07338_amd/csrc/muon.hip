@@ -14,7 +14,9 @@
 // and B are bounded by their spectral norms (1.203, 1.45, 2.81), so the power is 2^14 for all of them: the terms hold 23
 // bits of an entry down to 2^-16, and 2^-39 below; what is left out, lo lo, is 2^-22 of a product at most.  (With a I in B
 // the sums of B X would carry a X from their beginning and be rounded at its size throughout: three times the error after
-// one step.)  All three live in fragment order only (frag_product.h), the order in which the matrix cores take them; X in
+// one step.)  All three live in fragment order only, frag[16-row tile][step of 32][lane][8]: word `lane` holds row lane % 16 and
+// elements 8 (lane / 16) + 0..7 of the step, what the lane feeds to one v_mfma_f32_16x16x32_f16 (1.9 PFLOP/s on this card with
+// operands in registers; the 32 x 32 x 16 form, by the power it draws, 1.6); X in
 // two of them, by rows (the contraction of X X^T runs along n) and by columns (that of B X along m): the tile that a block
 // has finished goes through LDS and leaves in both.
 //
@@ -119,9 +121,10 @@ __device__ __forceinline__ double inverse_norm(const MuonTensor& t, double* wave
 }
 
 // ---- a wave's 64 x 64 values in LDS -----------------------------------------------------------------------------------
-// Element (i, j) at 64 i + (j ^ shift(i)): conflict-free along j, for a row's four neighbours in eight rows at a time, and for
-// rows four apart.
-__device__ __forceinline__ int shift_of(int i) { return (i & 7) << 2 ^ (i & 4) << 3; }
+// Element (i, j) at 64 i + (j ^ shift(i)), shift a multiple of four: the accumulators' writes (sixteen neighbours of rows four
+// apart), the reads of rows (four neighbours of sixteen rows) and of columns (sixteen neighbours of rows eight apart) each meet
+// all 64 banks.
+__device__ __forceinline__ int shift_of(int i) { return (i & 7) << 2 ^ (i & 4) << 3 ^ (i & 8) << 1 ^ (i & 16) << 1; }
 __device__ __forceinline__ int at64(int i, int j) { return i * 64 + (j ^ shift_of(i)); }
 
 // Eight values (times 2^14) as two terms.
@@ -141,13 +144,13 @@ __device__ __forceinline__ void join8(const uint4* src, int64_t term, int64_t wo
   for (int e = 0; e < 8; ++e) v[e] = ((float)hi[e] + (float)lo[e]) * kUnscale;
 }
 
-// Fragment f (of two row tiles by four steps) of the 64 x 64 values: rows i and contraction j, or (COLS) rows j and
+// Fragment f (of four row tiles by two steps) of the 64 x 64 values: rows i and contraction j, or (COLS) rows j and
 // contraction i.  word0: the word of fragment 0; change(v, word): eight values and their place.
 template <bool COLS, typename F>
 __device__ __forceinline__ void put_fragment(const float* v64, uint4* dst, int64_t term, int64_t word0, int steps, int f,
                                              F change) {
   const int lane = threadIdx.x & 63;
-  const int row = (f >> 2) * 32 + (lane & 31), k = (f & 3) * 16 + (lane >> 5) * 8;
+  const int row = (f >> 1) * 16 + (lane & 15), k = (f & 1) * 32 + (lane >> 4) * 8;
   float v[8];
   if (COLS) {
 #pragma unroll
@@ -159,145 +162,179 @@ __device__ __forceinline__ void put_fragment(const float* v64, uint4* dst, int64
       v[e] = p.x, v[e + 1] = p.y, v[e + 2] = p.z, v[e + 3] = p.w;
     }
   }
-  const int64_t word = word0 + ((int64_t)(f >> 2) * steps + (f & 3)) * 64 + lane;
+  const int64_t word = word0 + ((int64_t)(f >> 1) * steps + (f & 1)) * 64 + lane;
   change(v, word);
   uint4 hi, lo;
   split8(v, &hi, &lo);
   dst[word] = hi, dst[term + word] = lo;
 }
 // Word (without the lane) of the fragment at row i0, contraction j0.
-__device__ __forceinline__ int64_t word_of(int i0, int j0, int steps) { return ((int64_t)(i0 / 32) * steps + j0 / 16) * 64; }
+__device__ __forceinline__ int64_t word_of(int i0, int j0, int steps) { return ((int64_t)(i0 / 16) * steps + j0 / 32) * 64; }
 struct AsIs {
   __device__ __forceinline__ void operator()(float (&)[8], int64_t) const {}
 };
 
 // ---- X = U / |U| in both orders ---------------------------------------------------------------------------------------
-// (a block's four waves take neighbouring 64 x 64 parts)
+// A block makes one 64 x 64 part.
 __global__ __launch_bounds__(kThreads) void muon_begin_kernel(MuonBatch b) {
-  __shared__ __attribute__((aligned(16))) float smem[4][64 * 64];
+  __shared__ __attribute__((aligned(16))) float v64[64 * 64];
   const int at_tensor = tensor_of(b);
   const MuonTensor& t = b.t[at_tensor];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const double inverse = inverse_norm(t, reinterpret_cast<double*>(smem[0]));
-  const int parts_m = (t.small + 63) / 64, parts_n = (t.large + 63) / 64;
-  const int part = (blockIdx.x - b.first[at_tensor]) * 4 + wave;
-  if (part >= parts_m * parts_n) return;
+  const int part = blockIdx.x - b.first[at_tensor], parts_m = (t.small + 63) / 64, parts_n = (t.large + 63) / 64;
   // neighbouring parts lie along the rows as stored
-  const int pi = t.tall ? part % parts_m : part / parts_n, pj = t.tall ? part / parts_m : part % parts_n;
-  const int i0 = pi * 64, j0 = pj * 64;
-  float* const v64 = smem[wave];
-  const bool whole = i0 + 64 <= t.small && j0 + 64 <= t.large;
+  const int i0 = (t.tall ? part % parts_m : part / parts_n) * 64, j0 = (t.tall ? part / parts_m : part % parts_n) * 64;
   const int64_t at0 = t.tall ? (int64_t)j0 * t.small + i0 : (int64_t)i0 * t.large + j0;
   const int pitch = t.tall ? t.small : t.large;
   const int rows_left = t.tall ? t.large - j0 : t.small - i0, cols_left = t.tall ? t.small - i0 : t.large - j0;
-#pragma unroll 1
-  for (int r0 = 0; r0 < 64; r0 += 16) {  // rows of the matrix as stored: of X, or of a tall matrix its columns
-    float x[16];
+  float x[16];  // of sixteen rows of the matrix as stored: of X, or of a tall matrix its columns
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      x[r] = 0.f;
-      if (whole || (r0 + r < rows_left && lane < cols_left)) {
-        const int64_t at = at0 + (int64_t)(r0 + r) * pitch + lane;
-        x[r] = t.m ? direction(b, t.g[at], t.m[at]) : t.g[at];
-      }
-    }
-#pragma unroll
-    for (int r = 0; r < 16; ++r) v64[t.tall ? at64(lane, r0 + r) : at64(r0 + r, lane)] = (float)(x[r] * inverse);
+  for (int r = 0; r < 16; ++r) {
+    const bool there = wave * 16 + r < rows_left && lane < cols_left;
+    const int64_t at = at0 + (int64_t)(wave * 16 + r) * pitch + lane;
+    x[r] = !there ? 0.f : t.m ? direction(b, t.g[at], t.m[at]) : t.g[at];
   }
-#pragma unroll 2
-  for (int f = 0; f < 8; ++f) {
-    put_fragment<false>(v64, x_rows(t), x_term(t), word_of(i0, j0, t.nt * 8), t.nt * 8, f, AsIs());
-    put_fragment<true>(v64, x_cols(t, b.turn), x_term(t), word_of(j0, i0, t.mt * 8), t.mt * 8, f, AsIs());
+  const double inverse = inverse_norm(t, reinterpret_cast<double*>(v64));
+#pragma unroll
+  for (int r = 0; r < 16; ++r) v64[t.tall ? at64(lane, wave * 16 + r) : at64(wave * 16 + r, lane)] = (float)(x[r] * inverse);
+  __syncthreads();
+  const int by_rows = t.nt * (kPad / 32), by_cols = t.mt * (kPad / 32);
+#pragma unroll
+  for (int f = 2 * wave; f < 2 * wave + 2; ++f) {
+    put_fragment<false>(v64, x_rows(t), x_term(t), word_of(i0, j0, by_rows), by_rows, f, AsIs());
+    put_fragment<true>(v64, x_cols(t, b.turn), x_term(t), word_of(j0, i0, by_cols), by_cols, f, AsIs());
   }
 }
 
 // ---- products -----------------------------------------------------------------------------------------------------------
-// A block's tile: C[i][j] = sum over `steps` steps (of 16) of rows i of one operand times rows j of the other, handed out
-// as 64 x 64 parts in LDS.  Row tiles of 32 behind the last one read that one again.
+// A block's tile: C[i][j] = sum over `steps` steps (of 32) of rows i of one operand times rows j of the other, handed out
+// as 64 x 64 parts in LDS.  Row tiles behind the last one read that one again.
 struct Operand {
   const uint4* src;
   int64_t term;
   int row_tile;   // first of the tile
   int row_tiles;  // of the operand
   int pitch;      // steps of a row tile
-  __device__ __forceinline__ const uint4* frag(int row, int t, int step) const {
-    return src + t * term + ((int64_t)min(row_tile + row, row_tiles - 1) * pitch + step) * 64;
+  __device__ __forceinline__ const uint4* frag(int row, int t) const {
+    return src + t * term + (int64_t)min(row_tile + row, row_tiles - 1) * pitch * 64;
   }
 };
 
-// Tiles of 32 TM WM x 32 TN WN, a wave 32 TM x 32 TN of them.  A slab is two steps; wave w brings two row tiles of it, 1 KB a
-// load, while the slab before is multiplied.
-template <int TM_, int TN_, int WM_, int WN_>
+// The accumulators of TA x 4 tiles (register q of lane l: row 4 (l / 16) + q, column l % 16), four by four from row tile
+// `first` on, as values in LDS.
+template <int TA>
+__device__ __forceinline__ void spread(const f32x4 (&acc)[TA][4], int first, float* v64) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        v64[at64(i * 16 + (lane >> 4) * 4 + q, j * 16 + (lane & 15))] = acc[first + i][j][q] * (kUnscale * kUnscale);
+}
+
+// Tiles of 16 TA WM x 64 WN, a wave 16 TA x 64 of them.  A slab is one step of both operands, both terms; it goes to LDS by
+// direct loads, 1 KB each, while the slab before is multiplied: wave w brings four row tiles of it.  A wave's row tiles are
+// multiplied in two halves h, in the order  hi_h Bhi, lo_h Bhi, hi_h Blo:  while a half is multiplied the other's fragments
+// are read, Bhi of the next slab while the last products are made, Blo while the first are.  One barrier a slab, before the
+// last products: behind it the next slab is there, and this one's place is free for the one after.
+// RING slabs in LDS, RING - 1 ahead: four where a CU has one tile only and nothing else to do while a slab is on its way.
+template <int TA_, int WM_, int WN_, int RING_>
 struct SlabTile {
-  static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, WAVES = WM * WN, THREADS = 64 * WAVES;
-  static constexpr int BM = 32 * TM * WM, BN = 32 * TN * WN;
-  static constexpr int ROWS = TM * WM + TN * WN;  // row tiles of both operands
-  static constexpr int WORDS = ROWS * 256;        // of a slab
-  static constexpr size_t LDS = 2 * WORDS * 16;
-  static_assert(ROWS == 2 * WAVES && TM % 2 == 0 && TN == 2, "two row tiles a wave, parts of 64 x 64");
+  static constexpr int TA = TA_, WM = WM_, WN = WN_, RING = RING_, WAVES = WM * WN, THREADS = 64 * WAVES;
+  static constexpr int BM = 16 * TA * WM, BN = 64 * WN;
+  static constexpr int ROWS = TA * WM + 4 * WN;  // row tiles of both operands
+  static constexpr int WORDS = ROWS * 128;       // of a slab
+  static constexpr size_t LDS = RING * WORDS * 16;
+  static_assert(ROWS == 4 * WAVES && TA % 4 == 0, "four row tiles a wave, parts of 64 x 64");
   static_assert(LDS >= WAVES * 64 * 64 * 4, "the parts fit the slabs' memory");
 
   // part(v64, i0, j0, f0, f1): a 64 x 64 part at (i0, j0) within the tile, for one wave: fragments 0 .. 8 are its own
   template <typename F>
   __device__ static __forceinline__ void run(const Operand& a, const Operand& b, int steps, uint4* smem, F part) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint4* src[2][2];  // [row tile][term]
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint4* src[4][2];  // [row tile][term]: wave-uniform
 #pragma unroll
-    for (int r = 0; r < 2; ++r)
+    for (int r = 0; r < 4; ++r)
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const int row = 2 * wave + r;
-        src[r][t] = (row < TM * WM ? a.frag(row, t, 0) : b.frag(row - TM * WM, t, 0)) + lane;
+        const int row = 4 * wave + r;
+        src[r][t] = row < TA * WM ? a.frag(row, t) : b.frag(row - TA * WM, t);
       }
-    auto stage = [&](int sl, uint4* buf) {
-#pragma unroll
-      for (int r = 0; r < 2; ++r)
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int s = 0; s < 2; ++s)
-            load_to_lds16(src[r][t] + (2 * sl + s) * 64, buf + (((2 * wave + r) * 2 + t) * 2 + s) * 64);
+    auto stage = [&](int s, int n) {  // load n of eight of slab s (behind the last: that one again, for nobody)
+      load_to_lds16(src[n / 2][n % 2] + (int64_t)min(s, steps - 1) * 64, lane * 16,
+                    smem + (s % RING) * WORDS + (4 * wave * 2 + n) * 64);
     };
-    const int ra = (wave % WM) * TM, rb = TM * WM + (wave / WM) * TN;
-    f32x16 acc[TM][TN];
-    zero_acc<TM, TN>(acc);
-    const int slabs = (steps + 1) / 2;
-    stage(0, smem);
-    for (int sl = 0; sl < slabs; ++sl) {
-      const uint4* const buf = smem + (sl & 1) * WORDS + lane;
-      __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): this wave's share of the slab has landed
-      __syncthreads();                     // everyone's has, and the other buffer is free
-      if (sl + 1 < slabs) stage(sl + 1, smem + ((sl + 1) & 1) * WORDS);
+    constexpr int H = TA / 2, LEFT = 8 * (RING - 2);  // loads that may be on their way when the next slab has to be there
+    constexpr int WAIT = 0x0F70 | (LEFT & 15) | (LEFT >> 4) << 14;  // vmcnt(LEFT)
+    const int ra = (wave % WM) * TA, rb = TA * WM + (wave / WM) * 4;
+    f32x4 acc[TA][4];
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        uint4 fa[2][TM], fb[2][TN];
+    for (int i = 0; i < TA; ++i)
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
+      for (int j = 0; j < 4; ++j) acc[i][j] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    uint4 fa[2][2][H], fb[2][4];  // [half][term], [term]
+    auto read_a = [&](int s, int h) {
+      const uint4* const buf = smem + (s % RING) * WORDS + lane;
 #pragma unroll
-          for (int i = 0; i < TM; ++i) fa[t][i] = buf[(((ra + i) * 2 + t) * 2 + s) * 64];
+      for (int t = 0; t < 2; ++t)
 #pragma unroll
-          for (int j = 0; j < TN; ++j) fb[t][j] = buf[(((rb + j) * 2 + t) * 2 + s) * 64];
+        for (int i = 0; i < H; ++i) fa[h][t][i] = buf[((ra + h * H + i) * 2 + t) * 64];
+    };
+    auto read_b = [&](int s, int t) {
+      const uint4* const buf = smem + (s % RING) * WORDS + lane;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) fb[t][j] = buf[((rb + j) * 2 + t) * 64];
+    };
+    // loads n0 .. n1 of slab s among the products: one waits its turn behind those of the other waves, and the matrix cores
+    // are not to wait with it
+    auto multiply = [&](int h, int ta, int tb, int s, int n0, int n1) {
+      constexpr int PRODUCTS = 4 * H;
+#pragma unroll
+      for (int n = 0; n < PRODUCTS; ++n) {
+        const int i = n / 4, j = n % 4;
+        acc[h * H + i][j] = mfma_f16(fa[h][ta][i], fb[tb][j], acc[h * H + i][j]);
+        if (n1 > n0 && n % (PRODUCTS / 2) == PRODUCTS / 2 - 1 && n0 + n / (PRODUCTS / 2) < n1) {
+          __builtin_amdgcn_sched_barrier(0);
+          stage(s, n0 + n / (PRODUCTS / 2));
+          __builtin_amdgcn_sched_barrier(0);
         }
-#pragma unroll
-        for (int p = 0; p < 3; ++p)  // hi hi, hi lo, lo hi: consecutive products go to different accumulators
-#pragma unroll
-          for (int i = 0; i < TM; ++i)
-#pragma unroll
-            for (int j = 0; j < TN; ++j) acc[i][j] = mfma_f16(fa[p == 2][i], fb[p == 1][j], acc[i][j]);
       }
+      __builtin_amdgcn_sched_barrier(0);
+    };
+#pragma unroll
+    for (int s = 0; s < RING - 1; ++s)
+#pragma unroll
+      for (int n = 0; n < 8; ++n) stage(s, n);
+    __builtin_amdgcn_s_waitcnt(WAIT);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    read_b(0, 0), read_a(0, 0);
+    for (int s = 0; s < steps; ++s) {
+      read_b(s, 1);
+      __builtin_amdgcn_sched_barrier(0);
+      multiply(0, 0, 0, s + RING - 1, 0, 2);
+      read_a(s, 1);
+      __builtin_amdgcn_sched_barrier(0);
+      multiply(0, 1, 0, s + RING - 1, 2, 4);
+      multiply(0, 0, 1, s + RING - 1, 4, 6);
+      multiply(1, 0, 0, s + RING - 1, 6, 8);
+      multiply(1, 1, 0, 0, 0, 0);
+      __builtin_amdgcn_s_waitcnt(WAIT);  // this wave's share of the next slab has landed
+      __builtin_amdgcn_s_barrier();      // everyone's has, and everyone has read this one
+      asm volatile("" ::: "memory");
+      read_b(s + 1, 0), read_a(s + 1, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      multiply(1, 0, 1, 0, 0, 0);
     }
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): nothing more is on its way to LDS
     __syncthreads();
     float* const v64 = reinterpret_cast<float*>(smem) + wave * (64 * 64);
 #pragma unroll
-    for (int h = 0; h < TM / 2; ++h) {
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < TN; ++j)
-#pragma unroll
-          for (int q = 0; q < 16; ++q)
-            v64[at64(i * 32 + acc_row(q, lane), j * 32 + (lane & 31))] = acc[2 * h + i][j][q] * (kUnscale * kUnscale);
-      part(v64, (ra / 2 + h) * 64, (wave / WM) * 64, 0, 8);
+    for (int h = 0; h < TA / 4; ++h) {
+      spread(acc, 4 * h, v64);
+      part(v64, (ra / 4 + h) * 64, (wave / WM) * 64, 0, 8);
     }
   }
 };
@@ -310,50 +347,47 @@ struct FewTile {
   // part(v64, 0, 0, f0, f1): the whole tile for every wave, fragments f0 .. f1 are its own
   template <typename F>
   __device__ static __forceinline__ void run(const Operand& a, const Operand& b, int steps, uint4* smem, F part) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint4* src[4][2];  // [row tile of either operand][term]
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint4* src[8][2];  // [row tile of either operand][term]: wave-uniform
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
+    for (int r = 0; r < 8; ++r)
 #pragma unroll
-      for (int t = 0; t < 2; ++t) src[r][t] = (r < 2 ? a.frag(r, t, wave) : b.frag(r - 2, t, wave)) + lane;
-    f32x16 acc[2][2];
-    zero_acc<2, 2>(acc);
-    uint4 f[4][2], g[4][2];
-    auto fetch = [&](int s, uint4 (&to)[4][2]) {  // (the last one again behind the last)
-      const int at = min(s, (steps - 1 - wave) / WAVES) * (WAVES * 64);
+      for (int t = 0; t < 2; ++t) src[r][t] = (r < 4 ? a.frag(r, t) : b.frag(r - 4, t)) + wave * 64;
+    f32x4 acc[4][4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int t = 0; t < 2; ++t) to[r][t] = src[r][t][at];
+      for (int j = 0; j < 4; ++j) acc[i][j] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    uint4 f[8][2], g[8][2];
+    const int mine = wave < steps ? (steps - 1 - wave) / WAVES + 1 : 0;
+    auto fetch = [&](int s, uint4 (&to)[8][2]) {  // (behind the last: that one again)
+      const int64_t at = (int64_t)min(s, mine - 1) * (WAVES * 64);
+#pragma unroll
+      for (int r = 0; r < 8; ++r)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) to[r][t] = (src[r][t] + at)[lane];
     };
-    auto products = [&](const uint4 (&x)[4][2]) {
+    auto products = [&](const uint4 (&x)[8][2]) {
 #pragma unroll
       for (int p = 0; p < 3; ++p)
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-          for (int j = 0; j < 2; ++j) acc[i][j] = mfma_f16(x[i][p == 2], x[2 + j][p == 1], acc[i][j]);
+          for (int j = 0; j < 4; ++j) acc[i][j] = mfma_f16(x[i][p == 2], x[4 + j][p == 1], acc[i][j]);
     };
-    if (wave < steps) {
-      const int mine = (steps - 1 - wave) / WAVES + 1;
+    if (mine > 0) {
       fetch(0, f);
-      for (int s = 0; s < mine; s += 2) {
+      int s = 0;
+      for (; s + 1 < mine; s += 2) {
         fetch(s + 1, g);
         products(f);
-        if (s + 1 == mine) break;
         fetch(s + 2, f);
         products(g);
       }
+      if (s < mine) products(f);
     }
     float* const all = reinterpret_cast<float*>(smem);
-    float* const v64 = all + wave * (64 * 64);
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int q = 0; q < 16; ++q)
-          v64[at64(i * 32 + acc_row(q, lane), j * 32 + (lane & 31))] = acc[i][j][q] * (kUnscale * kUnscale);
+    spread(acc, 0, all + wave * (64 * 64));
     __syncthreads();
     float4* const sums = reinterpret_cast<float4*>(all);  // (the waves' parts lie alike: places are added)
 #pragma unroll
@@ -371,6 +405,34 @@ struct FewTile {
   }
 };
 
+// Consecutive blocks go to the eight XCDs in turn.  Each takes a contiguous eighth of a matrix' tiles, in patches eight tiles
+// wide, so that what its blocks stream at one time is shared in its L2 (34 TB/s; a miss of it is served at 10).
+__device__ __forceinline__ int xcd_item(int block, int total) {
+  const int per = total / 8;
+  return block < per * 8 ? (block % 8) * per + block / 8 : block;
+}
+// Tile `item` of rows x cols ones.
+__device__ __forceinline__ void tile_of(int item, int rows, int cols, int* it, int* jt) {
+  const int band = item / (8 * cols), in = item - band * 8 * cols, wide = min(8, rows - band * 8);
+  *jt = in / wide, *it = band * 8 + in % wide;
+}
+// Tile `item` of those on and above the diagonal (it <= jt) of n x n: bands of eight columns, row by row.
+__device__ __forceinline__ void triangle_of(int item, int n, int* it, int* jt) {
+  int band = 0, wide = min(8, n);
+  for (int in_band; item >= (in_band = wide * band + wide * (wide + 1) / 2);) {
+    item -= in_band;
+    band += 8, wide = min(8, n - band);
+  }
+  if (item < wide * band) {
+    *it = item / wide, *jt = band + item % wide;
+    return;
+  }
+  item -= wide * band;
+  int j = 0;
+  while (item > j) item -= ++j;  // column j of the band's own triangle has j + 1 tiles
+  *it = band + item, *jt = band + j;
+}
+
 // MUON_A: A = X X^T.  MUON_B: B = b A + c A A^T.
 template <typename TILE, int WHAT>
 __global__ __launch_bounds__(TILE::THREADS, 2) void muon_square_kernel(MuonBatch b) {
@@ -378,15 +440,16 @@ __global__ __launch_bounds__(TILE::THREADS, 2) void muon_square_kernel(MuonBatch
   static_assert(TILE::BM == TILE::BN, "the tiles of a symmetric matrix");
   const int at_tensor = tensor_of(b);
   const MuonTensor& t = b.t[at_tensor];
-  int it = blockIdx.x - b.first[at_tensor], jt = 0;
-  while (it > jt) it -= ++jt;  // column jt of the upper triangle has jt + 1 tiles
-  const int pitch = (WHAT == MUON_A ? t.nt : t.mt) * 8, depth = WHAT == MUON_A ? t.large : t.small;
-  Operand x{WHAT == MUON_A ? x_rows(t) : mat_a(t), WHAT == MUON_A ? x_term(t) : a_term(t), it * (TILE::BM / 32), t.mt * 4, pitch};
+  const int tiles = (t.small + TILE::BM - 1) / TILE::BM;
+  int it, jt;
+  triangle_of(xcd_item(blockIdx.x - b.first[at_tensor], tiles * (tiles + 1) / 2), tiles, &it, &jt);
+  const int pitch = (WHAT == MUON_A ? t.nt : t.mt) * (kPad / 32), depth = WHAT == MUON_A ? t.large : t.small;
+  Operand x{WHAT == MUON_A ? x_rows(t) : mat_a(t), WHAT == MUON_A ? x_term(t) : a_term(t), it * (TILE::BM / 16), t.mt * (kPad / 16), pitch};
   Operand y = x;
-  y.row_tile = jt * (TILE::BM / 32);
+  y.row_tile = jt * (TILE::BM / 16);
   uint4* const dst = WHAT == MUON_A ? mat_a(t) : mat_b(t);
-  const int steps = t.mt * 8;
-  TILE::run(x, y, (depth + 15) / 16, smem16, [&](const float* v64, int i1, int j1, int f0, int f1) {
+  const int steps = t.mt * (kPad / 32);
+  TILE::run(x, y, (depth + 31) / 32, smem16, [&](const float* v64, int i1, int j1, int f0, int f1) {
     const int i0 = it * TILE::BM + i1, j0 = jt * TILE::BN + j1;
     if (max(i0, j0) >= t.mt * kPad) return;
     const auto polynomial = [&](float (&v)[8], int64_t word) {
@@ -410,21 +473,23 @@ __global__ __launch_bounds__(TILE::THREADS, 2) void muon_apply_kernel(MuonBatch 
   extern __shared__ uint4 smem16[];
   const int at_tensor = tensor_of(b);
   const MuonTensor& t = b.t[at_tensor];
-  const int tiles_m = (t.small + TILE::BM - 1) / TILE::BM;
-  const int tile = blockIdx.x - b.first[at_tensor], it = tile % tiles_m, jt = tile / tiles_m;
-  const Operand x{mat_b(t), a_term(t), it * (TILE::BM / 32), t.mt * 4, t.mt * 8};
-  const Operand y{x_cols(t, b.turn), x_term(t), jt * (TILE::BN / 32), t.nt * 4, t.mt * 8};
-  TILE::run(x, y, (t.small + 15) / 16, smem16, [&](float* v64, int i1, int j1, int f0, int f1) {
+  const int tiles_m = (t.small + TILE::BM - 1) / TILE::BM, tiles_n = (t.large + TILE::BN - 1) / TILE::BN;
+  int it, jt;
+  tile_of(xcd_item(blockIdx.x - b.first[at_tensor], tiles_m * tiles_n), tiles_m, tiles_n, &it, &jt);
+  const Operand x{mat_b(t), a_term(t), it * (TILE::BM / 16), t.mt * (kPad / 16), t.mt * (kPad / 32)};
+  const Operand y{x_cols(t, b.turn), x_term(t), jt * (TILE::BN / 16), t.nt * (kPad / 16), t.mt * (kPad / 32)};
+  TILE::run(x, y, (t.small + 31) / 32, smem16, [&](float* v64, int i1, int j1, int f0, int f1) {
     const int i0 = it * TILE::BM + i1, j0 = jt * TILE::BN + j1;
     const bool inside = i0 < t.mt * kPad && j0 < t.nt * kPad;  // (the same for all waves that share a part)
     const int lane = threadIdx.x & 63;
-    const int64_t by_rows = word_of(i0, j0, t.nt * 8);
+    const int steps_n = t.nt * (kPad / 32), steps_m = t.mt * (kPad / 32);
+    const int64_t by_rows = word_of(i0, j0, steps_n);
     if (inside) {
 #pragma unroll 2
       for (int f = f0; f < f1; ++f) {  // a X, from X by rows (whose place the same lanes write below)
-        const int row = (f >> 2) * 32 + (lane & 31), k = (f & 3) * 16 + (lane >> 5) * 8;
+        const int row = (f >> 1) * 16 + (lane & 15), k = (f & 1) * 32 + (lane >> 4) * 8;
         float v[8];
-        join8(x_rows(t), x_term(t), by_rows + ((int64_t)(f >> 2) * (t.nt * 8) + (f & 3)) * 64 + lane, v);
+        join8(x_rows(t), x_term(t), by_rows + ((int64_t)(f >> 1) * steps_n + (f & 1)) * 64 + lane, v);
 #pragma unroll
         for (int e = 0; e < 8; e += 4) {
           float4* const p = reinterpret_cast<float4*>(v64 + at64(row, k + e));
@@ -438,8 +503,8 @@ __global__ __launch_bounds__(TILE::THREADS, 2) void muon_apply_kernel(MuonBatch 
     if constexpr (!LAST) {
 #pragma unroll 2
       for (int f = f0; f < f1; ++f) {
-        put_fragment<false>(v64, x_rows(t), x_term(t), by_rows, t.nt * 8, f, AsIs());
-        put_fragment<true>(v64, x_cols(t, b.turn ^ 1), x_term(t), word_of(j0, i0, t.mt * 8), t.mt * 8, f, AsIs());
+        put_fragment<false>(v64, x_rows(t), x_term(t), by_rows, steps_n, f, AsIs());
+        put_fragment<true>(v64, x_cols(t, b.turn ^ 1), x_term(t), word_of(j0, i0, steps_m), steps_m, f, AsIs());
       }
     } else {
       const float step = b.lr * t.factor;
@@ -497,6 +562,8 @@ size_t muon_workspace(int tensors, const int32_t* rows, const int32_t* cols) {
 
 template <typename K, typename N>
 static vcnn_status launch_phase(const char* what, K kernel, MuonBatch* b, int threads, size_t lds, hipStream_t st, N blocks_of) {
+  // the matrices whose blocks take longest first: their larger side stands for both
+  std::stable_sort(b->t, b->t + b->tensors, [](const MuonTensor& x, const MuonTensor& y) { return x.large > y.large; });
   int64_t blocks = 0;
   for (int t = 0; t < b->tensors; ++t) {
     b->first[t] = (unsigned)blocks;
@@ -509,18 +576,48 @@ static vcnn_status launch_phase(const char* what, K kernel, MuonBatch* b, int th
   return check_launch(what);
 }
 
+// Tiles of a phase: of the whole X, or on and above the diagonal.
 template <typename TILE>
-static vcnn_status launch_steps(MuonBatch b, int steps, hipStream_t st) {
-  const auto tiles = [](const MuonTensor& t) { return ceil_div(t.small, TILE::BM) * ceil_div(t.large, TILE::BN); };
-  const auto triangle = [](const MuonTensor& t) { const int64_t n = ceil_div(t.small, TILE::BM); return n * (n + 1) / 2; };
-  for (int i = 0; i < steps; ++i, b.turn ^= 1) {
-    if (vcnn_status s = launch_phase("muon A", muon_square_kernel<TILE, MUON_A>, &b, TILE::THREADS, TILE::LDS, st, triangle)) return s;
-    if (vcnn_status s = launch_phase("muon B", muon_square_kernel<TILE, MUON_B>, &b, TILE::THREADS, TILE::LDS, st, triangle)) return s;
-    if (vcnn_status s = i + 1 < steps ? launch_phase("muon apply", muon_apply_kernel<TILE, false>, &b, TILE::THREADS, TILE::LDS, st, tiles)
-                                      : launch_phase("muon apply", muon_apply_kernel<TILE, true>, &b, TILE::THREADS, TILE::LDS, st, tiles))
-      return s;
+static int64_t tiles_of(const MuonTensor& t, bool triangle) {
+  const int64_t m = ceil_div(t.small, TILE::BM);
+  return triangle ? m * (m + 1) / 2 : m * ceil_div(t.large, TILE::BN);
+}
+using TileDeep = SlabTile<4, 2, 2, 4>;  // 128 x 128, a tile a CU
+using TileTwo = SlabTile<4, 2, 2, 2>;   // 128 x 128, two tiles a CU
+using TileWide = SlabTile<8, 2, 4, 2>;  // 256 x 256
+
+// The tile of a phase, by how many there are for 256 CUs; launch(tile) with its type.  Measured, us a phase (Few / Deep / Two
+// / Wide): X X^T of 1024 x 4096 (36 tiles of 128) 28 / 69 / 96 / 215, of 2048 x 2048 (136) 50 / 45 / 56 / 118; B X of 1024 x 4096
+// (256) 50 / 34 / 39 / 74, of 2048 x 4096 (512) 168 / 115 / 100 / 134, of 4096 x 4096 (1024) 536 / 397 / 361 / 329.
+template <typename F>
+static vcnn_status with_tile(const MuonBatch& b, bool triangle, F launch) {
+  int64_t few = 0, two = 0, wide = 0;
+  for (int t = 0; t < b.tensors; ++t) {
+    few += tiles_of<FewTile>(b.t[t], triangle);
+    two += tiles_of<TileTwo>(b.t[t], triangle);
+    wide += tiles_of<TileWide>(b.t[t], triangle);
   }
-  return VCNN_OK;
+  if (few <= 512) return launch(FewTile());
+  if (two <= 256) return launch(TileDeep());
+  if (wide >= 256) return launch(TileWide());
+  return launch(TileTwo());
+}
+
+template <int WHAT>
+static vcnn_status launch_square(MuonBatch* b, hipStream_t st) {
+  return with_tile(*b, true, [&](auto tile) {
+    using TILE = decltype(tile);
+    return launch_phase("muon square", muon_square_kernel<TILE, WHAT>, b, TILE::THREADS, TILE::LDS, st,
+                        [](const MuonTensor& t) { return tiles_of<TILE>(t, true); });
+  });
+}
+template <bool LAST>
+static vcnn_status launch_apply(MuonBatch* b, hipStream_t st) {
+  return with_tile(*b, false, [&](auto tile) {
+    using TILE = decltype(tile);
+    return launch_phase("muon apply", muon_apply_kernel<TILE, LAST>, b, TILE::THREADS, TILE::LDS, st,
+                        [](const MuonTensor& t) { return tiles_of<TILE>(t, false); });
+  });
 }
 
 vcnn_status launch_muon(const MuonTensor* tensors, int count, float lr, float momentum, int nesterov, float weight_decay,
@@ -529,23 +626,22 @@ vcnn_status launch_muon(const MuonTensor* tensors, int count, float lr, float mo
   b.tensors = count;
   b.lr = lr, b.momentum = momentum, b.nesterov = nesterov, b.keep = 1.f - lr * weight_decay;
   uint4* work = (uint4*)workspace;
-  int64_t tiles128 = 0;
   for (int t = 0; t < b.tensors; ++t) {
     b.t[t] = tensors[t];
     lay_out(&b.t[t]);
     b.t[t].work = work;
     work += work_words(b.t[t]);
-    tiles128 += (int64_t)b.t[t].mt * b.t[t].nt;
   }
   const auto norm_blocks = [](const MuonTensor& t) { return t.norm_blocks; };
-  const auto parts = [](const MuonTensor& t) { return ceil_div(ceil_div(t.small, 64) * ceil_div(t.large, 64), 4); };
+  const auto parts = [](const MuonTensor& t) { return ceil_div(t.small, 64) * ceil_div(t.large, 64); };
   if (vcnn_status s = launch_phase("muon moment", muon_moment_kernel, &b, kThreads, 0, st, norm_blocks)) return s;
   if (vcnn_status s = launch_phase("muon begin", muon_begin_kernel, &b, kThreads, 0, st, parts)) return s;
-  const char* const force = getenv("MUON_TILE");
-  const int tile = force ? atoi(force) : tiles128 <= 128 ? 64 : 128;
-  if (tile == 64) return launch_steps<FewTile>(b, steps, st);
-  if (tile == 256) return launch_steps<SlabTile<4, 2, 2, 4>>(b, steps, st);
-  return launch_steps<SlabTile<2, 2, 2, 2>>(b, steps, st);
+  for (int i = 0; i < steps; ++i, b.turn ^= 1) {
+    if (vcnn_status s = launch_square<MUON_A>(&b, st)) return s;
+    if (vcnn_status s = launch_square<MUON_B>(&b, st)) return s;
+    if (vcnn_status s = i + 1 < steps ? launch_apply<false>(&b, st) : launch_apply<true>(&b, st)) return s;
+  }
+  return VCNN_OK;
 }
 
 }  // namespace vcnn

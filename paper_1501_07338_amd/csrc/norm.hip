@@ -175,6 +175,14 @@ __device__ __forceinline__ float to_i8(float u, float a, float inverse) {
 
 enum { NORM_PLAIN = 0, NORM_I8 = 1, QUANT_I8 = 2 };
 
+// Waves a SIMD of the kernel that keeps nv groups of `group` elements a thread: its registers (the elements, their gain, and
+// two tensors' groups of the next row) are held to it, and no more blocks are launched than that makes resident, for a block
+// that comes later has nothing on its way yet.
+constexpr int waves_for(int nv, int group) {
+  const int registers = nv * (2 * group + 8);
+  return registers <= 24 ? 6 : registers <= 48 ? 4 : registers <= 72 ? 3 : 2;
+}
+
 struct NormArgs {
   const void* x;
   const void* residual;  // null: none
@@ -187,7 +195,7 @@ struct NormArgs {
 };
 
 template <typename T, int MODE, int NV, bool WAVE>
-__global__ __launch_bounds__(WAVE ? kWaveThreads : NV ? kKeptThreads : 1024) void norm_kernel(NormArgs a) {
+__global__ __launch_bounds__(WAVE ? kWaveThreads : NV ? kKeptThreads : 1024, NV ? waves_for(NV, 16 / (int)sizeof(T)) : 4) void norm_kernel(NormArgs a) {
   constexpr int N = Group<T>::N;
   __shared__ RowSums sums;
   const int per_row = WAVE ? 64 : blockDim.x, tid = WAVE ? threadIdx.x & 63 : threadIdx.x;
@@ -198,20 +206,31 @@ __global__ __launch_bounds__(WAVE ? kWaveThreads : NV ? kKeptThreads : 1024) voi
 #pragma unroll
     for (int k = 0; k < NV; ++k) load_gain(a.gain, (k * per_row + tid) * N, cols, gain[k]);
   }
+  const bool added = MODE != QUANT_I8 && a.residual;
+  const int64_t stride = (int64_t)gridDim.x * rows_at_once;
+  int64_t row = (int64_t)blockIdx.x * rows_at_once + (WAVE ? threadIdx.x >> 6 : 0);
+  // a row's groups are on their way while the row before is reduced and written
+  Loose16 px[NV ? NV : 1], pr[NV ? NV : 1];
+  auto fetch = [&](int64_t at) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int c = (k * per_row + tid) * N;
+      if (c >= cols) continue;
+      px[k] = load_group(reinterpret_cast<const T*>(a.x) + at * cols, c, cols);
+      if (added) pr[k] = load_group(reinterpret_cast<const T*>(a.residual) + at * cols, c, cols);
+    }
+  };
+  if (NV > 0 && row < a.rows) fetch(row);
   int turn = 0;
-  for (int64_t row = (int64_t)blockIdx.x * rows_at_once + (WAVE ? threadIdx.x >> 6 : 0); row < a.rows;
-       row += (int64_t)gridDim.x * rows_at_once, turn ^= 1) {
+  for (; row < a.rows; row += stride, turn ^= 1) {
     const T* const x = reinterpret_cast<const T*>(a.x) + row * cols;
-    const T* const r = MODE != QUANT_I8 && a.residual ? reinterpret_cast<const T*>(a.residual) + row * cols : nullptr;
     T* const h = reinterpret_cast<T*>(a.h) + row * cols;
-    // the group at c, the residual added (and stored: with the other tensors' rows still to come from memory, the store is
-    // on its way while the row is reduced)
-    auto take = [&](int c, float (&v)[N]) {
-      const Loose16 px = load_group(x, c, cols);
-      if (!r) return unpack(px, v);
+    // the group at c, the residual added and the sum stored
+    auto take = [&](int c, const Loose16& gx, const Loose16& gr, float (&v)[N]) {
+      unpack(gx, v);
+      if (!added) return;
       float w[N];
-      unpack(px, v);
-      unpack(load_group(r, c, cols), w);
+      unpack(gr, w);
 #pragma unroll
       for (int i = 0; i < N; ++i) v[i] += w[i];
       const Loose16 ph = pack(v);
@@ -234,23 +253,26 @@ __global__ __launch_bounds__(WAVE ? kWaveThreads : NV ? kKeptThreads : 1024) voi
       for (int k = 0; k < NV; ++k) {
         const int c = (k * per_row + tid) * N;
         if (c < cols) {
-          take(c, v[k]);
+          take(c, px[k], pr[k], v[k]);
         } else {
 #pragma unroll
           for (int i = 0; i < N; ++i) v[k][i] = 0.f;
         }
       }
+      if (row + stride < a.rows) fetch(row + stride);
 #pragma unroll
       for (int k = 0; k < NV; ++k) count(v[k], gain[k]);
     } else {
       for (int c = tid * N; c < cols; c += per_row * N) {
-        take(c, v[0]);
+        px[0] = load_group(x, c, cols);
+        if (added) pr[0] = load_group(reinterpret_cast<const T*>(a.residual) + row * cols, c, cols);
+        take(c, px[0], pr[0], v[0]);
         if (MODE == NORM_I8) load_gain(a.gain, c, cols, gain[0]);
         count(v[0], gain[0]);
       }
     }
     row_reduce<WAVE>(sums, turn, sum, most);
-    const T* const kept = r ? h : x;  // (rows read twice: every thread meets its own elements again)
+    const T* const kept = added ? h : x;  // (rows read twice: every thread meets its own elements again)
     float rstd = 1.f;
     if (MODE != QUANT_I8) {
       rstd = 1.f / sqrtf(sum / (float)cols + a.eps);
@@ -312,17 +334,23 @@ struct RowShape {
   int threads;  // of a row
   int blocks;
 };
-static RowShape row_shape(int64_t rows, int cols, int group, int most_blocks) {
+// quarters: rows by four waves where that will do, since blocks of four fill a CU evenly (8192 x 5120: blocks of five 79 us, of
+// four 64); all eight where rows are few and a row's own time counts.
+static RowShape row_shape(int64_t rows, int cols, int group, bool quarters) {
   const int64_t groups = ceil_div(cols, group);
   RowShape s;
   if (groups <= 128) s.nv = groups <= 64 ? 1 : 2, s.threads = 64;
   else if (cols > 32 * kKeptThreads) s.nv = 0, s.threads = 1024;
   else {
-    s.nv = groups <= kKeptThreads ? 1 : groups <= 2 * kKeptThreads ? 2 : groups <= 4 * kKeptThreads ? 4 : 8;
-    s.threads = (int)ceil_div(ceil_div(groups, s.nv), 64) * 64;
+    const int most = quarters && rows > 512 && groups <= 4 * 256 ? 256 : kKeptThreads;
+    s.nv = (int)ceil_div(groups, most);
+    if (s.nv > 4) s.nv = s.nv <= 6 ? 6 : 8;
+    s.threads = most == 256 ? 256 : (int)ceil_div(ceil_div(groups, s.nv), 64) * 64;
   }
   const int64_t blocks = s.threads == 64 ? ceil_div(rows, kWaveThreads / 64) : rows;
-  s.blocks = (int)std::min<int64_t>(blocks, most_blocks);
+  const int waves = s.threads == 64 ? kWaveThreads / 64 : s.threads / 64;
+  const int resident = s.nv ? std::max(2, 4 * waves_for(s.nv, group) / waves) : 2;
+  s.blocks = (int)std::min<int64_t>(blocks, 256 * resident);
   return s;
 }
 
@@ -336,13 +364,17 @@ static void with_shape(const RowShape& s, F launch) {
   } else if (s.nv == 0) launch(integral_constant<int, 0>(), std::false_type());
   else if (s.nv == 1) launch(integral_constant<int, 1>(), std::false_type());
   else if (s.nv == 2) launch(integral_constant<int, 2>(), std::false_type());
+  else if (s.nv == 3) launch(integral_constant<int, 3>(), std::false_type());
   else if (s.nv == 4) launch(integral_constant<int, 4>(), std::false_type());
-  else if constexpr (Group<T>::N == 4) launch(integral_constant<int, 8>(), std::false_type());
+  else if constexpr (Group<T>::N == 4) {  // (32 elements a thread at most)
+    if (s.nv == 6) launch(integral_constant<int, 6>(), std::false_type());
+    else launch(integral_constant<int, 8>(), std::false_type());
+  }
 }
 
 template <typename T, int MODE>
 static void launch_norm_typed(const NormArgs& a, hipStream_t st) {
-  const RowShape s = row_shape(a.rows, a.cols, Group<T>::N, 4096);
+  const RowShape s = row_shape(a.rows, a.cols, Group<T>::N, true);
   with_shape<T>(s, [&](auto nv, auto wave) {
     hipLaunchKernelGGL((norm_kernel<T, MODE, decltype(nv)::value, decltype(wave)::value>), dim3(s.blocks),
                        dim3(s.threads == 64 ? kWaveThreads : s.threads), 0, st, a);
@@ -507,18 +539,21 @@ __global__ __launch_bounds__(WAVE ? kWaveThreads : NV ? kKeptThreads : 1024) voi
   }
 }
 
-// dg[c] = the blocks' shares: sixteen threads a column take every sixteenth, their sums are added in order.
+// dg[c] = the blocks' shares: 64 threads a column take every 64th, and their sums are added in pairs, always the same ones.
 __global__ __launch_bounds__(1024) void gain_grad_kernel(const float* partial, float* dg, int blocks, int cols) {
-  __shared__ float sums[16][64];
-  const int col = blockIdx.x * 64 + (threadIdx.x & 63), part = threadIdx.x >> 6;
+  __shared__ float sums[64][17];
+  const int in = threadIdx.x & 15, col = blockIdx.x * 16 + in, part = threadIdx.x >> 4;
   float s = 0.f;
-  if (col < cols)
-    for (int b = part; b < blocks; b += 16) s += partial[(int64_t)b * cols + col];
-  sums[part][threadIdx.x & 63] = s;
-  __syncthreads();
-  if (part != 0 || col >= cols) return;
-  for (int p = 1; p < 16; ++p) s += sums[p][threadIdx.x & 63];
-  dg[col] = s;
+  if (col < cols) {
+#pragma unroll 8
+    for (int b = part; b < blocks; b += 64) s += partial[(int64_t)b * cols + col];
+  }
+  sums[part][in] = s;
+  for (int n = 32; n > 0; n >>= 1) {
+    __syncthreads();
+    if (part < n) sums[part][in] += sums[part + n][in];
+  }
+  if (part == 0 && col < cols) dg[col] = sums[0][in];
 }
 
 size_t rmsnorm_bwd_partial_bytes(int rows, int cols) {
@@ -527,7 +562,8 @@ size_t rmsnorm_bwd_partial_bytes(int rows, int cols) {
 
 template <typename T>
 static int launch_norm_bwd_typed(const NormBwdArgs& a, hipStream_t st) {
-  const RowShape s = row_shape(a.rows, a.cols, Group<T>::N, kNormBwdBlocks);
+  RowShape s = row_shape(a.rows, a.cols, Group<T>::N, false);
+  s.blocks = std::min(s.blocks, kNormBwdBlocks);
   with_shape<T>(s, [&](auto nv, auto wave) {
     hipLaunchKernelGGL((norm_bwd_kernel<T, decltype(nv)::value, decltype(wave)::value>), dim3(s.blocks),
                        dim3(s.threads == 64 ? kWaveThreads : s.threads), 0, st, a);
@@ -541,7 +577,7 @@ vcnn_status launch_rmsnorm_bwd(int dtype, int rows, int cols, const void* h, con
   const int blocks = dtype == VCNN_BF16 ? launch_norm_bwd_typed<bf16>(a, st) : launch_norm_bwd_typed<float>(a, st);
   if (vcnn_status s = check_launch("rmsnorm_bwd")) return s;
   if (!dgain) return VCNN_OK;
-  hipLaunchKernelGGL(gain_grad_kernel, dim3((unsigned)ceil_div(cols, 64)), dim3(1024), 0, st, partial, dgain, blocks, cols);
+  hipLaunchKernelGGL(gain_grad_kernel, dim3((unsigned)ceil_div(cols, 16)), dim3(1024), 0, st, partial, dgain, blocks, cols);
   return check_launch("rmsnorm_bwd gain");
 }
 

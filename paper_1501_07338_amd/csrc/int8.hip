@@ -5,7 +5,8 @@
 // by the two scales and rounded once more to the type of y.
 //
 // Three kernels.  One or two samples: dot products of whole rows (i8_dot_kernel; 4096 -> 16384 in 12.2 us with the call's own
-// 6, the matrix cores' kernel 15.1).  Up to 64: the weights are read once and nothing of them is reused, so a block owns 16
+// 6, the matrix cores' kernel 15.1).  Up to 32, or 128 where the layer
+// is small: the weights are read once and nothing of them is reused, so a block owns 16
 // outputs, its eight waves take every eighth 128 bytes of the rows and feed the matrix cores from global memory, all operands
 // of four such steps in flight at once (i8_rows_kernel).  More: tiles of 256 x 256 or 128 x 128 from slabs of 64 bytes of
 // both operands in LDS (i8_tile_kernel), the contraction divided over blocks where the tiles alone do not fill the chip;
@@ -185,7 +186,7 @@ static constexpr int kRowsThreads = 512;
 
 template <typename T, int NB>
 __global__ __launch_bounds__(kRowsThreads) void i8_rows_kernel(I8Args a) {
-  constexpr int AHEAD = 4, WAVES = kRowsThreads / 64;
+  constexpr int AHEAD = NB <= 4 ? 4 : 2, WAVES = kRowsThreads / 64;
   __shared__ int share[WAVES - 1][NB][4][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int o0 = blockIdx.x * 16, row = lane & 15, at = (lane >> 4) * 32;
@@ -258,11 +259,12 @@ __global__ __launch_bounds__(kRowsThreads) void i8_rows_kernel(I8Args a) {
 // ---- tiles -------------------------------------------------------------------------------------------------------------
 // BO outputs x BB samples by waves of 16 TO x 16 TB, on the 16 x 16 x 64 form: with operands in registers it reaches 4.2 POP/s
 // on this card, the 32 x 32 x 32 form 2.7.
-template <int BO_, int BB_, int TO_, int TB_, int RING_>
+template <int BO_, int BB_, int TO_, int TB_, int RING_, bool AHEAD_>
 struct I8Tile {
   static constexpr int BO = BO_, BB = BB_, TO = TO_, TB = TB_;
   static constexpr int WO = BO / (16 * TO), THREADS = WO * (BB / (16 * TB)) * 64, WAVES = THREADS / 64;
   static constexpr int RING = RING_;                 // slabs in LDS
+  static constexpr bool AHEAD = AHEAD_;              // a wave reads a whole step ahead (else half a one)
   static constexpr int WORDS = (BO + BB) * 4;        // 16-byte words of a slab of 64 bytes a row
   static constexpr size_t LDS = (size_t)RING * WORDS * 16;
   static constexpr int LO = BO * 4 / THREADS, LB = BB * 4 / THREADS;  // words a thread brings of one
@@ -380,54 +382,63 @@ __global__ __launch_bounds__(TILE::THREADS, 2) void i8_tile_kernel(I8Args a) {
     for (int j = 0; j < TB; ++j) acc[i][j] = (i32x4){0, 0, 0, 0};
   const int wo = (wave % TILE::WO) * 16 * TO, wb = (wave / TILE::WO) * 16 * TB;
   const int mine = (lane & 15) * 4 + ((lane >> 4) ^ swizzle(lane & 15));  // this lane's word of a 16-row tile
-  uint4 fo[2][TO / 2], fb[2][TB];
-  auto read_o = [&](int s, int h) {
+  constexpr bool AHEAD = TILE::AHEAD;
+  constexpr int H = AHEAD ? TO : TO / 2;  // row tiles of a set of fragments
+  uint4 fo[2][H], fb[2][TB];
+  auto read_o = [&](int s, int p, int first) {
     const uint4* const buf = smem16 + (s % TILE::RING) * TILE::WORDS + mine;
 #pragma unroll
-    for (int i = 0; i < TO / 2; ++i) fo[h][i] = buf[(wo + (h * (TO / 2) + i) * 16) * 4];
+    for (int i = 0; i < H; ++i) fo[p][i] = buf[(wo + (first + i) * 16) * 4];
   };
   auto read_b = [&](int s, int p) {
     const uint4* const buf = smem16 + (s % TILE::RING) * TILE::WORDS + mine;
 #pragma unroll
     for (int j = 0; j < TB; ++j) fb[p][j] = buf[(TILE::BO + wb + j * 16) * 4];
   };
-  // The products of one half, slab s's share of the loads among them: a load waits its turn behind those of the other waves,
-  // and the matrix cores are not to wait with it.
-  auto multiply = [&](int h, int p, int s) {
-    constexpr int PRODUCTS = TO / 2 * TB, EVERY = PRODUCTS / (L / 2);
-    static_assert(L % 2 == 0 && PRODUCTS % (L / 2) == 0, "loads spread evenly");
+  // The products of set po, loads l0 .. l1 of slab s among them: a load waits its turn behind those of the other waves, and the
+  // matrix cores are not to wait with it.
+  auto multiply = [&](int first, int po, int pb, int s, int l0, int l1) {
+    const int every = H * TB / (l1 - l0);
 #pragma unroll
-    for (int n = 0; n < PRODUCTS; ++n) {
+    for (int n = 0; n < H * TB; ++n) {
       const int i = n / TB, j = n % TB;
-      acc[h * (TO / 2) + i][j] = mfma_i8(fo[h][i], fb[p][j], acc[h * (TO / 2) + i][j]);
-      if (n % EVERY == EVERY / 2) {
+      acc[first + i][j] = mfma_i8(fo[po][i], fb[pb][j], acc[first + i][j]);
+      if (n % every == every / 2) {
         __builtin_amdgcn_sched_barrier(0);
-        stage(s, h * (L / 2) + n / EVERY);
+        stage(s, l0 + n / every);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
   };
   constexpr int R = TILE::RING;
-  static_assert((R - 2) * L < 16, "the counts fit");
+  static_assert((R - 2) * L < 64, "the counts fit");
+  constexpr auto all_but = [](int n) { return 0x0F70 | (n & 15) | n >> 4 << 14; };  // vmcnt(n)
 #pragma unroll
   for (int s = 0; s < R - 1; ++s)
 #pragma unroll
     for (int i = 0; i < L; ++i) stage(s, i);
-  __builtin_amdgcn_s_waitcnt(0x0F70 | (R - 2) * L);  // all but the last R - 2 slabs' loads
+  __builtin_amdgcn_s_waitcnt(all_but((R - 2) * L));
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
-  read_b(0, 0), read_o(0, 0);
+  read_b(0, 0), read_o(0, 0, 0);
   auto step = [&](int s, int p) {
-    __builtin_amdgcn_s_waitcnt(0x0F70 | (R - 3) * L);  // slab s + 1 is there, for everyone; slab s - 1 has been read by everyone
+    // slab s + 1 is there, for everyone; slab s - 1 has been read by everyone
+    __builtin_amdgcn_s_waitcnt(all_but((R - 3) * L));
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    read_o(s, 1);
-    __builtin_amdgcn_sched_barrier(0);
-    multiply(0, p, s + R - 1);
-    __builtin_amdgcn_sched_barrier(0);
-    read_b(s + 1, p ^ 1), read_o(s + 1, 0);
-    __builtin_amdgcn_sched_barrier(0);
-    multiply(1, p, s + R - 1);
+    if constexpr (AHEAD) {
+      read_b(s + 1, p ^ 1), read_o(s + 1, p ^ 1, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      multiply(0, p, p, s + R - 1, 0, L);
+    } else {
+      read_o(s, 1, H);
+      __builtin_amdgcn_sched_barrier(0);
+      multiply(0, 0, p, s + R - 1, 0, L / 2);
+      __builtin_amdgcn_sched_barrier(0);
+      read_b(s + 1, p ^ 1), read_o(s + 1, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      multiply(H, 1, p, s + R - 1, L / 2, L);
+    }
     __builtin_amdgcn_sched_barrier(0);
   };
   for (int s = 0; s < slabs; s += 2) {
@@ -527,22 +538,28 @@ struct I8Plan {
 
 static I8Plan i8_plan(int batch, int k, int out, size_t budget) {
   I8Plan p{};
-  // 33 to 64 samples: with 16 Mi weights (4096 x 4096) 13 us without tiles and 18 with them, with 64 Mi 39 and 30
-  if (batch <= 32 || (batch <= 64 && (int64_t)k * out <= 1 << 25)) {
-    p.few = batch <= 16 ? 1 : batch <= 32 ? 2 : 4;
+  // Without tiles or with them, us: 64 samples of 16 Mi weights (4096 x 4096) 13 and 16, of 64 Mi 28 and 25; 65 samples of 1 Mi
+  // 8 and 10, of 4 Mi 15 and 14.
+  const int64_t weights = (int64_t)k * out;
+  if (batch <= 32 || (batch <= 64 && weights <= 1 << 25) || (batch <= 128 && weights <= 1 << 20)) {
+    p.few = batch <= 16 ? 1 : batch <= 32 ? 2 : batch <= 64 ? 4 : 8;
     return p;
   }
-  const int64_t big = ceil_div(batch, 256) * ceil_div(out, 256);
-  p.tile = big >= 192 ? 256 : 128;
-  const int64_t tiles = ceil_div(batch, p.tile) * ceil_div(out, p.tile);
   const int slabs = (int)ceil_div(k, 64);
-  const int64_t room = p.tile == 256 ? 256 : 512;  // blocks resident at once
-  int splits = 1;
-  if (tiles * 2 <= room) splits = (int)std::min<int64_t>({room / tiles, slabs / 8, 16});
-  splits = std::max(splits, 1);
-  while (splits > 1 && (size_t)splits * batch * out * 4 > budget) --splits;
-  p.slabs_per_split = (int)ceil_div(slabs, splits);
-  p.splits = (int)ceil_div(slabs, p.slabs_per_split);
+  p.tile = ceil_div(batch, 256) * ceil_div(out, 256) >= 192 ? 256 : 128;  // (1024 4096 -> 16384, 256 large tiles: 75 us either way)
+  p.splits = 1, p.slabs_per_split = slabs;
+  if (p.tile == 256) return p;
+  // How many blocks share a sum: a slab takes a CU's one block 0.28 us and each further round of 256 blocks as long, the
+  // join 4 us and the time of the shares, written and read at some 3.3 TB/s (within 10 % of what 65 to 512 samples took,
+  // 1024 x 1024 to 8192 x 8192).
+  const int64_t tiles = ceil_div(batch, 128) * ceil_div(out, 128);
+  const double share = (double)batch * out * 4;
+  double best = 0.28 * slabs * ceil_div(tiles, 256);
+  for (int n = 2; n <= 16 && n * 4 <= slabs && n * share <= (double)budget; ++n) {
+    const int each = (int)ceil_div(slabs, n), real = (int)ceil_div(slabs, each);
+    const double us = 0.28 * each * ceil_div(tiles * real, 256) + 4 + real * share * 2 / 3.3e6;
+    if (us < best) best = us, p.splits = real, p.slabs_per_split = each;
+  }
   if (p.splits > 1) p.workspace_bytes = (size_t)p.splits * batch * out * 4;
   return p;
 }
@@ -566,14 +583,15 @@ static vcnn_status launch_fc_i8_typed(I8Args a, void* workspace, size_t bytes, h
     else if (a.batch == 2) hipLaunchKernelGGL((i8_dot_kernel<T, 2>), grid, dim3(256), 0, st, a);
     else if (p.few == 1) hipLaunchKernelGGL((i8_rows_kernel<T, 1>), grid, dim3(kRowsThreads), 0, st, a);
     else if (p.few == 2) hipLaunchKernelGGL((i8_rows_kernel<T, 2>), grid, dim3(kRowsThreads), 0, st, a);
-    else hipLaunchKernelGGL((i8_rows_kernel<T, 4>), grid, dim3(kRowsThreads), 0, st, a);
+    else if (p.few == 4) hipLaunchKernelGGL((i8_rows_kernel<T, 4>), grid, dim3(kRowsThreads), 0, st, a);
+    else hipLaunchKernelGGL((i8_rows_kernel<T, 8>), grid, dim3(kRowsThreads), 0, st, a);
     return check_launch("fc_fwd_i8");
   }
   a.tiles_b = (int)ceil_div(a.batch, p.tile), a.tiles_o = (int)ceil_div(a.out, p.tile);
   a.slabs_per_split = p.slabs_per_split;
   a.partial = p.splits > 1 ? (int32_t*)workspace : nullptr;
-  if (p.tile == 256) launch_tile<T, I8Tile<256, 256, 8, 4, 4>>(a, p, st);
-  else launch_tile<T, I8Tile<128, 128, 4, 4, 4>>(a, p, st);
+  if (p.tile == 256) launch_tile<T, I8Tile<256, 256, 8, 4, 4, false>>(a, p, st);
+  else launch_tile<T, I8Tile<128, 128, 4, 2, 4, true>>(a, p, st);
   if (vcnn_status s = check_launch("fc_fwd_i8")) return s;
   if (p.splits == 1) return VCNN_OK;
   hipLaunchKernelGGL((i8_join_kernel<T>), dim3((unsigned)ceil_div(ceil_div(a.out, 4) * a.batch, 256)), dim3(256), 0, st, a,

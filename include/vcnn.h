@@ -303,7 +303,7 @@ vcnn_status vcnn_orthogonalize(int32_t rows, int32_t cols, int32_t steps, const 
  * are HOST arrays of length `tensors` holding sizes and DEVICE pointers; they are read before the call returns.  w_bf16 may be
  * NULL; a non-NULL w_bf16[t] receives the updated tensor rounded to bfloat16.  No two tensors may overlap.  lr, momentum and
  * weight_decay must be finite, steps 1 to 32.  workspace: vcnn_muon_workspace_bytes, three to five times the bytes of the
- * (first sixteen) matrices, their sides rounded up to multiples of 128. */
+ * (largest sixteen in a row) matrices, their sides rounded up to multiples of 128, and 4 MiB. */
 vcnn_status vcnn_muon_workspace_bytes(int32_t tensors, const int32_t* rows, const int32_t* cols, size_t* bytes);
 vcnn_status vcnn_muon_update_multi(int32_t tensors, const int32_t* rows, const int32_t* cols, float* const* w,
                                    const float* const* dw, float* const* m, void* const* w_bf16, float lr, float momentum,

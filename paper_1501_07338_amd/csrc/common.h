@@ -503,6 +503,7 @@ struct MuonTensor {
   int rows, cols;
   // set by the launch: smaller and larger side, 128-tiles along them, this matrix' part of the workspace
   int tall, small, large, mt, nt, norm_blocks;
+  int parts;           // blocks that share a sum
   uint4* work;
 };
 size_t muon_workspace(int tensors, const int32_t* rows, const int32_t* cols);

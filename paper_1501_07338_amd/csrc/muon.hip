@@ -35,6 +35,8 @@ namespace vcnn {
 
 static constexpr int kThreads = 256;
 static constexpr int kNormBlocks = 1024;  // of a matrix, at most
+static constexpr int kJoinBlocks = 256;  // of a phase whose sums are shared by several blocks
+static constexpr int kSharedSteps = 64;  // of the longest, from which on sums are shared
 static constexpr int kPad = 128;         // sides in the workspace are multiples of it
 static constexpr float kScale = 16384.f, kUnscale = 1.f / kScale;  // 2^14 * 2.81 < 65504
 static constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
@@ -49,6 +51,7 @@ struct MuonBatch {
   float momentum, keep, lr;  // keep = 1 - lr * weight decay
   int nesterov;
   int turn;                  // which of the two copies of X by columns is read
+  float* shares;             // [kJoinBlocks][64 * 64]: sums of blocks that share a tile
 };
 
 // The buffers of a matrix in the workspace, in 16-byte words (terms: hi, then lo).
@@ -339,7 +342,10 @@ struct SlabTile {
   }
 };
 
-// A tile of 64 x 64, every eighth step a wave's; the waves' sums are added in order.
+// A tile of 64 x 64, every eighth step a wave's; the waves' sums are added in order.  A wave's fragments come at the rate of the
+// CU's cache, a step of all eight in a microsecond, so where a few tiles have long sums each is shared by several blocks, which
+// leave theirs in memory to a kernel of their own (muon_join_kernel; the last block to arrive adding them by itself was slower
+// than no sharing: its fences write all of an L2 back).
 struct FewTile {
   static constexpr int WAVES = 8, THREADS = 512, BM = 64, BN = 64;
   static constexpr size_t LDS = WAVES * 64 * 64 * 4;
@@ -347,12 +353,19 @@ struct FewTile {
   // part(v64, 0, 0, f0, f1): the whole tile for every wave, fragments f0 .. f1 are its own
   template <typename F>
   __device__ static __forceinline__ void run(const Operand& a, const Operand& b, int steps, uint4* smem, F part) {
+    sum(a, b, 0, steps, smem);
+    __syncthreads();
+    const int wave = threadIdx.x >> 6;
+    part(reinterpret_cast<float*>(smem), 0, 0, wave, wave + 1);
+  }
+  // Steps s0 .. s0 + steps, as values in LDS; every thread writes places n * 512 + threadIdx.x (of four values), n < 2.
+  __device__ static __forceinline__ void sum(const Operand& a, const Operand& b, int s0, int steps, uint4* smem) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint4* src[8][2];  // [row tile of either operand][term]: wave-uniform
 #pragma unroll
     for (int r = 0; r < 8; ++r)
 #pragma unroll
-      for (int t = 0; t < 2; ++t) src[r][t] = (r < 4 ? a.frag(r, t) : b.frag(r - 4, t)) + wave * 64;
+      for (int t = 0; t < 2; ++t) src[r][t] = (r < 4 ? a.frag(r, t) : b.frag(r - 4, t)) + (int64_t)(s0 + wave) * 64;
     f32x4 acc[4][4];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -400,8 +413,6 @@ struct FewTile {
       }
       sums[n * 512 + threadIdx.x] = v;
     }
-    __syncthreads();
-    part(all, 0, 0, wave, wave + 1);
   }
 };
 
@@ -433,6 +444,27 @@ __device__ __forceinline__ void triangle_of(int item, int n, int* it, int* jt) {
   *it = band + item, *jt = band + j;
 }
 
+// A 64 x 64 part of A (MUON_A: the values themselves) or B (MUON_B: b A + c times the values) at (i0, j0), and at (j0, i0) where
+// that is another place: fragments f0 .. f1.
+template <int WHAT>
+__device__ __forceinline__ void put_symmetric(const MuonTensor& t, const float* v64, int i0, int j0, bool both, int f0, int f1) {
+  if (max(i0, j0) >= t.mt * kPad) return;
+  uint4* const dst = WHAT == MUON_A ? mat_a(t) : mat_b(t);
+  const int steps = t.mt * (kPad / 32);
+  const auto polynomial = [&](float (&v)[8], int64_t word) {
+    if (WHAT == MUON_A) return;
+    float a8[8];
+    join8(mat_a(t), a_term(t), word, a8);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = fmaf(kC, v[e], kB * a8[e]);
+  };
+#pragma unroll 2
+  for (int f = f0; f < f1; ++f) {
+    put_fragment<false>(v64, dst, a_term(t), word_of(i0, j0, steps), steps, f, polynomial);
+    if (both) put_fragment<true>(v64, dst, a_term(t), word_of(j0, i0, steps), steps, f, polynomial);
+  }
+}
+
 // MUON_A: A = X X^T.  MUON_B: B = b A + c A A^T.
 template <typename TILE, int WHAT>
 __global__ __launch_bounds__(TILE::THREADS, 2) void muon_square_kernel(MuonBatch b) {
@@ -447,24 +479,54 @@ __global__ __launch_bounds__(TILE::THREADS, 2) void muon_square_kernel(MuonBatch
   Operand x{WHAT == MUON_A ? x_rows(t) : mat_a(t), WHAT == MUON_A ? x_term(t) : a_term(t), it * (TILE::BM / 16), t.mt * (kPad / 16), pitch};
   Operand y = x;
   y.row_tile = jt * (TILE::BM / 16);
-  uint4* const dst = WHAT == MUON_A ? mat_a(t) : mat_b(t);
-  const int steps = t.mt * (kPad / 32);
   TILE::run(x, y, (depth + 31) / 32, smem16, [&](const float* v64, int i1, int j1, int f0, int f1) {
-    const int i0 = it * TILE::BM + i1, j0 = jt * TILE::BN + j1;
-    if (max(i0, j0) >= t.mt * kPad) return;
-    const auto polynomial = [&](float (&v)[8], int64_t word) {
-      if (WHAT == MUON_A) return;
-      float a8[8];
-      join8(mat_a(t), a_term(t), word, a8);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = fmaf(kC, v[e], kB * a8[e]);
-    };
-#pragma unroll 2
-    for (int f = f0; f < f1; ++f) {
-      put_fragment<false>(v64, dst, a_term(t), word_of(i0, j0, steps), steps, f, polynomial);
-      if (it != jt) put_fragment<true>(v64, dst, a_term(t), word_of(j0, i0, steps), steps, f, polynomial);
-    }
+    put_symmetric<WHAT>(t, v64, it * TILE::BM + i1, jt * TILE::BN + j1, it != jt, f0, f1);
   });
+}
+
+// A = X X^T where t.parts blocks share a tile's steps: their sums ...
+__global__ __launch_bounds__(FewTile::THREADS, 2) void muon_share_kernel(MuonBatch b) {
+  extern __shared__ uint4 smem16[];
+  const int at_tensor = tensor_of(b);
+  const MuonTensor& t = b.t[at_tensor];
+  const int block = blockIdx.x - b.first[at_tensor], part = block % t.parts, tiles = (t.small + 63) / 64;
+  int it, jt;
+  triangle_of(block / t.parts, tiles, &it, &jt);
+  Operand x{x_rows(t), x_term(t), it * 4, t.mt * (kPad / 16), t.nt * (kPad / 32)};
+  Operand y = x;
+  y.row_tile = jt * 4;
+  const int steps = (t.large + 31) / 32;
+  const int s0 = (int)((int64_t)steps * part / t.parts), s1 = (int)((int64_t)steps * (part + 1) / t.parts);
+  FewTile::sum(x, y, s0, s1 - s0, smem16);
+#pragma unroll
+  for (int n = 0; n < 2; ++n)
+    reinterpret_cast<float4*>(b.shares)[blockIdx.x * 1024 + n * 512 + threadIdx.x] = reinterpret_cast<const float4*>(smem16)[n * 512 + threadIdx.x];
+}
+// ... and their join, a block a tile, in the order of the blocks.
+__global__ __launch_bounds__(FewTile::THREADS) void muon_join_kernel(MuonBatch b) {
+  __shared__ __attribute__((aligned(16))) float v64[64 * 64];
+  int tile = blockIdx.x, at_tensor = 0, n = 0;
+  for (;; ++at_tensor, tile -= n) {
+    n = (b.first[at_tensor + 1] - b.first[at_tensor]) / b.t[at_tensor].parts;
+    if (tile < n) break;
+  }
+  const MuonTensor& t = b.t[at_tensor];
+  const float4* const from = reinterpret_cast<const float4*>(b.shares) + (int64_t)(b.first[at_tensor] + tile * t.parts) * 1024 + threadIdx.x;
+  float4 v[2] = {from[0], from[512]};
+#pragma unroll 4
+  for (int p = 1; p < t.parts; ++p)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const float4 u = from[p * 1024 + h * 512];
+      v[h].x += u.x, v[h].y += u.y, v[h].z += u.z, v[h].w += u.w;
+    }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) reinterpret_cast<float4*>(v64)[h * 512 + threadIdx.x] = v[h];
+  __syncthreads();
+  int it, jt;
+  triangle_of(tile, (t.small + 63) / 64, &it, &jt);
+  const int wave = threadIdx.x >> 6;
+  put_symmetric<MUON_A>(t, v64, it * 64, jt * 64, it != jt, wave, wave + 1);
 }
 
 // X <- a X + B X; the last one: the result, or the weights moved by it.
@@ -545,7 +607,11 @@ static void lay_out(MuonTensor* t) {
   t->norm_blocks = (int)std::min<int64_t>(kNormBlocks, ceil_div((int64_t)t->rows * t->cols, 8 * kThreads));
 }
 
+// At the start of the workspace: the shares.
+static constexpr size_t kJoinBytes = (size_t)kJoinBlocks * 64 * 64 * sizeof(float);
+
 size_t muon_workspace(int tensors, const int32_t* rows, const int32_t* cols) {
+  if (tensors == 0) return 0;
   int64_t most = 0;
   for (int t0 = 0; t0 < tensors; t0 += kMuonBatch) {  // batches follow one another in the same memory
     int64_t words = 0;
@@ -557,7 +623,7 @@ size_t muon_workspace(int tensors, const int32_t* rows, const int32_t* cols) {
     }
     most = std::max(most, words);
   }
-  return (size_t)most * 16;
+  return (size_t)most * 16 + kJoinBytes;
 }
 
 template <typename K, typename N>
@@ -605,6 +671,24 @@ static vcnn_status with_tile(const MuonBatch& b, bool triangle, F launch) {
 
 template <int WHAT>
 static vcnn_status launch_square(MuonBatch* b, hipStream_t st) {
+  if constexpr (WHAT == MUON_A) {
+    // Its sums are long where A is small: blocks share them as far as there are idle CUs, sixteen steps a block at least, where
+    // that more than makes up for the second launch.
+    int64_t few = 0, longest = 0;
+    for (int t = 0; t < b->tensors; ++t) {
+      few += tiles_of<FewTile>(b->t[t], true);
+      longest = std::max(longest, ceil_div(b->t[t].large, 32));
+    }
+    if (few * 2 <= kJoinBlocks && longest >= kSharedSteps) {
+      for (int t = 0; t < b->tensors; ++t)
+        b->t[t].parts = (int)std::max<int64_t>(1, std::min(kJoinBlocks / few, ceil_div(b->t[t].large, 32) / 16));
+      if (vcnn_status s = launch_phase("muon share", muon_share_kernel, b, FewTile::THREADS, FewTile::LDS, st,
+                                       [](const MuonTensor& t) { return tiles_of<FewTile>(t, true) * t.parts; }))
+        return s;
+      hipLaunchKernelGGL(muon_join_kernel, dim3((unsigned)few), dim3(FewTile::THREADS), 0, st, *b);
+      return check_launch("muon join");
+    }
+  }
   return with_tile(*b, true, [&](auto tile) {
     using TILE = decltype(tile);
     return launch_phase("muon square", muon_square_kernel<TILE, WHAT>, b, TILE::THREADS, TILE::LDS, st,
@@ -625,7 +709,8 @@ vcnn_status launch_muon(const MuonTensor* tensors, int count, float lr, float mo
   MuonBatch b{};
   b.tensors = count;
   b.lr = lr, b.momentum = momentum, b.nesterov = nesterov, b.keep = 1.f - lr * weight_decay;
-  uint4* work = (uint4*)workspace;
+  b.shares = (float*)workspace;
+  uint4* work = (uint4*)((char*)workspace + kJoinBytes);
   for (int t = 0; t < b.tensors; ++t) {
     b.t[t] = tensors[t];
     lay_out(&b.t[t]);

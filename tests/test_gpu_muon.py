@@ -17,7 +17,7 @@ from test_gpu_norm import DEV, Guarded, dev
 A, B, C = 3.4445, -4.7750, 2.0315
 U = 2.0 ** -24
 SHAPES = [(1, 1), (1, 9), (7, 1), (3, 5), (20, 25), (64, 800), (500, 50), (127, 129), (128, 128), (129, 260), (300, 1000),
-          (513, 40), (700, 650)]
+          (513, 40), (700, 650), (60, 5000), (4100, 130), (200, 9000)]
 
 
 def matrix(seed, rows, cols):
@@ -160,7 +160,8 @@ def test_update(shapes, nesterov):
 
 @pytest.mark.gpu
 def test_the_same_bits_alone_together_and_replayed():
-    """A matrix' update does not depend on the ones beside it; a graph gives what the eager calls give, step after step."""
+    """Matrices of these sizes take the same tiles alone and together, and so give the same bits; a graph gives what the eager
+    calls give, step after step."""
     w, dw, m = tensors(DIGITS, 50)
 
     def fresh():
@@ -209,7 +210,8 @@ def test_refusals_need_no_gpu():
         assert lib.vcnn_orthogonalize(4, 8, 5, f, f, ws, size, None) == vcnn.ERR_WORKSPACE
     assert lib.vcnn_orthogonalize_workspace_bytes(4, 8, None) == vcnn.ERR_NULL
     assert n == vcnn.muon_workspace_bytes([(4, 8)]) and vcnn.muon_workspace_bytes([]) == 0
-    assert vcnn.muon_workspace_bytes([(4, 8)] * 16) == 16 * n == vcnn.muon_workspace_bytes([(4, 8)] * 40)
+    sixteen = vcnn.muon_workspace_bytes([(4, 8)] * 16)
+    assert n < sixteen < 16 * n and sixteen == vcnn.muon_workspace_bytes([(4, 8)] * 40)  # (batches share it)
 
     def go(count=1, p=(f, f, f), lr=0.1, mu=0.9, wd=0.0, steps=5, ws=0x1000, size=n):
         one = (ctypes.c_int32 * 1)

@@ -1302,7 +1302,7 @@ vcnn_status vcnn_fc_fwd_i8(int32_t dtype, int32_t batch, int32_t in_f, int32_t o
   if (vcnn_status s = check_dtype(dtype, "fc_fwd_i8")) return s;
   if (!xq || !xscale || !wq || !wscale || !y) return fail(VCNN_ERR_NULL, "fc_fwd_i8: NULL tensor");
   if (!workspace) workspace_bytes = 0;
-  if (vcnn_status s = check_ws(workspace, workspace_bytes, workspace ? 1 : 0, "fc_fwd_i8")) return s;
+  if (vcnn_status s = check_ws(workspace, workspace_bytes, workspace_bytes ? 1 : 0, "fc_fwd_i8")) return s;
   return launch_fc_i8(dtype, batch, in_f, out_f, act, xq, xscale, wq, wscale, bias, y, workspace, workspace_bytes,
                       (hipStream_t)stream);
 }

@@ -67,6 +67,18 @@ def test_against_exact_sums(batch, k, out, dtype, offset):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("offset", [0, 1])
+@pytest.mark.parametrize("batch,k,out", [(1000, 112, 12300), (1000, 100, 12300), (770, 200, 16390)])
+def test_large_tiles(batch, k, out, offset):
+    """Enough tiles of 256 x 256, the last of them ragged on both sides."""
+    x, w, xs, ws, bias = make(batch + k, batch, k, out)
+    want, size = reference(x, w, xs, ws, bias, vcnn.ACT_RELU)
+    for dtype in (vcnn.F32, vcnn.BF16):
+        off = (call(dtype, vcnn.ACT_RELU, x, w, xs, ws, bias, None, offset).double() - want).abs()
+        assert bool((off <= want.abs() * half_step(dtype) * 1.01 + size * 4 * U).all())
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("batch", [1, 20, 64, 70, 260])
 def test_every_sum_is_whole(batch):
     """Scales of one: floats of the sums themselves, below 2^24 with every bit; large ones at the longest rows."""
@@ -168,6 +180,7 @@ def test_refusals_need_no_gpu():
     for i in range(5):
         assert go(p=tuple(None if j == i else f for j in range(5))) == vcnn.ERR_NULL
     assert go(ws=0x1010, n=256) == vcnn.ERR_WORKSPACE
+    assert go(ws=0x1010, n=0, act=9) == vcnn.ERR_UNSUPPORTED
     assert lib.vcnn_fc_i8_workspace_bytes(4, 8, 4, None) == vcnn.ERR_NULL
     assert lib.vcnn_fc_i8_workspace_bytes(4, 0, 4, ctypes.byref(ctypes.c_size_t())) == vcnn.ERR_SHAPE
     assert vcnn.fc_i8_workspace_bytes(1, 4096, 4096) == 0

@@ -66,6 +66,47 @@ def test_against_64_bits(rows, cols, steps):
         assert off <= 2 * float(torch.linalg.vector_norm(products(g, steps).double() - want))
 
 
+def large(seed, rows, cols):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    k = min(rows, cols) // 16
+    return torch.randn(rows, k, device=DEV, generator=g) @ torch.randn(k, cols, device=DEV, generator=g) + \
+        torch.randn(rows, cols, device=DEV, generator=g)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,cols", [(1500, 1570), (2150, 2070), (2900, 2950), (4000, 4100), (5900, 5830)])
+def test_every_tile(rows, cols):
+    """Sizes at which the phases take the larger tiles, one kind after the other."""
+    g = large(rows, rows, cols)
+    out = Guarded((rows, cols), torch.float32)
+    vcnn.orthogonalize(rows, cols, 3, g, out.t, workspace(vcnn.orthogonalize_workspace_bytes(rows, cols)))
+    out.cpu()
+    want = products(g.double(), 3)
+    off = float(torch.linalg.vector_norm(out.t.double() - want))
+    assert off <= bound(rows, cols, 3)
+    assert off <= 2 * float(torch.linalg.vector_norm(products(g, 3).double() - want))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shapes", [[(300, 5000), (2150, 1300), (1200, 4100), (7, 9)], [(40, 9000), (6000, 70), (130, 2100)]],
+                         ids=["large", "long sums"])
+def test_update_of_unlike_matrices(shapes):
+    lr, mu = 0.05, 0.9
+    ms, dws = [large(i, *s) for i, s in enumerate(shapes)], [large(9 + i, *s) for i, s in enumerate(shapes)]
+    ws = [torch.zeros(s, device=DEV) for s in shapes]
+    kept = [m.clone() for m in ms]
+    vcnn.muon_update_multi(lr, mu, True, 0.0, 5, ws, dws, ms, workspace(vcnn.muon_workspace_bytes(shapes)))
+    for (rows, cols), w, g, m in zip(shapes, ws, dws, kept):
+        u = g.double() + mu * (mu * m.double() + g.double())
+        step = lr * max(1.0, rows / cols) ** 0.5
+        want = -step * products(u, 5)
+        off = float(torch.linalg.vector_norm(w.double() - want))
+        assert off <= step * 2 * bound(rows, cols, 5)  # (u as floats: as above)
+        if min(rows, cols) >= 64:
+            f = step * float(torch.linalg.vector_norm(products(u.float(), 5).double() - want / -step))
+            assert off <= 2 * f + 4 * U * float(torch.linalg.vector_norm(want))
+
+
 @pytest.mark.gpu
 def test_singular_values_come_near_one():
     g = torch.linalg.qr(torch.randn(200, 200, generator=torch.Generator().manual_seed(1), dtype=torch.float64))[0]

@@ -450,10 +450,12 @@ __global__ __launch_bounds__(TILE::THREADS, 2) void i8_tile_kernel(I8Args a) {
   i8_store<T, TILE>(a, acc, o0, b0, smem16);
 }
 
-// Rows that start anywhere: a slab goes through registers, fetched before the one before is multiplied, put behind it.
+// Rows that start anywhere: a slab goes through registers, fetched HELD slabs before it is multiplied and put into one of two
+// places in LDS while the one before is.
 template <typename T, typename TILE>
 __global__ __launch_bounds__(TILE::THREADS, 2) void i8_tile_loose_kernel(I8Args a) {
   constexpr int TO = TILE::TO, TB = TILE::TB, LO = TILE::LO, L = TILE::LO + TILE::LB, THREADS = TILE::THREADS;
+  constexpr int HELD = L <= 2 ? 4 : 2;
   extern __shared__ uint4 smem16[];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   int to, tb;
@@ -469,19 +471,19 @@ __global__ __launch_bounds__(TILE::THREADS, 2) void i8_tile_loose_kernel(I8Args 
     const int r = (i < LO ? i : i - LO) * (THREADS / 4) + (tid >> 2);
     offset[i] = (uint32_t)(i < LO ? min(r, a.out - 1 - o0) : min(r, a.batch - 1 - b0)) * (uint32_t)a.k;
   }
-  uint4 held[L];
-  auto fetch = [&](int s) {
-    if ((s + 1) * 64 <= a.k) {
+  uint4 held[HELD][L];
+  auto fetch = [&](int s, uint4 (&to)[L]) {  // (zeros behind the last slab)
+    if (s < s1 && (s + 1) * 64 <= a.k) {
 #pragma unroll
-      for (int i = 0; i < L; ++i) held[i] = load16_whole((i < LO ? w0 : x0) + (int64_t)s * 64 + offset[i] + place);
+      for (int i = 0; i < L; ++i) to[i] = load16_whole((i < LO ? w0 : x0) + (int64_t)s * 64 + offset[i] + place);
     } else {
 #pragma unroll
-      for (int i = 0; i < L; ++i) held[i] = load16((i < LO ? w0 : x0) + offset[i], s * 64 + place, a.k);
+      for (int i = 0; i < L; ++i) to[i] = load16((i < LO ? w0 : x0) + offset[i], s < s1 ? s * 64 + place : a.k, a.k);
     }
   };
-  auto put = [&](int s) {
+  auto put = [&](int s, const uint4 (&from)[L]) {
 #pragma unroll
-    for (int i = 0; i < L; ++i) smem16[(s & 1) * TILE::WORDS + i * THREADS + tid] = held[i];
+    for (int i = 0; i < L; ++i) smem16[(s & 1) * TILE::WORDS + i * THREADS + tid] = from[i];
   };
   i32x4 acc[TO][TB];
 #pragma unroll
@@ -490,22 +492,27 @@ __global__ __launch_bounds__(TILE::THREADS, 2) void i8_tile_loose_kernel(I8Args 
     for (int j = 0; j < TB; ++j) acc[i][j] = (i32x4){0, 0, 0, 0};
   const int wo = (wave % TILE::WO) * 16 * TO, wb = (wave / TILE::WO) * 16 * TB;
   const int mine = (lane & 15) * 4 + ((lane >> 4) ^ swizzle(lane & 15));
-  fetch(s0);
-  put(s0);
-  for (int s = s0; s < s1; ++s) {
-    __syncthreads();  // slab s is there, the other buffer is free
-    if (s + 1 < s1) fetch(s + 1);
-    const uint4* const buf = smem16 + (s & 1) * TILE::WORDS + mine;
-    uint4 fo[TO], fb[TB];
 #pragma unroll
-    for (int j = 0; j < TB; ++j) fb[j] = buf[(TILE::BO + wb + j * 16) * 4];
+  for (int u = 0; u < HELD; ++u) fetch(s0 + u, held[u]);
+  put(s0, held[0]);
+  fetch(s0 + HELD, held[0]);
+  for (int s = s0; s < s1; s += HELD) {
 #pragma unroll
-    for (int i = 0; i < TO; ++i) fo[i] = buf[(wo + i * 16) * 4];
+    for (int u = 0; u < HELD; ++u) {  // (slabs behind the last are zeros, so that every turn is the same)
+      __syncthreads();                // slab s + u is there, the other place is free
+      const uint4* const buf = smem16 + ((s + u) & 1) * TILE::WORDS + mine;
+      uint4 fo[TO], fb[TB];
 #pragma unroll
-    for (int i = 0; i < TO; ++i)
+      for (int j = 0; j < TB; ++j) fb[j] = buf[(TILE::BO + wb + j * 16) * 4];
 #pragma unroll
-      for (int j = 0; j < TB; ++j) acc[i][j] = mfma_i8(fo[i], fb[j], acc[i][j]);
-    if (s + 1 < s1) put(s + 1);
+      for (int i = 0; i < TO; ++i) fo[i] = buf[(wo + i * 16) * 4];
+      put(s + u + 1, held[(u + 1) % HELD]);
+      fetch(s + u + 1 + HELD, held[(u + 1) % HELD]);
+#pragma unroll
+      for (int i = 0; i < TO; ++i)
+#pragma unroll
+        for (int j = 0; j < TB; ++j) acc[i][j] = mfma_i8(fo[i], fb[j], acc[i][j]);
+    }
   }
   __syncthreads();
   i8_store<T, TILE>(a, acc, o0, b0, smem16);

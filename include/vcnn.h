@@ -299,7 +299,8 @@ vcnn_status vcnn_orthogonalize(int32_t rows, int32_t cols, int32_t steps, const 
 /* The Muon update of `tensors` weight matrices (a convolution's kernels count as [k][c*r*s], the kernel matrix of Eq. 2):
  *     m[t] = momentum * m[t] + dw[t],   u = nesterov ? dw[t] + momentum * m[t] : m[t]
  *     w[t] = (1 - lr * weight_decay) * w[t] - lr * sqrt(max(1, rows[t] / cols[t])) * orthogonalize(u)
- * All matrices go through each of its 2 + 3 steps launches together (sixteen at a time).  rows, cols, w, dw, m and w_bf16
+ * All matrices go through each of its launches together, sixteen at a time: two, and two to four a step.  How their sums are
+ * divided follows from all of them, so the last bits of one may differ with the others beside it (not from run to run).  rows, cols, w, dw, m and w_bf16
  * are HOST arrays of length `tensors` holding sizes and DEVICE pointers; they are read before the call returns.  w_bf16 may be
  * NULL; a non-NULL w_bf16[t] receives the updated tensor rounded to bfloat16.  No two tensors may overlap.  lr, momentum and
  * weight_decay must be finite, steps 1 to 32.  workspace: vcnn_muon_workspace_bytes, three to five times the bytes of the

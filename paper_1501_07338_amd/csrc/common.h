@@ -503,7 +503,7 @@ struct MuonTensor {
   int rows, cols;
   // set by the launch: smaller and larger side, 128-tiles along them, this matrix' part of the workspace
   int tall, small, large, mt, nt, norm_blocks;
-  int parts;           // blocks that share a sum
+  int parts, share0;   // blocks that share a sum; the first one's share
   uint4* work;
 };
 size_t muon_workspace(int tensors, const int32_t* rows, const int32_t* cols);

@@ -23,7 +23,13 @@
 // Tiles.  256 x 256 and 128 x 128 from slabs in LDS; where there are too few of those for the chip, 64 x 64 with the
 // contraction divided over the block's eight waves, which read their fragments straight from the caches.
 //
-// All matrices of an update go through each phase in one launch: two launches and three a step for all of them.
+// All matrices of an update go through each phase in one launch: two at first, then a step in two (all matrices of at most 64
+// rows), three, or four (long sums over few tiles, shared by blocks).  4096 x 4096 and 8192 x 2048 together take 5.34 ms, five
+// steps: 1.08 PFLOP/s of f16 products (B X of both 1.23, X X^T 1.04, A^2 0.92, whose tiles come in 1.3 rounds of what the chip
+// holds), a plain f16 product of 8192^3 1.32.  The products draw so much power that the clock falls to 1.9 GHz; the
+// matrix cores are then busy 57 to 61 % of the time.  1024 x 4096 takes 0.38 ms, bound by the rate at which a CU reads its
+// cache (X X^T) and by the latency of 32 steps (B X); 64 x 800 68 us and 500 x 800 beside three smaller ones 166, by that of
+// the launches.
 #include <algorithm>
 
 #include "common.h"
@@ -529,7 +535,66 @@ __global__ __launch_bounds__(FewTile::THREADS) void muon_join_kernel(MuonBatch b
   put_symmetric<MUON_A>(t, v64, it * 64, jt * 64, it != jt, wave, wave + 1);
 }
 
-// X <- a X + B X; the last one: the result, or the weights moved by it.
+// X <- a X + B X of a 64 x 64 part at (i0, j0), given B X; the last one: the result, or the weights moved by it.  Fragments
+// f0 .. f1 are this wave's; waves that share a part all come here.
+template <bool LAST>
+__device__ __forceinline__ void put_applied(const MuonBatch& b, const MuonTensor& t, float* v64, int i0, int j0, int f0, int f1) {
+  const bool inside = i0 < t.mt * kPad && j0 < t.nt * kPad;  // (the same for all waves that share a part)
+  const int lane = threadIdx.x & 63;
+  const int steps_n = t.nt * (kPad / 32), steps_m = t.mt * (kPad / 32);
+  const int64_t by_rows = word_of(i0, j0, steps_n);
+  if (inside) {
+#pragma unroll 2
+    for (int f = f0; f < f1; ++f) {  // a X, from X by rows (whose place the same lanes write below)
+      const int row = (f >> 1) * 16 + (lane & 15), k = (f & 1) * 32 + (lane >> 4) * 8;
+      float v[8];
+      join8(x_rows(t), x_term(t), by_rows + ((int64_t)(f >> 1) * steps_n + (f & 1)) * 64 + lane, v);
+#pragma unroll
+      for (int e = 0; e < 8; e += 4) {
+        float4* const p = reinterpret_cast<float4*>(v64 + at64(row, k + e));
+        const float4 u = *p;
+        *p = make_float4(fmaf(kA, v[e], u.x), fmaf(kA, v[e + 1], u.y), fmaf(kA, v[e + 2], u.z), fmaf(kA, v[e + 3], u.w));
+      }
+    }
+  }
+  if (f1 - f0 < 8) __syncthreads();  // (a part of several waves)
+  if (!inside) return;
+  if constexpr (!LAST) {
+#pragma unroll 2
+    for (int f = f0; f < f1; ++f) {
+      put_fragment<false>(v64, x_rows(t), x_term(t), by_rows, steps_n, f, AsIs());
+      put_fragment<true>(v64, x_cols(t, b.turn ^ 1), x_term(t), word_of(j0, i0, steps_m), steps_m, f, AsIs());
+    }
+  } else {
+    const float step = b.lr * t.factor;
+    const int64_t at0 = t.tall ? (int64_t)j0 * t.small + i0 : (int64_t)i0 * t.large + j0;
+    const int pitch = t.tall ? t.small : t.large;
+    const int rows_left = t.tall ? t.large - j0 : t.small - i0, cols_left = t.tall ? t.small - i0 : t.large - j0;
+    if (lane >= cols_left) return;
+#pragma unroll 1
+    for (int r0 = f0 * 8; r0 < min(f1 * 8, rows_left); r0 += 8) {  // rows of the matrix as stored
+      float w[8];
+      if (!t.out) {
+#pragma unroll
+        for (int r = 0; r < 8; ++r) w[r] = r0 + r < rows_left ? t.w[at0 + (int64_t)(r0 + r) * pitch + lane] : 0.f;
+      }
+#pragma unroll
+      for (int r = 0; r < 8; ++r) {
+        if (r0 + r >= rows_left) break;
+        const int64_t at = at0 + (int64_t)(r0 + r) * pitch + lane;
+        const float o = v64[t.tall ? at64(lane, r0 + r) : at64(r0 + r, lane)];
+        if (t.out) {
+          t.out[at] = o;
+        } else {
+          const float v = fmaf(-step, o, b.keep * w[r]);
+          t.w[at] = v;
+          if (t.w16) st(reinterpret_cast<bf16*>(t.w16) + at, v);
+        }
+      }
+    }
+  }
+}
+
 template <typename TILE, bool LAST>
 __global__ __launch_bounds__(TILE::THREADS, 2) void muon_apply_kernel(MuonBatch b) {
   extern __shared__ uint4 smem16[];
@@ -541,62 +606,85 @@ __global__ __launch_bounds__(TILE::THREADS, 2) void muon_apply_kernel(MuonBatch 
   const Operand x{mat_b(t), a_term(t), it * (TILE::BM / 16), t.mt * (kPad / 16), t.mt * (kPad / 32)};
   const Operand y{x_cols(t, b.turn), x_term(t), jt * (TILE::BN / 16), t.nt * (kPad / 16), t.mt * (kPad / 32)};
   TILE::run(x, y, (t.small + 31) / 32, smem16, [&](float* v64, int i1, int j1, int f0, int f1) {
-    const int i0 = it * TILE::BM + i1, j0 = jt * TILE::BN + j1;
-    const bool inside = i0 < t.mt * kPad && j0 < t.nt * kPad;  // (the same for all waves that share a part)
-    const int lane = threadIdx.x & 63;
-    const int steps_n = t.nt * (kPad / 32), steps_m = t.mt * (kPad / 32);
-    const int64_t by_rows = word_of(i0, j0, steps_n);
-    if (inside) {
-#pragma unroll 2
-      for (int f = f0; f < f1; ++f) {  // a X, from X by rows (whose place the same lanes write below)
-        const int row = (f >> 1) * 16 + (lane & 15), k = (f & 1) * 32 + (lane >> 4) * 8;
-        float v[8];
-        join8(x_rows(t), x_term(t), by_rows + ((int64_t)(f >> 1) * steps_n + (f & 1)) * 64 + lane, v);
-#pragma unroll
-        for (int e = 0; e < 8; e += 4) {
-          float4* const p = reinterpret_cast<float4*>(v64 + at64(row, k + e));
-          const float4 u = *p;
-          *p = make_float4(fmaf(kA, v[e], u.x), fmaf(kA, v[e + 1], u.y), fmaf(kA, v[e + 2], u.z), fmaf(kA, v[e + 3], u.w));
-        }
-      }
-    }
-    if (f1 - f0 < 8) __syncthreads();  // (a part of several waves)
-    if (!inside) return;
-    if constexpr (!LAST) {
-#pragma unroll 2
-      for (int f = f0; f < f1; ++f) {
-        put_fragment<false>(v64, x_rows(t), x_term(t), by_rows, steps_n, f, AsIs());
-        put_fragment<true>(v64, x_cols(t, b.turn ^ 1), x_term(t), word_of(j0, i0, steps_m), steps_m, f, AsIs());
-      }
-    } else {
-      const float step = b.lr * t.factor;
-      const int64_t at0 = t.tall ? (int64_t)j0 * t.small + i0 : (int64_t)i0 * t.large + j0;
-      const int pitch = t.tall ? t.small : t.large;
-      const int rows_left = t.tall ? t.large - j0 : t.small - i0, cols_left = t.tall ? t.small - i0 : t.large - j0;
-      if (lane >= cols_left) return;
-#pragma unroll 1
-      for (int r0 = f0 * 8; r0 < min(f1 * 8, rows_left); r0 += 8) {  // rows of the matrix as stored
-        float w[8];
-        if (!t.out) {
-#pragma unroll
-          for (int r = 0; r < 8; ++r) w[r] = r0 + r < rows_left ? t.w[at0 + (int64_t)(r0 + r) * pitch + lane] : 0.f;
-        }
-#pragma unroll
-        for (int r = 0; r < 8; ++r) {
-          if (r0 + r >= rows_left) break;
-          const int64_t at = at0 + (int64_t)(r0 + r) * pitch + lane;
-          const float o = v64[t.tall ? at64(lane, r0 + r) : at64(r0 + r, lane)];
-          if (t.out) {
-            t.out[at] = o;
-          } else {
-            const float v = fmaf(-step, o, b.keep * w[r]);
-            t.w[at] = v;
-            if (t.w16) st(reinterpret_cast<bf16*>(t.w16) + at, v);
-          }
-        }
-      }
-    }
+    put_applied<LAST>(b, t, v64, it * TILE::BM + i1, jt * TILE::BN + j1, f0, f1);
   });
+}
+
+// Matrices of at most 64 rows (as X): a block adds the shares of A by itself, makes B of it and then its 64 columns of X, in place
+// of three launches with a few blocks each.  A wave makes two 16 x 16 tiles of either product.
+template <bool LAST>
+__global__ __launch_bounds__(512) void muon_small_kernel(MuonBatch b) {
+  __shared__ __attribute__((aligned(16))) float v64[64 * 64];
+  __shared__ uint4 frag[8][2][64];  // [4 row tiles][2 steps], [term]
+  const int at_tensor = tensor_of(b);
+  const MuonTensor& t = b.t[at_tensor];
+  const int j0 = (blockIdx.x - b.first[at_tensor]) * 64;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int rt = wave >> 1, ct = (wave & 1) * 2;
+  uint4 x[2][2][2];  // [tile][step][term] of X by columns
+#pragma unroll
+  for (int c = 0; c < 2; ++c)
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        x[c][s][h] = x_cols(t, b.turn)[h * x_term(t) + word_of(j0 + (ct + c) * 16, s * 32, t.mt * (kPad / 32)) + lane];
+  const float4* const from = reinterpret_cast<const float4*>(b.shares) + (int64_t)t.share0 * 1024 + threadIdx.x;
+  float4 v[2] = {from[0], from[512]};
+#pragma unroll 4
+  for (int p = 1; p < t.parts; ++p)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const float4 u = from[p * 1024 + h * 512];
+      v[h].x += u.x, v[h].y += u.y, v[h].z += u.z, v[h].w += u.w;
+    }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) reinterpret_cast<float4*>(v64)[h * 512 + threadIdx.x] = v[h];
+  __syncthreads();
+  const auto take = [&]() {  // the values' fragment `wave`
+    const int row = rt * 16 + (lane & 15), k = (wave & 1) * 32 + (lane >> 4) * 8;
+    float u[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) u[e] = v64[at64(row, k + e)];
+    uint4 hi, lo;
+    split8(u, &hi, &lo);
+    frag[wave][0][lane] = hi, frag[wave][1][lane] = lo;
+  };
+  take();
+  __syncthreads();
+  f32x4 acc[2] = {};
+#pragma unroll
+  for (int s = 0; s < 2; ++s)
+#pragma unroll
+    for (int p = 0; p < 3; ++p)
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+        acc[c] = mfma_f16(frag[rt * 2 + s][p == 2][lane], frag[(ct + c) * 2 + s][p == 1][lane], acc[c]);
+#pragma unroll
+  for (int c = 0; c < 2; ++c)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {  // B in A's place: every value is one lane's own
+      float* const at = v64 + at64(rt * 16 + (lane >> 4) * 4 + q, (ct + c) * 16 + (lane & 15));
+      *at = fmaf(kC * (kUnscale * kUnscale), acc[c][q], kB * *at);
+    }
+  __syncthreads();
+  take();
+  __syncthreads();
+#pragma unroll
+  for (int c = 0; c < 2; ++c) acc[c] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int s = 0; s < 2; ++s)
+#pragma unroll
+    for (int p = 0; p < 3; ++p)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) acc[c] = mfma_f16(frag[rt * 2 + s][p == 2][lane], x[c][s][p == 1], acc[c]);
+#pragma unroll
+  for (int c = 0; c < 2; ++c)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      v64[at64(rt * 16 + (lane >> 4) * 4 + q, (ct + c) * 16 + (lane & 15))] = acc[c][q] * (kUnscale * kUnscale);
+  __syncthreads();
+  put_applied<LAST>(b, t, v64, 0, j0, wave, wave + 1);
 }
 
 // ---- launches -----------------------------------------------------------------------------------------------------------
@@ -669,22 +757,27 @@ static vcnn_status with_tile(const MuonBatch& b, bool triangle, F launch) {
   return launch(TileTwo());
 }
 
+// The shares of A = X X^T: blocks share its sums as far as there are idle CUs, `each` steps a block at least.
+static vcnn_status launch_shares(MuonBatch* b, int64_t tiles, int each, int most, hipStream_t st) {
+  for (int t = 0; t < b->tensors; ++t)
+    b->t[t].parts = (int)std::max<int64_t>(1, std::min<int64_t>({kJoinBlocks / tiles, most, ceil_div(b->t[t].large, 32) / each}));
+  if (vcnn_status s = launch_phase("muon share", muon_share_kernel, b, FewTile::THREADS, FewTile::LDS, st,
+                                   [](const MuonTensor& t) { return tiles_of<FewTile>(t, true) * t.parts; }))
+    return s;
+  for (int t = 0; t < b->tensors; ++t) b->t[t].share0 = (int)b->first[t];
+  return VCNN_OK;
+}
+
 template <int WHAT>
 static vcnn_status launch_square(MuonBatch* b, hipStream_t st) {
-  if constexpr (WHAT == MUON_A) {
-    // Its sums are long where A is small: blocks share them as far as there are idle CUs, sixteen steps a block at least, where
-    // that more than makes up for the second launch.
+  if constexpr (WHAT == MUON_A) {  // its sums are long where A is small
     int64_t few = 0, longest = 0;
     for (int t = 0; t < b->tensors; ++t) {
       few += tiles_of<FewTile>(b->t[t], true);
       longest = std::max(longest, ceil_div(b->t[t].large, 32));
     }
     if (few * 2 <= kJoinBlocks && longest >= kSharedSteps) {
-      for (int t = 0; t < b->tensors; ++t)
-        b->t[t].parts = (int)std::max<int64_t>(1, std::min(kJoinBlocks / few, ceil_div(b->t[t].large, 32) / 16));
-      if (vcnn_status s = launch_phase("muon share", muon_share_kernel, b, FewTile::THREADS, FewTile::LDS, st,
-                                       [](const MuonTensor& t) { return tiles_of<FewTile>(t, true) * t.parts; }))
-        return s;
+      if (vcnn_status s = launch_shares(b, few, 16, kJoinBlocks, st)) return s;
       hipLaunchKernelGGL(muon_join_kernel, dim3((unsigned)few), dim3(FewTile::THREADS), 0, st, *b);
       return check_launch("muon join");
     }
@@ -721,7 +814,17 @@ vcnn_status launch_muon(const MuonTensor* tensors, int count, float lr, float mo
   const auto parts = [](const MuonTensor& t) { return ceil_div(t.small, 64) * ceil_div(t.large, 64); };
   if (vcnn_status s = launch_phase("muon moment", muon_moment_kernel, &b, kThreads, 0, st, norm_blocks)) return s;
   if (vcnn_status s = launch_phase("muon begin", muon_begin_kernel, &b, kThreads, 0, st, parts)) return s;
+  bool small = true;  // all of them: a step is two launches (64 x 800: five steps 68 us, with three launches each 107)
+  for (int t = 0; t < b.tensors; ++t) small = small && b.t[t].small <= 64;
   for (int i = 0; i < steps; ++i, b.turn ^= 1) {
+    if (small) {
+      const auto columns = [](const MuonTensor& t) { return ceil_div(t.large, 64); };
+      if (vcnn_status s = launch_shares(&b, b.tensors, 8, 16, st)) return s;
+      if (vcnn_status s = i + 1 < steps ? launch_phase("muon small", muon_small_kernel<false>, &b, 512, 0, st, columns)
+                                        : launch_phase("muon small", muon_small_kernel<true>, &b, 512, 0, st, columns))
+        return s;
+      continue;
+    }
     if (vcnn_status s = launch_square<MUON_A>(&b, st)) return s;
     if (vcnn_status s = launch_square<MUON_B>(&b, st)) return s;
     if (vcnn_status s = i + 1 < steps ? launch_apply<false>(&b, st) : launch_apply<true>(&b, st)) return s;

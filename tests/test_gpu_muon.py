@@ -167,8 +167,9 @@ DIGITS = [(20, 1, 5, 5), (50, 20, 5, 5), (500, 800), (10, 500)]
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("nesterov", [False, True])
-@pytest.mark.parametrize("shapes", [DIGITS, [(3, 7)] * 9 + [(40, 30)] * 6 + [(200, 100), (5, 2, 3, 3)] + [(64, 65)] * 5],
-                         ids=["digits", "more than a batch"])
+@pytest.mark.parametrize("shapes", [DIGITS, [(3, 7)] * 9 + [(40, 30)] * 6 + [(200, 100), (5, 2, 3, 3)] + [(64, 65)] * 5,
+                                    [(3, 7), (40, 30), (64, 65), (500, 20), (5, 3000), (1, 1), (64, 64)]],
+                         ids=["digits", "more than a batch", "small"])
 def test_update(shapes, nesterov):
     lr, mu, decay = 0.05, 0.9, 0.1
     w, dw, m = tensors(shapes)
@@ -200,10 +201,10 @@ def test_update(shapes, nesterov):
 
 
 @pytest.mark.gpu
-def test_the_same_bits_alone_together_and_replayed():
-    """Matrices of these sizes take the same tiles alone and together, and so give the same bits; a graph gives what the eager
-    calls give, step after step."""
-    w, dw, m = tensors(DIGITS, 50)
+@pytest.mark.parametrize("shapes", [DIGITS, DIGITS[:2], [(300, 5000), (70, 2100)]], ids=["digits", "small", "shared sums"])
+def test_the_same_bits_in_every_run_and_replayed(shapes):
+    """Eager calls, calls on a stream of their own and a graph's replays give the same bits, step after step."""
+    w, dw, m = tensors(shapes, 50)
 
     def fresh():
         return [[dev(t) for t in ts] for ts in (w, dw, m)]
@@ -211,17 +212,16 @@ def test_the_same_bits_alone_together_and_replayed():
     def go(ts, ws):
         vcnn.muon_update_multi(0.02, 0.95, True, 0.0, 5, *ts, ws)
 
-    alone = fresh()
-    for i in range(len(DIGITS)):
-        for _ in range(3):
-            go([[t[i]] for t in alone], workspace(vcnn.muon_workspace_bytes([DIGITS[i]])))
-    ws = workspace(vcnn.muon_workspace_bytes(DIGITS))
-    together, replayed = fresh(), fresh()
+    ws = workspace(vcnn.muon_workspace_bytes(shapes))
+    eager, other, replayed = fresh(), fresh(), fresh()
+    for _ in range(3):
+        go(eager, ws)
+        ws.fill_(255)  # nothing is carried from call to call in the workspace
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):
         for _ in range(3):
-            go(together, ws)
+            go(other, ws)
     torch.cuda.synchronize()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
@@ -229,9 +229,9 @@ def test_the_same_bits_alone_together_and_replayed():
     for _ in range(3):
         graph.replay()
         torch.cuda.synchronize()
-        ws.fill_(255)  # nothing is carried from call to call in the workspace
+        ws.fill_(255)
     torch.cuda.synchronize()
-    for a, b, c in zip(alone[0] + alone[2], together[0] + together[2], replayed[0] + replayed[2]):
+    for a, b, c in zip(eager[0] + eager[2], other[0] + other[2], replayed[0] + replayed[2]):
         assert torch.equal(a, b) and torch.equal(a, c)
 
 

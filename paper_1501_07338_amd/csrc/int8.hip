@@ -4,15 +4,15 @@
 // division over waves and blocks changes a bit of the result.  A sum is rounded to float (2^-24) in the epilogue, multiplied
 // by the two scales and rounded once more to the type of y.
 //
-// Three kernels.  One or two samples: dot products of whole rows (i8_dot_kernel; 4096 -> 16384 in 12.2 us with the call's own
-// 6, the matrix cores' kernel 15.1).  Up to 32, or 128 where the layer
-// is small: the weights are read once and nothing of them is reused, so a block owns 16
-// outputs, its eight waves take every eighth 128 bytes of the rows and feed the matrix cores from global memory, all operands
-// of four such steps in flight at once (i8_rows_kernel).  More: tiles of 256 x 256 or 128 x 128 from slabs of 64 bytes of
-// both operands in LDS (i8_tile_kernel), the contraction divided over blocks where the tiles alone do not fill the chip;
-// their shares are added by i8_join_kernel.  4096 x 8192 -> 8192 takes 247 us, 2.22 POP/s: 53 % of what the instruction
-// reaches with operands in registers (4.2, bound by power).  Of those 247 us, the products alone are 135, and bringing the
-// slabs into LDS costs as much as 70: not by its latency (a ring of five slabs in place of four changes nothing).
+// Three kernels.  One or two samples: dot products of whole rows (i8_dot_kernel; 4096 -> 16384 in 11.9 us with the call's own,
+// the next kernel 15.1).  Up to 32, or 128 where the layer is small: the weights are read once and nothing of them is reused,
+// so a block owns 16 outputs, its eight waves take every eighth 128 bytes of the rows and feed the matrix cores from global
+// memory, all operands of four such steps in flight at once (i8_rows_kernel; 48 samples 4096 -> 4096 in 12 us, one round of
+// loads).  More: tiles of 256 x 256 or 128 x 128 from slabs of 64 bytes of both operands in LDS (i8_tile_kernel), the
+// contraction divided over blocks where the tiles alone do not fill the chip; their shares are added by i8_join_kernel.
+// 4096 x 8192 -> 8192 takes 246 us, 2.23 POP/s: 53 % of what the instruction reaches with operands in registers (4.2, bound by
+// power).  Of those 246 us, the products alone are 135, and bringing the slabs into LDS costs as much as 70: not by its latency
+// (a ring of five slabs in place of four changes nothing).
 #include <algorithm>
 
 #include "common.h"

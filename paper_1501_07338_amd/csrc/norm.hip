@@ -9,7 +9,8 @@
 // written.  A row of at most 128 groups belongs to one wave (no barrier; four rows a block), a longer one to a block of as
 // many waves as its groups fill (at most eight), one of more than 16384 elements is read twice.  Rows start wherever the row
 // length puts them: a group is loaded as a 16-byte type of alignment one, which the target serves at full width, and only
-// the last group of a row whose length is no multiple of it goes by elements.
+// the last group of a row whose length is no multiple of it goes by elements.  bfloat16, with the residual: 8192 x 5120 to 8
+// bits 61 us (4.8 TB/s; a large copy 5.1), 4096 x 4096 forward 22 and backward 26 us (read from the last-level cache in part).
 #include <algorithm>
 #include <type_traits>
 

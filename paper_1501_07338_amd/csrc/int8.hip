@@ -549,7 +549,7 @@ static I8Plan i8_plan(int batch, int k, int out, size_t budget) {
   // 8 and 10, of 4 Mi 15 and 14.
   const int64_t weights = (int64_t)k * out;
   if (batch <= 32 || (batch <= 64 && weights <= 1 << 25) || (batch <= 128 && weights <= 1 << 20)) {
-    p.few = batch <= 16 ? 1 : batch <= 32 ? 2 : batch <= 64 ? 4 : 8;
+    p.few = batch <= 64 ? (int)ceil_div(batch, 16) : 8;
     return p;
   }
   const int slabs = (int)ceil_div(k, 64);
@@ -590,6 +590,7 @@ static vcnn_status launch_fc_i8_typed(I8Args a, void* workspace, size_t bytes, h
     else if (a.batch == 2) hipLaunchKernelGGL((i8_dot_kernel<T, 2>), grid, dim3(256), 0, st, a);
     else if (p.few == 1) hipLaunchKernelGGL((i8_rows_kernel<T, 1>), grid, dim3(kRowsThreads), 0, st, a);
     else if (p.few == 2) hipLaunchKernelGGL((i8_rows_kernel<T, 2>), grid, dim3(kRowsThreads), 0, st, a);
+    else if (p.few == 3) hipLaunchKernelGGL((i8_rows_kernel<T, 3>), grid, dim3(kRowsThreads), 0, st, a);
     else if (p.few == 4) hipLaunchKernelGGL((i8_rows_kernel<T, 4>), grid, dim3(kRowsThreads), 0, st, a);
     else hipLaunchKernelGGL((i8_rows_kernel<T, 8>), grid, dim3(kRowsThreads), 0, st, a);
     return check_launch("fc_fwd_i8");

@@ -28,7 +28,7 @@
 // steps: 1.08 PFLOP/s of f16 products (B X of both 1.23, X X^T 1.04, A^2 0.92, whose tiles come in 1.3 rounds of what the chip
 // holds), a plain f16 product of 8192^3 1.32.  The products draw so much power that the clock falls to 1.9 GHz; the
 // matrix cores are then busy 57 to 61 % of the time.  1024 x 4096 takes 0.38 ms, bound by the rate at which a CU reads its
-// cache (X X^T) and by the latency of 32 steps (B X); 64 x 800 68 us and 500 x 800 beside three smaller ones 166, by that of
+// cache (X X^T) and by the latency of 32 steps (B X); 64 x 800 76 us and 500 x 800 beside three smaller ones 166, by that of
 // the launches.
 #include <algorithm>
 
@@ -57,6 +57,7 @@ struct MuonBatch {
   float momentum, keep, lr;  // keep = 1 - lr * weight decay
   int nesterov;
   int turn;                  // which of the two copies of X by columns is read
+  int small;                 // all matrices have at most 64 rows (as X)
   float* shares;             // [kJoinBlocks][64 * 64]: sums of blocks that share a tile
 };
 
@@ -67,8 +68,14 @@ __device__ __forceinline__ uint4* x_rows(const MuonTensor& t) { return t.work; }
 __device__ __forceinline__ uint4* x_cols(const MuonTensor& t, int turn) { return t.work + (2 + 2 * turn) * x_term(t); }
 __device__ __forceinline__ uint4* mat_a(const MuonTensor& t) { return t.work + 6 * x_term(t); }
 __device__ __forceinline__ uint4* mat_b(const MuonTensor& t) { return mat_a(t) + 2 * a_term(t); }
-static inline int64_t work_words(const MuonTensor& t) { return 6 * x_term(t) + 4 * a_term(t) + kNormBlocks * 8 / 16; }
 __device__ __forceinline__ double* norms(const MuonTensor& t) { return reinterpret_cast<double*>(mat_b(t) + 2 * a_term(t)); }
+// X of at most 64 rows as floats, 64 x 64 parts as in LDS below (muon_small_kernel).
+__device__ __forceinline__ float4* x_floats(const MuonTensor& t, int part) {
+  return reinterpret_cast<float4*>(mat_b(t) + 2 * a_term(t) + kNormBlocks * 8 / 16) + (int64_t)part * 1024;
+}
+static inline int64_t work_words(const MuonTensor& t) {
+  return 6 * x_term(t) + 4 * a_term(t) + kNormBlocks * 8 / 16 + (t.small <= 64 ? ceil_div(t.large, 64) * 1024 : 0);
+}
 
 __device__ __forceinline__ int tensor_of(const MuonBatch& b) {
   int t = 0;
@@ -207,11 +214,16 @@ __global__ __launch_bounds__(kThreads) void muon_begin_kernel(MuonBatch b) {
 #pragma unroll
   for (int r = 0; r < 16; ++r) v64[t.tall ? at64(lane, wave * 16 + r) : at64(wave * 16 + r, lane)] = (float)(x[r] * inverse);
   __syncthreads();
+  if (b.small) {
+#pragma unroll
+    for (int n = 0; n < 4; ++n)
+      x_floats(t, j0 / 64)[n * kThreads + threadIdx.x] = reinterpret_cast<const float4*>(v64)[n * kThreads + threadIdx.x];
+  }
   const int by_rows = t.nt * (kPad / 32), by_cols = t.mt * (kPad / 32);
 #pragma unroll
   for (int f = 2 * wave; f < 2 * wave + 2; ++f) {
     put_fragment<false>(v64, x_rows(t), x_term(t), word_of(i0, j0, by_rows), by_rows, f, AsIs());
-    put_fragment<true>(v64, x_cols(t, b.turn), x_term(t), word_of(j0, i0, by_cols), by_cols, f, AsIs());
+    if (!b.small) put_fragment<true>(v64, x_cols(t, b.turn), x_term(t), word_of(j0, i0, by_cols), by_cols, f, AsIs());
   }
 }
 
@@ -359,12 +371,13 @@ struct FewTile {
   // part(v64, 0, 0, f0, f1): the whole tile for every wave, fragments f0 .. f1 are its own
   template <typename F>
   __device__ static __forceinline__ void run(const Operand& a, const Operand& b, int steps, uint4* smem, F part) {
-    sum(a, b, 0, steps, smem);
+    sum<3>(a, b, 0, steps, smem);
     __syncthreads();
     const int wave = threadIdx.x >> 6;
     part(reinterpret_cast<float*>(smem), 0, 0, wave, wave + 1);
   }
-  // Steps s0 .. s0 + steps, as values in LDS; every thread writes places n * 512 + threadIdx.x (of four values), n < 2.
+  // Steps s0 .. s0 + steps by three term products or all four, as values in LDS; every thread writes places n * 512 + threadIdx.x (of four values), n < 2.
+  template <int PRODUCTS>
   __device__ static __forceinline__ void sum(const Operand& a, const Operand& b, int s0, int steps, uint4* smem) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint4* src[8][2];  // [row tile of either operand][term]: wave-uniform
@@ -388,11 +401,11 @@ struct FewTile {
     };
     auto products = [&](const uint4 (&x)[8][2]) {
 #pragma unroll
-      for (int p = 0; p < 3; ++p)
+      for (int p = 0; p < PRODUCTS; ++p)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) acc[i][j] = mfma_f16(x[i][p == 2], x[4 + j][p == 1], acc[i][j]);
+          for (int j = 0; j < 4; ++j) acc[i][j] = mfma_f16(x[i][p >> 1], x[4 + j][p & 1], acc[i][j]);
     };
     if (mine > 0) {
       fetch(0, f);
@@ -503,7 +516,7 @@ __global__ __launch_bounds__(FewTile::THREADS, 2) void muon_share_kernel(MuonBat
   y.row_tile = jt * 4;
   const int steps = (t.large + 31) / 32;
   const int s0 = (int)((int64_t)steps * part / t.parts), s1 = (int)((int64_t)steps * (part + 1) / t.parts);
-  FewTile::sum(x, y, s0, s1 - s0, smem16);
+  FewTile::sum<4>(x, y, s0, s1 - s0, smem16);  // (the fragments' way here takes longer than the products)
 #pragma unroll
   for (int n = 0; n < 2; ++n)
     reinterpret_cast<float4*>(b.shares)[blockIdx.x * 1024 + n * 512 + threadIdx.x] = reinterpret_cast<const float4*>(smem16)[n * 512 + threadIdx.x];
@@ -535,35 +548,17 @@ __global__ __launch_bounds__(FewTile::THREADS) void muon_join_kernel(MuonBatch b
   put_symmetric<MUON_A>(t, v64, it * 64, jt * 64, it != jt, wave, wave + 1);
 }
 
-// X <- a X + B X of a 64 x 64 part at (i0, j0), given B X; the last one: the result, or the weights moved by it.  Fragments
-// f0 .. f1 are this wave's; waves that share a part all come here.
-template <bool LAST>
-__device__ __forceinline__ void put_applied(const MuonBatch& b, const MuonTensor& t, float* v64, int i0, int j0, int f0, int f1) {
-  const bool inside = i0 < t.mt * kPad && j0 < t.nt * kPad;  // (the same for all waves that share a part)
+// X' of a 64 x 64 part at (i0, j0) to where the next step finds it; after the last one: the result, or the weights moved by it.
+// Fragments f0 .. f1 are this wave's.  COLS: X is read by columns too.
+template <bool LAST, bool COLS = true>
+__device__ __forceinline__ void put_next(const MuonBatch& b, const MuonTensor& t, const float* v64, int i0, int j0, int f0, int f1) {
   const int lane = threadIdx.x & 63;
   const int steps_n = t.nt * (kPad / 32), steps_m = t.mt * (kPad / 32);
-  const int64_t by_rows = word_of(i0, j0, steps_n);
-  if (inside) {
-#pragma unroll 2
-    for (int f = f0; f < f1; ++f) {  // a X, from X by rows (whose place the same lanes write below)
-      const int row = (f >> 1) * 16 + (lane & 15), k = (f & 1) * 32 + (lane >> 4) * 8;
-      float v[8];
-      join8(x_rows(t), x_term(t), by_rows + ((int64_t)(f >> 1) * steps_n + (f & 1)) * 64 + lane, v);
-#pragma unroll
-      for (int e = 0; e < 8; e += 4) {
-        float4* const p = reinterpret_cast<float4*>(v64 + at64(row, k + e));
-        const float4 u = *p;
-        *p = make_float4(fmaf(kA, v[e], u.x), fmaf(kA, v[e + 1], u.y), fmaf(kA, v[e + 2], u.z), fmaf(kA, v[e + 3], u.w));
-      }
-    }
-  }
-  if (f1 - f0 < 8) __syncthreads();  // (a part of several waves)
-  if (!inside) return;
   if constexpr (!LAST) {
 #pragma unroll 2
     for (int f = f0; f < f1; ++f) {
-      put_fragment<false>(v64, x_rows(t), x_term(t), by_rows, steps_n, f, AsIs());
-      put_fragment<true>(v64, x_cols(t, b.turn ^ 1), x_term(t), word_of(j0, i0, steps_m), steps_m, f, AsIs());
+      put_fragment<false>(v64, x_rows(t), x_term(t), word_of(i0, j0, steps_n), steps_n, f, AsIs());
+      if (COLS) put_fragment<true>(v64, x_cols(t, b.turn ^ 1), x_term(t), word_of(j0, i0, steps_m), steps_m, f, AsIs());
     }
   } else {
     const float step = b.lr * t.factor;
@@ -595,6 +590,31 @@ __device__ __forceinline__ void put_applied(const MuonBatch& b, const MuonTensor
   }
 }
 
+// X <- a X + B X of such a part, given B X.  Waves that share a part all come here.
+template <bool LAST>
+__device__ __forceinline__ void put_applied(const MuonBatch& b, const MuonTensor& t, float* v64, int i0, int j0, int f0, int f1) {
+  const bool inside = i0 < t.mt * kPad && j0 < t.nt * kPad;  // (the same for all waves that share a part)
+  const int lane = threadIdx.x & 63;
+  const int steps_n = t.nt * (kPad / 32);
+  const int64_t by_rows = word_of(i0, j0, steps_n);
+  if (inside) {
+#pragma unroll 2
+    for (int f = f0; f < f1; ++f) {  // a X, from X by rows (whose place the same lanes write below)
+      const int row = (f >> 1) * 16 + (lane & 15), k = (f & 1) * 32 + (lane >> 4) * 8;
+      float v[8];
+      join8(x_rows(t), x_term(t), by_rows + ((int64_t)(f >> 1) * steps_n + (f & 1)) * 64 + lane, v);
+#pragma unroll
+      for (int e = 0; e < 8; e += 4) {
+        float4* const p = reinterpret_cast<float4*>(v64 + at64(row, k + e));
+        const float4 u = *p;
+        *p = make_float4(fmaf(kA, v[e], u.x), fmaf(kA, v[e + 1], u.y), fmaf(kA, v[e + 2], u.z), fmaf(kA, v[e + 3], u.w));
+      }
+    }
+  }
+  if (f1 - f0 < 8) __syncthreads();  // (a part of several waves)
+  if (inside) put_next<LAST>(b, t, v64, i0, j0, f0, f1);
+}
+
 template <typename TILE, bool LAST>
 __global__ __launch_bounds__(TILE::THREADS, 2) void muon_apply_kernel(MuonBatch b) {
   extern __shared__ uint4 smem16[];
@@ -611,25 +631,21 @@ __global__ __launch_bounds__(TILE::THREADS, 2) void muon_apply_kernel(MuonBatch 
 }
 
 // Matrices of at most 64 rows (as X): a block adds the shares of A by itself, makes B of it and then its 64 columns of X, in place
-// of three launches with a few blocks each.  A wave makes two 16 x 16 tiles of either product.
+// of three launches with a few blocks each.  The products are small (a wave makes two 16 x 16 tiles of either) and their sums
+// short, so that float products would round little: these are float products, of X kept in floats beside the terms that the
+// shares are made of.  (With term products here the error was up to twice that of float products, 64 x 800 in 68 us, not 76: a
+// float product has an eighth of the rate, and a block waits 1 us for each.)
 template <bool LAST>
 __global__ __launch_bounds__(512) void muon_small_kernel(MuonBatch b) {
-  __shared__ __attribute__((aligned(16))) float v64[64 * 64];
-  __shared__ uint4 frag[8][2][64];  // [4 row tiles][2 steps], [term]
+  __shared__ __attribute__((aligned(16))) float v64[64 * 64], x64[64 * 64];
   const int at_tensor = tensor_of(b);
   const MuonTensor& t = b.t[at_tensor];
   const int j0 = (blockIdx.x - b.first[at_tensor]) * 64;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int rt = wave >> 1, ct = (wave & 1) * 2;
-  uint4 x[2][2][2];  // [tile][step][term] of X by columns
-#pragma unroll
-  for (int c = 0; c < 2; ++c)
-#pragma unroll
-    for (int s = 0; s < 2; ++s)
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-        x[c][s][h] = x_cols(t, b.turn)[h * x_term(t) + word_of(j0 + (ct + c) * 16, s * 32, t.mt * (kPad / 32)) + lane];
+  const int rt = (wave >> 1) * 16, ct = (wave & 1) * 32, in = lane & 15, k4 = lane >> 4;  // rows, columns of the wave's tiles
+  float4* const kept = x_floats(t, j0 / 64) + threadIdx.x;
   const float4* const from = reinterpret_cast<const float4*>(b.shares) + (int64_t)t.share0 * 1024 + threadIdx.x;
+  const float4 x[2] = {kept[0], kept[512]};
   float4 v[2] = {from[0], from[512]};
 #pragma unroll 4
   for (int p = 1; p < t.parts; ++p)
@@ -639,52 +655,53 @@ __global__ __launch_bounds__(512) void muon_small_kernel(MuonBatch b) {
       v[h].x += u.x, v[h].y += u.y, v[h].z += u.z, v[h].w += u.w;
     }
 #pragma unroll
-  for (int h = 0; h < 2; ++h) reinterpret_cast<float4*>(v64)[h * 512 + threadIdx.x] = v[h];
+  for (int h = 0; h < 2; ++h) {
+    reinterpret_cast<float4*>(v64)[h * 512 + threadIdx.x] = v[h];
+    reinterpret_cast<float4*>(x64)[h * 512 + threadIdx.x] = x[h];
+  }
   __syncthreads();
-  const auto take = [&]() {  // the values' fragment `wave`
-    const int row = rt * 16 + (lane & 15), k = (wave & 1) * 32 + (lane >> 4) * 8;
-    float u[8];
+  // v_mfma_f32_16x16x4_f32: lane l holds row l % 16 of one operand, column l % 16 of the other, contraction l / 16
+  const auto product = [&](auto column, f32x4 (&acc)[2]) {  // two halves of the sum at once
+    f32x4 part[2][2] = {};
 #pragma unroll
-    for (int e = 0; e < 8; ++e) u[e] = v64[at64(row, k + e)];
-    uint4 hi, lo;
-    split8(u, &hi, &lo);
-    frag[wave][0][lane] = hi, frag[wave][1][lane] = lo;
+    for (int n = 0; n < 8; ++n)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int k = h * 32 + n * 4 + k4;
+        const float row = v64[at64(rt + in, k)];
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+          part[h][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(row, column(k, ct + c * 16 + in), part[h][c], 0, 0, 0);
+      }
+#pragma unroll
+    for (int c = 0; c < 2; ++c) acc[c] = part[0][c] + part[1][c];
   };
-  take();
+  f32x4 acc[2];
+  product([&](int k, int j) { return v64[at64(j, k)]; }, acc);
   __syncthreads();
-  f32x4 acc[2] = {};
-#pragma unroll
-  for (int s = 0; s < 2; ++s)
-#pragma unroll
-    for (int p = 0; p < 3; ++p)
-#pragma unroll
-      for (int c = 0; c < 2; ++c)
-        acc[c] = mfma_f16(frag[rt * 2 + s][p == 2][lane], frag[(ct + c) * 2 + s][p == 1][lane], acc[c]);
 #pragma unroll
   for (int c = 0; c < 2; ++c)
 #pragma unroll
     for (int q = 0; q < 4; ++q) {  // B in A's place: every value is one lane's own
-      float* const at = v64 + at64(rt * 16 + (lane >> 4) * 4 + q, (ct + c) * 16 + (lane & 15));
-      *at = fmaf(kC * (kUnscale * kUnscale), acc[c][q], kB * *at);
+      float* const at = v64 + at64(rt + 4 * k4 + q, ct + c * 16 + in);
+      *at = fmaf(kC, acc[c][q], kB * *at);
     }
   __syncthreads();
-  take();
+  product([&](int k, int j) { return x64[at64(k, j)]; }, acc);
   __syncthreads();
-#pragma unroll
-  for (int c = 0; c < 2; ++c) acc[c] = (f32x4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int s = 0; s < 2; ++s)
-#pragma unroll
-    for (int p = 0; p < 3; ++p)
-#pragma unroll
-      for (int c = 0; c < 2; ++c) acc[c] = mfma_f16(frag[rt * 2 + s][p == 2][lane], x[c][s][p == 1], acc[c]);
 #pragma unroll
   for (int c = 0; c < 2; ++c)
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-      v64[at64(rt * 16 + (lane >> 4) * 4 + q, (ct + c) * 16 + (lane & 15))] = acc[c][q] * (kUnscale * kUnscale);
+    for (int q = 0; q < 4; ++q) {
+      const int at = at64(rt + 4 * k4 + q, ct + c * 16 + in);
+      v64[at] = fmaf(kA, x64[at], acc[c][q]);
+    }
   __syncthreads();
-  put_applied<LAST>(b, t, v64, 0, j0, wave, wave + 1);
+  if (!LAST) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) kept[h * 512] = reinterpret_cast<const float4*>(v64)[h * 512 + threadIdx.x];
+  }
+  put_next<LAST, false>(b, t, v64, 0, j0, wave, wave + 1);
 }
 
 // ---- launches -----------------------------------------------------------------------------------------------------------
@@ -810,14 +827,14 @@ vcnn_status launch_muon(const MuonTensor* tensors, int count, float lr, float mo
     b.t[t].work = work;
     work += work_words(b.t[t]);
   }
+  b.small = 1;  // a step is two launches then (64 x 800: five steps 68 us, with three launches each 107)
+  for (int t = 0; t < b.tensors; ++t) b.small = b.small && b.t[t].small <= 64;
   const auto norm_blocks = [](const MuonTensor& t) { return t.norm_blocks; };
   const auto parts = [](const MuonTensor& t) { return ceil_div(t.small, 64) * ceil_div(t.large, 64); };
   if (vcnn_status s = launch_phase("muon moment", muon_moment_kernel, &b, kThreads, 0, st, norm_blocks)) return s;
   if (vcnn_status s = launch_phase("muon begin", muon_begin_kernel, &b, kThreads, 0, st, parts)) return s;
-  bool small = true;  // all of them: a step is two launches (64 x 800: five steps 68 us, with three launches each 107)
-  for (int t = 0; t < b.tensors; ++t) small = small && b.t[t].small <= 64;
   for (int i = 0; i < steps; ++i, b.turn ^= 1) {
-    if (small) {
+    if (b.small) {
       const auto columns = [](const MuonTensor& t) { return ceil_div(t.large, 64); };
       if (vcnn_status s = launch_shares(&b, b.tensors, 8, 16, st)) return s;
       if (vcnn_status s = i + 1 < steps ? launch_phase("muon small", muon_small_kernel<false>, &b, 512, 0, st, columns)

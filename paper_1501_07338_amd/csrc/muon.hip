@@ -827,7 +827,7 @@ vcnn_status launch_muon(const MuonTensor* tensors, int count, float lr, float mo
     b.t[t].work = work;
     work += work_words(b.t[t]);
   }
-  b.small = 1;  // a step is two launches then (64 x 800: five steps 68 us, with three launches each 107)
+  b.small = 1;  // a step is two launches then (64 x 800: five steps 76 us, with three launches each 107)
   for (int t = 0; t < b.tensors; ++t) b.small = b.small && b.t[t].small <= 64;
   const auto norm_blocks = [](const MuonTensor& t) { return t.norm_blocks; };
   const auto parts = [](const MuonTensor& t) { return ceil_div(t.small, 64) * ceil_div(t.large, 64); };

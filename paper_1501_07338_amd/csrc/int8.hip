@@ -180,16 +180,20 @@ __global__ __launch_bounds__(256) void i8_dot_kernel(I8Args a) {
 }
 
 // ---- few samples -------------------------------------------------------------------------------------------------------
-// Lane l holds row l % 16 of either operand and, of the 128 bytes of a step, the 32 from 32 (l / 16) on as two
-// instructions' words: a row's 128 bytes are read whole, and the order of a sum's terms is free.
+// Lane l holds row l % 16 of either operand and, of the 128 bytes of a step, the 16 from 16 (l / 16) on and the 16 that are 64
+// further: each load takes 64 neighbouring bytes of a row (with 32 neighbouring bytes a lane, in two loads that share every
+// 64, 32 samples of 16 Mi weights took 9.2 us, not 8.7).  With one tile of samples four steps are on their way at once, with
+// more two, for the registers of four leave a CU one block: 16 samples 6.9 and 7.8 us (four, two), 32 9.0 and 8.7, 48 samples
+// 4000 -> 4096 11.9 and 10.4; 48 samples 4096 -> 4096 take 11.2 either way, and 60 samples
+// 3000 -> 5000 lose, 13.7 and 14.6.
 static constexpr int kRowsThreads = 512;
 
 template <typename T, int NB>
 __global__ __launch_bounds__(kRowsThreads) void i8_rows_kernel(I8Args a) {
-  constexpr int AHEAD = NB <= 4 ? 4 : 2, WAVES = kRowsThreads / 64;
+  constexpr int AHEAD = NB == 1 ? 4 : 2, WAVES = kRowsThreads / 64;
   __shared__ int share[WAVES - 1][NB][4][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int o0 = blockIdx.x * 16, row = lane & 15, at = (lane >> 4) * 32;
+  const int o0 = blockIdx.x * 16, row = lane & 15, at = (lane >> 4) * 16;
   const int8_t* const w = a.w + (int64_t)min(o0 + row, a.out - 1) * a.k;
   const int8_t* x[NB];
   i32x4 acc[NB];
@@ -207,11 +211,11 @@ __global__ __launch_bounds__(kRowsThreads) void i8_rows_kernel(I8Args a) {
       const int c = (s + WAVES * u) * 128 + at;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const Loose16i p = *reinterpret_cast<const Loose16i*>(w + c + 16 * i);
+        const Loose16i p = *reinterpret_cast<const Loose16i*>(w + c + 64 * i);
         fw[u][i] = make_uint4(p.w[0], p.w[1], p.w[2], p.w[3]);
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
-          const Loose16i q = *reinterpret_cast<const Loose16i*>(x[n] + c + 16 * i);
+          const Loose16i q = *reinterpret_cast<const Loose16i*>(x[n] + c + 64 * i);
           fx[u][n][i] = make_uint4(q.w[0], q.w[1], q.w[2], q.w[3]);
         }
       }
@@ -227,9 +231,9 @@ __global__ __launch_bounds__(kRowsThreads) void i8_rows_kernel(I8Args a) {
     const int c = s * 128 + at;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const uint4 fw = load16(w, c + 16 * i, a.k);
+      const uint4 fw = load16(w, c + 64 * i, a.k);
 #pragma unroll
-      for (int n = 0; n < NB; ++n) acc[n] = mfma_i8(fw, load16(x[n], c + 16 * i, a.k), acc[n]);
+      for (int n = 0; n < NB; ++n) acc[n] = mfma_i8(fw, load16(x[n], c + 64 * i, a.k), acc[n]);
     }
   }
   if (wave > 0) {

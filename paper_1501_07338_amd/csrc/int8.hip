@@ -182,10 +182,10 @@ __global__ __launch_bounds__(256) void i8_dot_kernel(I8Args a) {
 // ---- few samples -------------------------------------------------------------------------------------------------------
 // Lane l holds row l % 16 of either operand and, of the 128 bytes of a step, the 16 from 16 (l / 16) on and the 16 that are 64
 // further: each load takes 64 neighbouring bytes of a row (with 32 neighbouring bytes a lane, in two loads that share every
-// 64, 32 samples of 16 Mi weights took 9.2 us, not 8.7).  With one tile of samples four steps are on their way at once, with
+// 64, 32 samples of 16 Mi weights took 9.2 us, not 9.0).  With one tile of samples four steps are on their way at once, with
 // more two, for the registers of four leave a CU one block: 16 samples 6.9 and 7.8 us (four, two), 32 9.0 and 8.7, 48 samples
-// 4000 -> 4096 11.9 and 10.4; 48 samples 4096 -> 4096 take 11.2 either way, and 60 samples
-// 3000 -> 5000 lose, 13.7 and 14.6.
+// 4000 -> 4096 11.9 and 10.4; 48 samples 4096 -> 4096 take 11.2 either way, and 60 samples 3000 -> 5000
+// lose, 13.7 and 14.6.
 static constexpr int kRowsThreads = 512;
 
 template <typename T, int NB>

@@ -276,8 +276,11 @@ __global__ __launch_bounds__(WAVE ? kWaveThreads : NV ? kKeptThreads : 1024, NV 
     const T* const kept = added ? h : x;  // (rows read twice: every thread meets its own elements again)
     float rstd = 1.f;
     if (MODE != QUANT_I8) {
-      rstd = 1.f / sqrtf(sum / (float)cols + a.eps);
-      if (!(sum < __builtin_inff())) {  // squares beyond the float range (or not finite): once more in double
+      const float mean = sum / (float)cols + a.eps;
+      rstd = 1.f / sqrtf(mean);
+      // squares beyond the float range (or not finite), or so small that their roundings, up to 2^-150 each, are seen in the
+      // mean (only with an eps as small): once more in double
+      if (!(sum < __builtin_inff()) || mean < 0x1p-120f) {
         double wide = 0.;
         if constexpr (NV > 0) {
 #pragma unroll

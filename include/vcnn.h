@@ -252,7 +252,7 @@ vcnn_status vcnn_sgd_update_multi(int32_t tensors, const size_t* counts, float* 
  * the residual's addition before it:
  *     h = x + residual (rounded to dtype),   rstd[r] = 1 / sqrt(mean_c h[r][c]^2 + eps),   y[r][c] = h[r][c] * rstd[r] * gain[c]
  * x, residual, h, y follow dtype; gain [cols] and rstd [rows] are float; sums are float (double where the squares leave its
- * range).  residual may be NULL: then h is x, and the argument h is not used.  rstd may be NULL; vcnn_rmsnorm_bwd needs it.
+ * range, and between the groups of rows of more than 16384 elements).  residual may be NULL: then h is x, and the argument h is not used.  rstd may be NULL; vcnn_rmsnorm_bwd needs it.
  * eps must be positive and finite, cols at most 2^30.  h may be x or residual itself (an update of the residual stream in place), y may be x
  * where h is not; nothing else may overlap.  A row with an infinity or NaN gives what the formula gives, in that row alone. */
 vcnn_status vcnn_rmsnorm_fwd(int32_t dtype, int32_t rows, int32_t cols, float eps, const void* x, const void* residual,

@@ -136,18 +136,21 @@ __device__ __forceinline__ double wave_sum(double v) {
 struct RowSums {  // one slot per wave; rows of even and odd turns take turns, so that a row needs one barrier
   float sum[2][kMaxWaves];
   uint32_t most[2][kMaxWaves];
-  double wide[kMaxWaves];
+  double wide[2][kMaxWaves], again[kMaxWaves];
+  __device__ __forceinline__ float* of(float, int turn) { return sum[turn]; }
+  __device__ __forceinline__ double* of(double, int turn) { return wide[turn]; }
 };
 // Sum (and largest magnitude's bits) over the row's threads, in every thread.
-template <bool WAVE>
-__device__ __forceinline__ void row_reduce(RowSums& s, int turn, float& sum, uint32_t& most) {
+template <bool WAVE, typename S>
+__device__ __forceinline__ void row_reduce(RowSums& s, int turn, S& sum, uint32_t& most) {
   sum = wave_sum(sum), most = wave_max(most);
   if constexpr (!WAVE) {
+    S* const sums = s.of(sum, turn);
     const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-    if ((threadIdx.x & 63) == 0) s.sum[turn][wave] = sum, s.most[turn][wave] = most;
+    if ((threadIdx.x & 63) == 0) sums[wave] = sum, s.most[turn][wave] = most;
     __syncthreads();
-    sum = 0.f, most = 0;
-    for (int w = 0; w < waves; ++w) sum += s.sum[turn][w], most = max(most, s.most[turn][w]);
+    sum = 0, most = 0;
+    for (int w = 0; w < waves; ++w) sum += sums[w], most = max(most, s.most[turn][w]);
   }
 }
 template <bool WAVE>
@@ -156,13 +159,19 @@ __device__ __forceinline__ double row_reduce(RowSums& s, double sum) {
   if constexpr (!WAVE) {
     const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
     __syncthreads();
-    if ((threadIdx.x & 63) == 0) s.wide[wave] = sum;
+    if ((threadIdx.x & 63) == 0) s.again[wave] = sum;
     __syncthreads();
     sum = 0.;
-    for (int w = 0; w < waves; ++w) sum += s.wide[w];
+    for (int w = 0; w < waves; ++w) sum += s.again[w];
   }
   return sum;
 }
+// What a thread adds its share of a row in.  Kept rows: at most 32 elements, in float.  Rows read twice: any number, and the
+// roundings of equal elements do not cancel, so the groups of one load, each added in float, are added in double (a row of
+// 3.2 million elements of 1.1 came out 1e-5 off in float; forward takes 1 to 4 % longer, 4096 x 20000 of bfloat16 85.3 us, not
+// 84.0, backward the same).
+template <int NV>
+using RowSum = std::conditional_t<(NV > 0), float, double>;
 
 // round(127 u / a), ties to even, for |u| <= a, a > 0: the quotient in float is off by at most 127 * 2^-23 = 1.5e-5, so only
 // a quotient within 1e-4 of the middle between two integers (one in 5000) needs the one rounded once in double, which is
@@ -238,15 +247,17 @@ __global__ __launch_bounds__(WAVE ? kWaveThreads : NV ? kKeptThreads : 1024, NV 
       unpack(ph, v);
       store_group(h, c, cols, ph);
     };
-    float sum = 0.f;
+    RowSum<NV> sum = 0;
     uint32_t most = 0;
     auto count = [&](const float (&v)[N], const float (&g)[N]) {
+      float part = NV > 0 ? (float)sum : 0.f;
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        if (MODE != QUANT_I8) sum = fmaf(v[i], v[i], sum);
+        if (MODE != QUANT_I8) part = fmaf(v[i], v[i], part);
         if (MODE == NORM_I8) most = max(most, __float_as_uint(v[i] * g[i]) & 0x7fffffffu);
         if (MODE == QUANT_I8) most = max(most, __float_as_uint(v[i]) & 0x7fffffffu);
       }
+      sum = NV > 0 ? part : sum + part;
     };
     float v[NV ? NV : 1][N];
     if constexpr (NV > 0) {
@@ -276,11 +287,11 @@ __global__ __launch_bounds__(WAVE ? kWaveThreads : NV ? kKeptThreads : 1024, NV 
     const T* const kept = added ? h : x;  // (rows read twice: every thread meets its own elements again)
     float rstd = 1.f;
     if (MODE != QUANT_I8) {
-      const float mean = sum / (float)cols + a.eps;
+      const float total = (float)sum, mean = total / (float)cols + a.eps;
       rstd = 1.f / sqrtf(mean);
       // squares beyond the float range (or not finite), or so small that their roundings, up to 2^-150 each, are seen in the
       // mean (only with an eps as small): once more in double
-      if (!(sum < __builtin_inff()) || mean < 0x1p-120f) {
+      if (!(total < __builtin_inff()) || mean < 0x1p-120f) {
         double wide = 0.;
         if constexpr (NV > 0) {
 #pragma unroll
@@ -447,12 +458,14 @@ __global__ __launch_bounds__(WAVE ? kWaveThreads : NV ? kKeptThreads : 1024) voi
     T* const dh = reinterpret_cast<T*>(a.dh) + row * cols;
     const float rstd = a.rstd[row];
     Loose16 ph[K], pd[K], pa[K];
-    float dot = 0.f;
+    RowSum<NV> dot = 0;
     // t z, z = h s: of the magnitude of dy, so that the sum stays in range wherever h is
     auto meet = [&](const Loose16& gh, const Loose16& gd, const float (&g)[N], float (&z)[N], float (&d)[N]) {
       unpack(gh, z), unpack(gd, d);
+      float part = NV > 0 ? (float)dot : 0.f;
 #pragma unroll
-      for (int i = 0; i < N; ++i) z[i] *= rstd, dot = fmaf(d[i] * g[i], z[i], dot);
+      for (int i = 0; i < N; ++i) z[i] *= rstd, part = fmaf(d[i] * g[i], z[i], part);
+      dot = NV > 0 ? part : dot + part;
     };
     if constexpr (NV > 0) {
 #pragma unroll
@@ -487,7 +500,7 @@ __global__ __launch_bounds__(WAVE ? kWaveThreads : NV ? kKeptThreads : 1024) voi
     uint32_t none = 0;
     row_reduce<WAVE>(sums, turn, dot, none);
     if (!a.dh) continue;
-    const float mean = dot / (float)cols;
+    const float mean = (float)dot / (float)cols;
     auto give = [&](int c, const Loose16& gh, const Loose16& gd, const Loose16& ga, const float (&g)[N]) {
       float hv[N], d[N], o[N];
       unpack(gh, hv), unpack(gd, d);

@@ -1,9 +1,15 @@
-"""The norm where its sums are delicate: squares below the float range.  Tolerances are those of test_gpu_norm."""
+"""The norm where its sums are delicate: squares below the float range, and rows of millions of like values, whose
+roundings do not cancel.
+
+Tolerances are those of test_gpu_norm, but for long rows: there a group of at most 8 elements is added in float and groups
+in double, so that the roundings of a sum, LONG, do not grow with the row."""
 import pytest
 import torch
 
 from paper_1501_07338_amd import vcnn
-from test_gpu_norm import U, Guarded, depth, dev, gain_of, tensor
+from test_gpu_norm import DEV, EXTRA, TYPES, U, Guarded, depth, dev, gain_of, half_step, tensor
+
+LONG = 8 + EXTRA
 
 
 @pytest.mark.gpu
@@ -25,3 +31,36 @@ def test_squares_below_the_float_range(cols, eps):
     vcnn.rmsnorm_fwd_i8(vcnn.F32, rows, cols, eps, dev(x), None, dev(gain), None, q.t, s.t)
     scale = (x * gain).abs().amax(1).double() * rstd / 127
     assert bool(((s.cpu().double() - scale).abs() <= scale * depth(cols) * U + 2.0 ** -149).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [vcnn.F32, vcnn.BF16])
+@pytest.mark.parametrize("cols", [64 * 224 * 224, 16 * 131 * 131 + 5])
+def test_long_rows_of_like_values(cols, dtype):
+    """The activations of a convolution as one row: all of them 1.1 (and one row with a few negative ones)."""
+    rows, eps = 2, 1e-6
+    h = torch.full((rows, cols), 1.1).to(TYPES[dtype])
+    h[1, ::7] = -0.7
+    dy, gain = torch.full_like(h, 0.3), torch.full((cols,), 0.9)
+    dy[1, ::5] = 0.8
+    hd, t = h.double(), dy.double() * gain.double()
+    rstd = (hd.square().mean(1) + eps).rsqrt()
+    s, y = Guarded((rows,), torch.float32), Guarded((rows, cols), h.dtype)
+    vcnn.rmsnorm_fwd(dtype, rows, cols, eps, dev(h), None, dev(gain), None, y.t, s.t)
+    assert bool(((s.cpu().double() - rstd).abs() <= rstd * LONG * U).all())
+    want = hd * rstd[:, None] * gain.double()
+    assert bool(((y.cpu().double() - want).abs() <= want.abs() * (half_step(dtype) * 1.01 + LONG * U)).all())
+    q, s8 = Guarded((rows, cols), torch.int8), Guarded((rows,), torch.float32)
+    vcnn.rmsnorm_fwd_i8(dtype, rows, cols, eps, dev(h), None, dev(gain), None, q.t, s8.t)
+    scale = (h.float() * gain).abs().amax(1).double() * rstd / 127
+    assert bool(((s8.cpu().double() - scale).abs() <= scale * LONG * U).all())
+    z = hd * rstd[:, None]
+    want = rstd[:, None] * (t - z * (t * z).mean(1, keepdim=True))  # (like values cancel: the error is that of the terms)
+    size = rstd[:, None] * (t.abs() + z.abs() * (t * z).abs().mean(1, keepdim=True))
+    dh, dg = Guarded((rows, cols), h.dtype), Guarded((cols,), torch.float32)
+    ws = torch.empty(vcnn.rmsnorm_workspace_bytes(rows, cols), dtype=torch.uint8, device=DEV)
+    vcnn.rmsnorm_bwd(dtype, rows, cols, dev(h), dev(gain), rstd.float().to(DEV), dev(dy), None, dh.t, dg.t, ws)
+    off = (dh.cpu().double() - want).abs()
+    assert bool((off <= want.abs() * half_step(dtype) * 1.01 + size * LONG * U + 1e-40).all())
+    want = (dy.double() * z).sum(0)
+    assert bool(((dg.cpu().double() - want).abs() <= (dy.double() * z).abs().sum(0) * LONG * U).all())

@@ -559,7 +559,7 @@ __global__ __launch_bounds__(WAVE ? kWaveThreads : NV ? kKeptThreads : 1024) voi
 // dg[c] = the blocks' shares: 64 threads a column take every 64th, and their sums are added in pairs, always the same ones.
 __global__ __launch_bounds__(1024) void gain_grad_kernel(const float* partial, float* dg, int blocks, int cols) {
   __shared__ float sums[64][17];
-  const int in = threadIdx.x & 15, col = blockIdx.x * 16 + in, part = threadIdx.x >> 4;
+  const int in = threadIdx.x & 15, col = (blockIdx.y * gridDim.x + blockIdx.x) * 16 + in, part = threadIdx.x >> 4;
   float s = 0.f;
   if (col < cols) {
 #pragma unroll 8
@@ -594,7 +594,8 @@ vcnn_status launch_rmsnorm_bwd(int dtype, int rows, int cols, const void* h, con
   const int blocks = dtype == VCNN_BF16 ? launch_norm_bwd_typed<bf16>(a, st) : launch_norm_bwd_typed<float>(a, st);
   if (vcnn_status s = check_launch("rmsnorm_bwd")) return s;
   if (!dgain) return VCNN_OK;
-  hipLaunchKernelGGL(gain_grad_kernel, dim3((unsigned)ceil_div(cols, 16)), dim3(1024), 0, st, partial, dgain, blocks, cols);
+  const unsigned groups = (unsigned)ceil_div(cols, 16), wide = std::min(groups, 1u << 16);  // (2^32 threads are no grid's width)
+  hipLaunchKernelGGL(gain_grad_kernel, dim3(wide, (unsigned)ceil_div(groups, wide)), dim3(1024), 0, st, partial, dgain, blocks, cols);
   return check_launch("rmsnorm_bwd gain");
 }
 

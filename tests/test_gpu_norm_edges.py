@@ -64,3 +64,21 @@ def test_long_rows_of_like_values(cols, dtype):
     assert bool((off <= want.abs() * half_step(dtype) * 1.01 + size * LONG * U + 1e-40).all())
     want = (dy.double() * z).sum(0)
     assert bool(((dg.cpu().double() - want).abs() <= (dy.double() * z).abs().sum(0) * LONG * U).all())
+
+
+@pytest.mark.gpu
+def test_gain_gradient_of_more_columns_than_a_grid_is_wide():
+    """2^26 columns and a few: sixteen a block of 1024 threads would be 2^32 threads and more in one dimension."""
+    rows, cols = 2, (1 << 26) + 37
+    g = torch.Generator(device=DEV).manual_seed(81)
+    h = torch.randn(rows, cols, device=DEV, generator=g).to(torch.bfloat16)
+    dy = torch.randn(rows, cols, device=DEV, generator=g).to(torch.bfloat16)
+    gain, rstd = torch.ones(cols, device=DEV), torch.tensor([0.7, 1.9], device=DEV)
+    dg = Guarded((cols,), torch.float32)
+    ws = torch.empty(vcnn.rmsnorm_workspace_bytes(rows, cols), dtype=torch.uint8, device=DEV)
+    vcnn.rmsnorm_bwd(vcnn.BF16, rows, cols, h, gain, rstd, dy, None, None, dg.t, ws)
+    dg.cpu()
+    for a in range(0, cols, 1 << 24):
+        part = slice(a, a + (1 << 24))
+        terms = dy[:, part].double() * h[:, part].double() * rstd.double()[:, None]
+        assert bool(((dg.t[part].double() - terms.sum(0)).abs() <= terms.abs().sum(0) * 4 * U).all())

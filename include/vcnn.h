@@ -280,7 +280,7 @@ vcnn_status vcnn_quant_rows_i8(int32_t dtype, int32_t rows, int32_t cols, const 
  *     y[b][o] = act(bias[o] + xscale[b] * wscale[o] * sum_i xq[b][i] * wq[o][i])
  * with xq [batch][in_f], wq [out_f][in_f] int8 and a float scale per row of either (vcnn_rmsnorm_fwd_i8, vcnn_quant_rows_i8, or
  * the caller's own); bias is float and may be NULL; y [batch][out_f] follows dtype.  The sums are exact; a scale of NaN gives
- * NaN.  in_f is at most 131071 (sums of 32 bits; VCNN_ERR_UNSUPPORTED).  Rows may start at any byte; in_f a multiple of 16 and
+ * NaN.  in_f is at most 131071 (sums of 32 bits; VCNN_ERR_UNSUPPORTED), out_f at most 2^26.  Rows may start at any byte; in_f a multiple of 16 and
  * 16-byte aligned operands are faster with more than 64 samples.  workspace: vcnn_fc_i8_workspace_bytes (0 for most
  * layers) divides the sums of layers with few tiles over more of the chip; with less of it, or none (NULL, 0), the call
  * gives the same bits more slowly. */

@@ -1282,7 +1282,8 @@ static vcnn_status check_fc_i8(int32_t batch, int32_t in_f, int32_t out_f) {
   if (vcnn_status s = check_fc(batch, in_f, out_f)) return s;
   if (in_f > kMaxI8Depth)
     return fail(VCNN_ERR_UNSUPPORTED, "fc_fwd_i8: sums of %d products do not fit 32 bits (at most %d)", in_f, kMaxI8Depth);
-  if (ceil_div(batch, 128) * ceil_div(out_f, 128) > 0x7fffffffLL)
+  // (a launch has fewer than 2^32 threads: 512 for sixteen outputs of few samples, or for a tile of 256 x 256)
+  if (out_f > 1 << 26 || ceil_div(batch, 256) * ceil_div(out_f, 256) >= 1 << 23)
     return fail(VCNN_ERR_UNSUPPORTED, "fc_fwd_i8: problem too large (batch=%d out_f=%d)", batch, out_f);
   return VCNN_OK;
 }

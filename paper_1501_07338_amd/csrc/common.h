@@ -15,6 +15,12 @@ vcnn_status check_launch(const char* what);
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// Orders a wave's LDS accesses among its lanes: they execute in program order, and the compiler keeps them in it.
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 // Shape of one convolution layer in the paper's matrix terms: the kernel matrix is M x K, the patch
 // matrix K x N, the feature-map matrix M x N (Fig. 2 / Fig. 5: one feature map per row, samples side
 // by side).

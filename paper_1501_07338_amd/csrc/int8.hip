@@ -311,7 +311,7 @@ __device__ __forceinline__ void i8_store(const I8Args& a, const i32x4 (&acc)[TIL
         const int r = h * 16 + (lane & 15), c = i * 4 + (lane >> 4);
         mine[r * WR + (c ^ (r & 7))] = __builtin_bit_cast(uint4, acc[i][j + h]);
       }
-    // (a wave's LDS accesses keep their order)
+    wave_sync();
     auto turn = [&](int n, float scale, bool smooth) {
       const int r = n * ROWS + r0, b = b0j + r;
       const uint4 v = mine[r * WR + (c0 ^ (r & 7))];
@@ -335,6 +335,7 @@ __device__ __forceinline__ void i8_store(const I8Args& a, const i32x4 (&acc)[TIL
 #pragma unroll
       for (int n = 0; n < TURNS; ++n) turn(n, xs[n], false);
     }
+    wave_sync();
   }
 }
 

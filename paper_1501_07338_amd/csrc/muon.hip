@@ -355,7 +355,9 @@ struct SlabTile {
 #pragma unroll
     for (int h = 0; h < TA / 4; ++h) {
       spread(acc, 4 * h, v64);
+      wave_sync();
       part(v64, (ra / 4 + h) * 64, (wave / WM) * 64, 0, 8);
+      wave_sync();
     }
   }
 };
@@ -612,6 +614,7 @@ __device__ __forceinline__ void put_applied(const MuonBatch& b, const MuonTensor
     }
   }
   if (f1 - f0 < 8) __syncthreads();  // (a part of several waves)
+  else wave_sync();
   if (inside) put_next<LAST>(b, t, v64, i0, j0, f0, f1);
 }
 

@@ -76,12 +76,6 @@ __device__ __forceinline__ void dft16(cx<T> (&v)[16]) {
   for (int i = 0; i < 16; ++i) v[i] = t[i];
 }
 
-// Orders a wave's LDS accesses among its lanes (they execute in program order).
-__device__ __forceinline__ void wave_sync() {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-}
-
 // A value from another lane of the same 16: one instruction of the vector units, where a general shuffle goes through LDS.
 template <int CTRL>
 __device__ __forceinline__ uint32_t moved(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true); }

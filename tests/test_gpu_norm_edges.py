@@ -1,9 +1,10 @@
 """The norm where its sums are delicate: squares below the float range, and rows of millions of like values, whose
-roundings do not cancel.
+roundings do not cancel; and with so many rows that a block takes several, one after another.
 
 Tolerances are those of test_gpu_norm, but for long rows: there a group of at most 8 elements is added in float and groups
 in double, so that the roundings of a sum, LONG, do not grow with the row."""
 import pytest
+import test_gpu_norm as plain
 import torch
 
 from paper_1501_07338_amd import vcnn
@@ -82,3 +83,56 @@ def test_gain_gradient_of_more_columns_than_a_grid_is_wide():
         part = slice(a, a + (1 << 24))
         terms = dy[:, part].double() * h[:, part].double() * rstd.double()[:, None]
         assert bool(((dg.t[part].double() - terms.sum(0)).abs() <= terms.abs().sum(0) * 4 * U).all())
+
+
+# More rows than blocks (or waves with a row each) are launched, one to three and six groups a thread; six and eight groups of
+# floats in a few rows.
+MANY_ROWS = [(6500, 200), (6500, 1000), (4500, 1030), (2100, 2049), (1700, 5120), (1100, 9000), (1030, 12288)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [vcnn.F32, vcnn.BF16])
+@pytest.mark.parametrize("rows,cols", MANY_ROWS + [(3, 9000), (3, 12288), (3, 16383)])
+def test_many_rows_a_block(rows, cols, dtype):
+    plain.test_forward(rows, cols, dtype, True, 0)
+    plain.test_forward(rows, cols, dtype, False, 1)
+    plain.test_eight_bits(rows, cols, dtype, 1)
+    plain.test_backward(rows, cols, dtype, True)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [vcnn.F32, vcnn.BF16])
+@pytest.mark.parametrize("rows,cols", [(6500, 200), (2100, 2049), (1700, 5120)])
+def test_many_rows_a_block_in_place(rows, cols, dtype):
+    """The next row is on its way while a block's row is written: both in one tensor."""
+    x, r, gain = tensor(91, rows, cols, dtype), tensor(92, rows, cols, dtype), dev(gain_of(93, cols))
+    xd, rd = dev(x), dev(r)
+    h, y, s = torch.empty_like(xd), torch.empty_like(xd), torch.empty(rows, device=DEV)
+    vcnn.rmsnorm_fwd(dtype, rows, cols, plain.EPS, xd, rd, gain, h, y, s)
+    assert torch.equal(h.cpu(), (x.float() + r.float()).to(x.dtype))
+    q, q8 = (torch.empty(rows, cols, dtype=torch.int8, device=DEV) for _ in range(2))
+    s8 = torch.empty(rows, device=DEV)
+    vcnn.rmsnorm_fwd_i8(dtype, rows, cols, plain.EPS, xd, rd, gain, torch.empty_like(xd), q, s8)
+    for which in ("h is x", "h is residual", "y is x"):
+        a, b = xd.clone(), rd.clone()
+        ho = {"h is x": a, "h is residual": b}.get(which, torch.empty_like(a))
+        yo = a if which == "y is x" else torch.empty_like(a)
+        vcnn.rmsnorm_fwd(dtype, rows, cols, plain.EPS, a, b, gain, ho, yo, None)
+        assert torch.equal(ho, h) and torch.equal(yo, y), which
+        if which != "y is x":
+            a, b = xd.clone(), rd.clone()
+            ho = a if which == "h is x" else b
+            vcnn.rmsnorm_fwd_i8(dtype, rows, cols, plain.EPS, a, b, gain, ho, q8, s8)
+            assert torch.equal(ho, h) and torch.equal(q8, q), which
+    a = xd.clone()
+    vcnn.rmsnorm_fwd(dtype, rows, cols, plain.EPS, a, None, gain, None, a, None)
+    y0 = torch.empty_like(a)
+    vcnn.rmsnorm_fwd(dtype, rows, cols, plain.EPS, xd, None, gain, None, y0, None)
+    assert torch.equal(a, y0)
+    dy, up = dev(tensor(94, rows, cols, dtype)), dev(tensor(95, rows, cols, dtype))
+    dh = torch.empty_like(dy)
+    vcnn.rmsnorm_bwd(dtype, rows, cols, h, gain, s, dy, up, dh, None)
+    for which in ("dy", "above"):
+        a, b = dy.clone(), up.clone()
+        vcnn.rmsnorm_bwd(dtype, rows, cols, h, gain, s, a, b, a if which == "dy" else b, None)
+        assert torch.equal(a if which == "dy" else b, dh), which

@@ -291,8 +291,9 @@ vcnn_status vcnn_fc_fwd_i8(int32_t dtype, int32_t batch, int32_t in_f, int32_t o
 /* The orthogonal part of a [rows][cols] float matrix by Newton-Schulz products: with X = g / |g| (Frobenius norm), `steps`
  * times  A = X X^T,  X <- a X + (b A + c A^2) X,  (a, b, c) = (3.4445, -4.7750, 2.0315)  (a tall matrix transposed).  The
  * singular vectors stay, and the singular values, wherever they were between 0.01 and 1 of the norm, come to lie between
- * 0.68 and 1.21 in five steps.  The products keep float accuracy.  A matrix of zeros gives zeros, one with an infinity or
- * NaN gives NaN throughout.  out may be g itself.  steps is 1 to 32; workspace: vcnn_orthogonalize_workspace_bytes. */
+ * 0.68 and 1.21 in five steps.  The products keep float accuracy, of every row and every column by itself, however small it
+ * is beside the others (down to some 10^-33 of the norm, where floats end).  A matrix of zeros gives zeros, one with an infinity
+ * or NaN gives NaN throughout.  out may be g itself.  steps is 1 to 32; workspace: vcnn_orthogonalize_workspace_bytes. */
 vcnn_status vcnn_orthogonalize_workspace_bytes(int32_t rows, int32_t cols, size_t* bytes);
 vcnn_status vcnn_orthogonalize(int32_t rows, int32_t cols, int32_t steps, const float* g, float* out, void* workspace,
                                size_t workspace_bytes, void* stream);
@@ -303,7 +304,7 @@ vcnn_status vcnn_orthogonalize(int32_t rows, int32_t cols, int32_t steps, const 
  * divided follows from all of them, so the last bits of one may differ with the others beside it (not from run to run).  rows, cols, w, dw, m and w_bf16
  * are HOST arrays of length `tensors` holding sizes and DEVICE pointers; they are read before the call returns.  w_bf16 may be
  * NULL; a non-NULL w_bf16[t] receives the updated tensor rounded to bfloat16.  No two tensors may overlap.  lr, momentum and
- * weight_decay must be finite, steps 1 to 32.  workspace: vcnn_muon_workspace_bytes, three to five times the bytes of the
+ * weight_decay must be finite, steps 1 to 32.  workspace: vcnn_muon_workspace_bytes, four to some six times the bytes of the
  * (largest sixteen in a row) matrices, their sides rounded up to multiples of 128, and 4 MiB. */
 vcnn_status vcnn_muon_workspace_bytes(int32_t tensors, const int32_t* rows, const int32_t* cols, size_t* bytes);
 vcnn_status vcnn_muon_update_multi(int32_t tensors, const int32_t* rows, const int32_t* cols, float* const* w,

@@ -507,8 +507,9 @@ struct MuonTensor {
   float* out;          // given: the orthogonalised matrix, in place of an update of w
   float factor;        // of the learning rate
   int rows, cols;
-  // set by the launch: smaller and larger side, 128-tiles along them, this matrix' part of the workspace
-  int tall, small, large, mt, nt, norm_blocks;
+  // set by the launch: smaller and larger side, 128-tiles and 64 x 64 parts along them, groups of parts, this matrix' part of the
+  // workspace
+  int tall, small, large, mt, nt, pm, pn, gm, gn;
   int parts, share0;   // blocks that share a sum; the first one's share
   uint4* work;
 };

@@ -10,25 +10,38 @@
 //
 // Products.  p multiplies small singular values, and with them the rounding errors beside them, by up to 3.44^steps, so the
 // products are kept to float accuracy: every operand v is two f16 terms, hi + lo of v times a power of two, and a product is
-// the three products hi hi + hi lo + lo hi on the half-precision matrix cores, in one float accumulator.  The entries of X, A
-// and B are bounded by their spectral norms (1.203, 1.45, 2.81), so the power is 2^14 for all of them: the terms hold 23
-// bits of an entry down to 2^-16, and 2^-39 below; what is left out, lo lo, is 2^-22 of a product at most.  (With a I in B
-// the sums of B X would carry a X from their beginning and be rounded at its size throughout: three times the error after
-// one step.)  All three live in fragment order only, frag[16-row tile][step of 32][lane][8]: word `lane` holds row lane % 16 and
-// elements 8 (lane / 16) + 0..7 of the step, what the lane feeds to one v_mfma_f32_16x16x32_f16 (1.9 PFLOP/s on this card with
-// operands in registers; the 32 x 32 x 16 form, by the power it draws, 1.6); X in
-// two of them, by rows (the contraction of X X^T runs along n) and by columns (that of B X along m): the tile that a block
-// has finished goes through LDS and leaves in both.
+// the three products hi hi + hi lo + lo hi on the half-precision matrix cores, in one float accumulator; what is left out, lo lo,
+// is 2^-22 of a product at most.  (With a I in B the sums of B X would carry a X from their beginning and be rounded at its
+// size throughout: three times the error after one step.)
+// The terms are of X by rows (the contraction of X X^T runs along n), X by columns (that of B X along m), A and B, in fragment
+// order, frag[16-row tile][step of 32][lane][8]: word `lane` holds row lane % 16 and elements 8 (lane / 16) + 0..7 of the step,
+// what the lane feeds to one v_mfma_f32_16x16x32_f16 (1.9 PFLOP/s on this card with operands in registers; the 32 x 32 x 16
+// form, by the power it draws, 1.6); X itself stays in floats beside them, for a X.  The tile that a block has finished goes
+// through LDS and leaves in all of them.
+//
+// The powers of two.  Float products keep a row, or a column, that is far smaller than the others to its own accuracy: a X and B X
+// scale row by row and column by column (the gradients of maps that are seldom active are such rows).  Under one power for all,
+// terms lose bits of what lies below 2^-16 of the norm, down to nothing.  So row i of X has a power d_i of its own, and
+// column j a power e_j:
+//     X by rows  d_i X_ij,    A  d_i A_ij,    B  d_i B_ij,    X by columns  X_ij e_j
+// A sum of products of two rows then carries d_i d_k, of B and a column d_i e_j, and the columns k of A and B, whose contribution
+// to row i is in proportion to |X_k|, need no power.  d_i |X_i| is kept below 2^14, which keeps rows of A below 1.21 and of B
+// below 2.82 of that (|x| <= |X_i| times the largest of s and of |b s + c s^3|), within f16.  A step multiplies the norm of a row or
+// column by 0.63 (the least of a + b s^2 + c s^4) to 3.4445, so d follows from the diagonal of A, d_i^2 |X_i|^2, one step ahead; e
+// from the largest entry of the column, which the blocks of a step collect by a maximum in memory (of integers, the same in any
+// order) and which bounds the norm to sqrt(m) of itself: the terms of what is below 2^-10 of it (m = 4096) are off by up to 2^-33
+// of it.  d of the first X is found like that too.  Beside one power for all and no X in floats this costs 2 to 6 % (4096 x 4096
+// 4.04 ms, not 3.94; 1024 x 4096 393 us, not 378; 64 x 800 82, not 79), most of it for writing X once more.
 //
 // Tiles.  256 x 256 and 128 x 128 from slabs in LDS; where there are too few of those for the chip, 64 x 64 with the
 // contraction divided over the block's eight waves, which read their fragments straight from the caches.
 //
 // All matrices of an update go through each phase in one launch: two at first, then a step in two (all matrices of at most 64
-// rows), three, or four (long sums over few tiles, shared by blocks).  4096 x 4096 and 8192 x 2048 together take 5.34 ms, five
-// steps: 1.08 PFLOP/s of f16 products (B X of both 1.23, X X^T 1.04, A^2 0.92, whose tiles come in 1.3 rounds of what the chip
+// rows), three, or four (long sums over few tiles, shared by blocks).  4096 x 4096 and 8192 x 2048 together take 5.53 ms, five
+// steps: 1.05 PFLOP/s of f16 products (B X of both 1.15, X X^T 1.03, A^2 0.91, whose tiles come in 1.3 rounds of what the chip
 // holds), a plain f16 product of 8192^3 1.32.  The products draw so much power that the clock falls to 1.9 GHz; the
-// matrix cores are then busy 57 to 61 % of the time.  1024 x 4096 takes 0.38 ms, bound by the rate at which a CU reads its
-// cache (X X^T) and by the latency of 32 steps (B X); 64 x 800 76 us and 500 x 800 beside three smaller ones 166, by that of
+// matrix cores are then busy 57 to 61 % of the time.  1024 x 4096 takes 0.40 ms, bound by the rate at which a CU reads its
+// cache (X X^T) and by the latency of 32 steps (B X); 64 x 800 79 us and 500 x 800 beside three smaller ones 170, by that of
 // the launches.
 #include <algorithm>
 
@@ -44,7 +57,8 @@ static constexpr int kNormBlocks = 1024;  // of a matrix, at most
 static constexpr int kJoinBlocks = 256;  // of a phase whose sums are shared by several blocks
 static constexpr int kSharedSteps = 64;  // of the longest, from which on sums are shared
 static constexpr int kPad = 128;         // sides in the workspace are multiples of it
-static constexpr float kScale = 16384.f, kUnscale = 1.f / kScale;  // 2^14 * 2.81 < 65504
+static constexpr int kRowTop = 14, kColTop = 15;  // d_i |X_i| < 2^14 (2.82 * 2^14 < 65504), e_j X_ij < 2^15
+static constexpr float kGrowth = 3.5f, kMost = 1.25f;  // of a row's norm in a step, and of any row: a little above the bounds
 static constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
 static constexpr int kTileWords = kPad * kPad / 8;  // 16-byte words of a 128 x 128 tile of one term
 
@@ -56,7 +70,8 @@ struct MuonBatch {
   int tensors;
   float momentum, keep, lr;  // keep = 1 - lr * weight decay
   int nesterov;
-  int turn;                  // which of the two copies of X by columns is read
+  int turn;                  // which of the two copies of X by columns, and of the powers, is read
+  int third;                 // which of the three arrays of columns' largest entries is
   int small;                 // all matrices have at most 64 rows (as X)
   float* shares;             // [kJoinBlocks][64 * 64]: sums of blocks that share a tile
 };
@@ -69,13 +84,36 @@ __device__ __forceinline__ uint4* x_cols(const MuonTensor& t, int turn) { return
 __device__ __forceinline__ uint4* mat_a(const MuonTensor& t) { return t.work + 6 * x_term(t); }
 __device__ __forceinline__ uint4* mat_b(const MuonTensor& t) { return mat_a(t) + 2 * a_term(t); }
 __device__ __forceinline__ double* norms(const MuonTensor& t) { return reinterpret_cast<double*>(mat_b(t) + 2 * a_term(t)); }
-// X of at most 64 rows as floats, 64 x 64 parts as in LDS below (muon_small_kernel).
-__device__ __forceinline__ float4* x_floats(const MuonTensor& t, int part) {
-  return reinterpret_cast<float4*>(mat_b(t) + 2 * a_term(t) + kNormBlocks * 8 / 16) + (int64_t)part * 1024;
+// X as floats, 64 x 64 parts as in LDS below: the one at (i0, j0).
+__device__ __forceinline__ float4* x_floats(const MuonTensor& t, int i0, int j0) {
+  return reinterpret_cast<float4*>(mat_b(t) + 2 * a_term(t) + kNormBlocks * 8 / 16) + ((int64_t)(i0 / 64) * t.pn + j0 / 64) * 1024;
 }
+// Per row: 1 / d_i (two turns).  Per column: 1 / e_j (two turns), the bits of its largest magnitude (three).  And the largest
+// magnitudes of U that the blocks of muon_moment_kernel saw, [gn] of a row and [gm] of a column.
+__host__ __device__ __forceinline__ int64_t row_pitch(const MuonTensor& t) { return (int64_t)t.mt * kPad; }
+__host__ __device__ __forceinline__ int64_t col_pitch(const MuonTensor& t) { return (int64_t)t.nt * kPad; }
+__device__ __forceinline__ float* inv_d(const MuonTensor& t, int turn) {
+  return reinterpret_cast<float*>(x_floats(t, t.pm * 64, 0)) + turn * row_pitch(t);
+}
+__device__ __forceinline__ float* inv_e(const MuonTensor& t, int turn) { return inv_d(t, 2) + turn * col_pitch(t); }
+__device__ __forceinline__ uint32_t* col_most(const MuonTensor& t, int third) {
+  return reinterpret_cast<uint32_t*>(inv_e(t, 2 + third));
+}
+__device__ __forceinline__ uint32_t* row_seen(const MuonTensor& t, int g) { return col_most(t, 3) + g * row_pitch(t); }
+__device__ __forceinline__ uint32_t* col_seen(const MuonTensor& t, int g) { return row_seen(t, t.gn) + g * col_pitch(t); }
 static inline int64_t work_words(const MuonTensor& t) {
-  return 6 * x_term(t) + 4 * a_term(t) + kNormBlocks * 8 / 16 + (t.small <= 64 ? ceil_div(t.large, 64) * 1024 : 0);
+  return 6 * x_term(t) + 4 * a_term(t) + kNormBlocks * 8 / 16 + (int64_t)t.pm * t.pn * 1024 +
+         ((2 + t.gn) * row_pitch(t) + (5 + t.gm) * col_pitch(t)) / 4;
 }
+
+// The power of two that takes what is at most `bound` below 2^top, up to 2^126, whose reciprocal is the smallest normal float.
+// (Any would do for zero.)
+__device__ __forceinline__ float power_for(float bound, int top) {
+  const int exponent = __float_as_int(bound) >> 23 & 255;  // bound < 2^(exponent - 126)
+  return __int_as_float((min(top + 126 - exponent, 126) + 127) << 23);
+}
+__device__ __forceinline__ float inverse_power(float p) { return __int_as_float(0x7f000000 - __float_as_int(p)); }
+__device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }  // (a NaN is the largest)
 
 __device__ __forceinline__ int tensor_of(const MuonBatch& b) {
   int t = 0;
@@ -88,44 +126,90 @@ __device__ __forceinline__ float direction(const MuonBatch& b, float g, float m)
   return b.nesterov ? fmaf(b.momentum, m, g) : m;
 }
 
-// ---- momentum, sum of squares -----------------------------------------------------------------------------------------
-// In double: the squares of floats and their sums leave no range and lose nothing that matters.
+// ---- momentum, sum of squares, largest magnitudes ------------------------------------------------------------------------
+// What a block of 256 threads sees of the 64 x 64 part at (i0, j0) of X in the matrix as stored: thread (wave, lane) has column
+// `lane` of rows wave * 16 + 0..15, which of a tall matrix are X's columns.
+struct Part {
+  int64_t at0;
+  int pitch, rows_left, cols_left;  // of the stored matrix
+  __device__ __forceinline__ Part(const MuonTensor& t, int i0, int j0)
+      : at0(t.tall ? (int64_t)j0 * t.small + i0 : (int64_t)i0 * t.large + j0), pitch(t.tall ? t.small : t.large),
+        rows_left(t.tall ? t.large - j0 : t.small - i0), cols_left(t.tall ? t.small - i0 : t.large - j0) {}
+  __device__ __forceinline__ bool there(int r) const {
+    return (int)(threadIdx.x >> 6) * 16 + r < rows_left && (int)(threadIdx.x & 63) < cols_left;
+  }
+  // (behind the end: the last one's, so that loads wait for no condition)
+  __device__ __forceinline__ int64_t at(int r) const {
+    return at0 + (int64_t)min((int)(threadIdx.x >> 6) * 16 + r, rows_left - 1) * pitch + min((int)(threadIdx.x & 63), cols_left - 1);
+  }
+};
+
+// A block takes one of gm x gn groups of parts.  Sums in double: the squares of floats and their sums leave no range and lose
+// nothing that matters.
 __global__ __launch_bounds__(kThreads) void muon_moment_kernel(MuonBatch b) {
+  __shared__ uint32_t over_rows[2][kThreads / 64][64], over_cols[2][64];  // parts take turns: one barrier each
+  __shared__ double waves[kThreads / 64];
   const int at_tensor = tensor_of(b);
   const MuonTensor& t = b.t[at_tensor];
-  const int block = blockIdx.x - b.first[at_tensor];
-  const int64_t count = (int64_t)t.rows * t.cols;
+  const int block = blockIdx.x - b.first[at_tensor], gi = block / t.gn, gj = block % t.gn;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  // (at most 2^18 parts a side, 256 groups)
+  const int p0 = (unsigned)(t.pm * gi) / t.gm, p1 = (unsigned)(t.pm * (gi + 1)) / t.gm;
+  const int q0 = (unsigned)(t.pn * gj) / t.gn, q1 = (unsigned)(t.pn * (gj + 1)) / t.gn;
   double sum = 0.;
-  const auto one = [&](float g, float m, float* out) {
-    if (t.m) *out = fmaf(b.momentum, m, g), g = direction(b, g, *out);
-    sum += (double)g * g;
-  };
-  const int64_t stride = (int64_t)t.norm_blocks * kThreads * 4;
-#pragma unroll 2
-  for (int64_t i = ((int64_t)block * kThreads + threadIdx.x) * 4; i + 4 <= count; i += stride) {
-    const float4 g = ld4_dword_aligned(t.g + i), m = t.m ? ld4_dword_aligned(t.m + i) : g;
-    float4_dword_aligned u;
-    one(g.x, m.x, &u.x), one(g.y, m.y, &u.y), one(g.z, m.z, &u.z), one(g.w, m.w, &u.w);
-    if (t.m) *reinterpret_cast<float4_dword_aligned*>(t.m + i) = u;
-  }
-  if (block == 0 && threadIdx.x < count % 4) {
-    const int64_t i = count - count % 4 + threadIdx.x;
-    float u;
-    one(t.g[i], t.m ? t.m[i] : 0.f, &u);
-    if (t.m) t.m[i] = u;
-  }
-  __shared__ double waves[kThreads / 64];
+  int turn = 0;
+  for (int p = p0; p < p1; ++p)
+    for (int q = q0; q < q1; ++q, turn ^= 1) {
+      const Part part(t, p * 64, q * 64);
+      float g[16], m[16];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) g[r] = t.g[part.at(r)];
+      if (t.m) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) m[r] = t.m[part.at(r)];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          m[r] = fmaf(b.momentum, m[r], g[r]), g[r] = direction(b, g[r], m[r]);
+          if (part.there(r)) t.m[part.at(r)] = m[r];
+        }
+      }
+      uint32_t v[16], most = 0;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        if (!part.there(r)) g[r] = 0.f;
+        sum += (double)g[r] * g[r];
+        v[r] = magnitude(g[r]), most = max(most, v[r]);
+      }
+      // over the lanes: each step keeps the half of the rows that a bit of the lane chooses; lane 4 r has row r in the end
+#pragma unroll
+      for (int n = 8, d = 32; n > 0; n >>= 1, d >>= 1) {
+        const bool up = lane & d;
+#pragma unroll
+        for (int i = 0; i < n; ++i) v[i] = max(up ? v[i + n] : v[i], (uint32_t)__shfl_xor((int)(up ? v[i] : v[i + n]), d));
+      }
+      v[0] = max(v[0], (uint32_t)__shfl_xor((int)v[0], 2));
+      v[0] = max(v[0], (uint32_t)__shfl_xor((int)v[0], 1));
+      over_rows[turn][wave][lane] = most;
+      if (lane % 4 == 0) over_cols[turn][wave * 16 + lane / 4] = v[0];
+      __syncthreads();
+      if (threadIdx.x < 128) {  // of a column as stored, of a row as stored: of X's row or column; this thread's in every part
+        const auto& waves_most = over_rows[turn];
+        most = threadIdx.x < 64 ? max(max(waves_most[0][lane], waves_most[1][lane]), max(waves_most[2][lane], waves_most[3][lane]))
+                                : over_cols[turn][lane];
+        const bool row = (threadIdx.x < 64) == (bool)t.tall;
+        uint32_t* const seen = row ? row_seen(t, gj) + p * 64 + lane : col_seen(t, gi) + q * 64 + lane;
+        *seen = (row ? q > q0 : p > p0) ? max(*seen, most) : most;
+      }
+    }
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
-  if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = sum;
+  if (lane == 0) waves[wave] = sum;
   __syncthreads();
   if (threadIdx.x == 0) norms(t)[block] = waves[0] + waves[1] + waves[2] + waves[3];
 }
-// 1 / |U|; zero for a matrix of zeros, NaN where an element is not finite.  Called by whole blocks;
-// `waves`: four doubles of LDS, free again afterwards.
-__device__ __forceinline__ double inverse_norm(const MuonTensor& t, double* waves) {
-  double sum = 0.;
-  for (int i = threadIdx.x; i < t.norm_blocks; i += kThreads) sum += norms(t)[i];
+// 1 / |U| from a thread's share of the sum of squares; zero for a matrix of zeros, NaN where an element is not finite.  Called
+// by whole blocks; `waves`: four doubles of LDS, free again afterwards.
+__device__ __forceinline__ double inverse_norm(double sum, double* waves) {
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
   if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = sum;
@@ -143,25 +227,24 @@ __device__ __forceinline__ double inverse_norm(const MuonTensor& t, double* wave
 __device__ __forceinline__ int shift_of(int i) { return (i & 7) << 2 ^ (i & 4) << 3 ^ (i & 8) << 1 ^ (i & 16) << 1; }
 __device__ __forceinline__ int at64(int i, int j) { return i * 64 + (j ^ shift_of(i)); }
 
-// Eight values (times 2^14) as two terms.
+// Eight values as two terms.
 __device__ __forceinline__ void split8(const float (&v)[8], uint4* hi, uint4* lo) {
   f16x8 h, l;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const float t = v[e] * kScale;
-    h[e] = (_Float16)t;
-    l[e] = (_Float16)(t - (float)h[e]);
+    h[e] = (_Float16)v[e];
+    l[e] = (_Float16)(v[e] - (float)h[e]);
   }
   *hi = __builtin_bit_cast(uint4, h), *lo = __builtin_bit_cast(uint4, l);
 }
 __device__ __forceinline__ void join8(const uint4* src, int64_t term, int64_t word, float (&v)[8]) {
   const f16x8 hi = __builtin_bit_cast(f16x8, src[word]), lo = __builtin_bit_cast(f16x8, src[term + word]);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = ((float)hi[e] + (float)lo[e]) * kUnscale;
+  for (int e = 0; e < 8; ++e) v[e] = (float)hi[e] + (float)lo[e];
 }
 
 // Fragment f (of four row tiles by two steps) of the 64 x 64 values: rows i and contraction j, or (COLS) rows j and
-// contraction i.  word0: the word of fragment 0; change(v, word): eight values and their place.
+// contraction i.  word0: the word of fragment 0; change(v, word, row, k): eight values, their place, row and first contraction.
 template <bool COLS, typename F>
 __device__ __forceinline__ void put_fragment(const float* v64, uint4* dst, int64_t term, int64_t word0, int steps, int f,
                                              F change) {
@@ -179,51 +262,98 @@ __device__ __forceinline__ void put_fragment(const float* v64, uint4* dst, int64
     }
   }
   const int64_t word = word0 + ((int64_t)(f >> 1) * steps + (f & 1)) * 64 + lane;
-  change(v, word);
+  change(v, word, row, k);
   uint4 hi, lo;
   split8(v, &hi, &lo);
   dst[word] = hi, dst[term + word] = lo;
 }
 // Word (without the lane) of the fragment at row i0, contraction j0.
 __device__ __forceinline__ int64_t word_of(int i0, int j0, int steps) { return ((int64_t)(i0 / 16) * steps + j0 / 32) * 64; }
-struct AsIs {
-  __device__ __forceinline__ void operator()(float (&)[8], int64_t) const {}
-};
+// Eight values times eight of an array, or times one.
+__device__ __forceinline__ void times8(float (&v)[8], const float* by) {  // (16-byte aligned)
+#pragma unroll
+  for (int e = 0; e < 8; e += 4) {
+    const float4 p = *reinterpret_cast<const float4*>(by + e);
+    v[e] *= p.x, v[e + 1] *= p.y, v[e + 2] *= p.z, v[e + 3] *= p.w;
+  }
+}
+__device__ __forceinline__ void times8(float (&v)[8], float by) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] *= by;
+}
+// Place p of the 1024 of four values: row i, columns j .. j + 3.
+__device__ __forceinline__ int row_at(int p) { return p >> 4; }
+__device__ __forceinline__ int col_at(int p) { return (p & 15) << 2 ^ shift_of(p >> 4); }
 
 // ---- X = U / |U| in both orders ---------------------------------------------------------------------------------------
 // A block makes one 64 x 64 part.
 __global__ __launch_bounds__(kThreads) void muon_begin_kernel(MuonBatch b) {
   __shared__ __attribute__((aligned(16))) float v64[64 * 64];
+  __shared__ uint32_t seen[2][kThreads / 64][64];  // of rows, of columns
+  __shared__ float power[2][64];                   // the same
   const int at_tensor = tensor_of(b);
   const MuonTensor& t = b.t[at_tensor];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int part = blockIdx.x - b.first[at_tensor], parts_m = (t.small + 63) / 64, parts_n = (t.large + 63) / 64;
+  const int at_part = blockIdx.x - b.first[at_tensor];
   // neighbouring parts lie along the rows as stored
-  const int i0 = (t.tall ? part % parts_m : part / parts_n) * 64, j0 = (t.tall ? part / parts_m : part % parts_n) * 64;
-  const int64_t at0 = t.tall ? (int64_t)j0 * t.small + i0 : (int64_t)i0 * t.large + j0;
-  const int pitch = t.tall ? t.small : t.large;
-  const int rows_left = t.tall ? t.large - j0 : t.small - i0, cols_left = t.tall ? t.small - i0 : t.large - j0;
+  const int i0 = (t.tall ? at_part % t.pm : at_part / t.pn) * 64, j0 = (t.tall ? at_part / t.pm : at_part % t.pn) * 64;
+  const Part part(t, i0, j0);
   float x[16];  // of sixteen rows of the matrix as stored: of X, or of a tall matrix its columns
 #pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    const bool there = wave * 16 + r < rows_left && lane < cols_left;
-    const int64_t at = at0 + (int64_t)(wave * 16 + r) * pitch + lane;
-    x[r] = !there ? 0.f : t.m ? direction(b, t.g[at], t.m[at]) : t.g[at];
-  }
-  const double inverse = inverse_norm(t, reinterpret_cast<double*>(v64));
+  for (int r = 0; r < 16; ++r) x[r] = t.g[part.at(r)];
+  if (t.m) {
+    float m[16];
 #pragma unroll
-  for (int r = 0; r < 16; ++r) v64[t.tall ? at64(lane, wave * 16 + r) : at64(wave * 16 + r, lane)] = (float)(x[r] * inverse);
+    for (int r = 0; r < 16; ++r) m[r] = t.m[part.at(r)];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) x[r] = direction(b, x[r], m[r]);
+  }
+  double sum = 0.;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < t.gm * t.gn; i += kThreads) sum += norms(t)[i];
+  // of row `lane` and of column `lane`, a wave every fourth group
+  const auto largest = [&](const uint32_t* from, int64_t pitch, int groups) {
+    uint32_t most = 0;
+#pragma unroll 8
+    for (int g = wave; g < groups; g += kThreads / 64) most = max(most, from[g * pitch + lane]);
+    return most;
+  };
+  const uint32_t of_row = largest(row_seen(t, 0) + i0, row_pitch(t), t.gn);
+  const uint32_t of_col = largest(col_seen(t, 0) + j0, col_pitch(t), t.gm);
+  seen[0][wave][lane] = of_row, seen[1][wave][lane] = of_col;
+  const double inverse = inverse_norm(sum, reinterpret_cast<double*>(v64));
+#pragma unroll
+  for (int r = 0; r < 16; ++r)
+    v64[t.tall ? at64(lane, wave * 16 + r) : at64(wave * 16 + r, lane)] = part.there(r) ? (float)(x[r] * inverse) : 0.f;
+  if (wave < 2) {
+    const uint32_t most = max(max(seen[wave][0][lane], seen[wave][1][lane]), max(seen[wave][2][lane], seen[wave][3][lane]));
+    const float bound = (float)(__uint_as_float(most) * inverse);
+    if (wave == 0) {
+      const float d = power_for(fminf(bound * sqrtf((float)t.large), 1.f), kRowTop);
+      power[0][lane] = d;
+      if (j0 == 0) inv_d(t, b.turn)[i0 + lane] = inverse_power(d);
+    } else {
+      const float e = power_for(bound, kColTop);
+      power[1][lane] = e;
+      if (i0 == 0 && !b.small) {
+        inv_e(t, b.turn)[j0 + lane] = inverse_power(e);
+        col_most(t, b.third)[j0 + lane] = magnitude(bound);
+        col_most(t, (b.third + 1) % 3)[j0 + lane] = 0;
+      }
+    }
+  }
   __syncthreads();
-  if (b.small) {
+  float4* const kept = x_floats(t, i0, j0) + threadIdx.x;
 #pragma unroll
-    for (int n = 0; n < 4; ++n)
-      x_floats(t, j0 / 64)[n * kThreads + threadIdx.x] = reinterpret_cast<const float4*>(v64)[n * kThreads + threadIdx.x];
-  }
+  for (int n = 0; n < 4; ++n) kept[n * kThreads] = reinterpret_cast<const float4*>(v64)[n * kThreads + threadIdx.x];
   const int by_rows = t.nt * (kPad / 32), by_cols = t.mt * (kPad / 32);
 #pragma unroll
   for (int f = 2 * wave; f < 2 * wave + 2; ++f) {
-    put_fragment<false>(v64, x_rows(t), x_term(t), word_of(i0, j0, by_rows), by_rows, f, AsIs());
-    if (!b.small) put_fragment<true>(v64, x_cols(t, b.turn), x_term(t), word_of(j0, i0, by_cols), by_cols, f, AsIs());
+    put_fragment<false>(v64, x_rows(t), x_term(t), word_of(i0, j0, by_rows), by_rows, f,
+                        [&](float (&v)[8], int64_t, int row, int) { times8(v, power[0][row]); });
+    if (!b.small)
+      put_fragment<true>(v64, x_cols(t, b.turn), x_term(t), word_of(j0, i0, by_cols), by_cols, f,
+                         [&](float (&v)[8], int64_t, int row, int) { times8(v, power[1][row]); });
   }
 }
 
@@ -242,7 +372,7 @@ struct Operand {
 };
 
 // The accumulators of TA x 4 tiles (register q of lane l: row 4 (l / 16) + q, column l % 16), four by four from row tile
-// `first` on, as values in LDS.
+// `first` on, as values in LDS (still times the powers of both operands' rows).
 template <int TA>
 __device__ __forceinline__ void spread(const f32x4 (&acc)[TA][4], int first, float* v64) {
   const int lane = threadIdx.x & 63;
@@ -252,7 +382,7 @@ __device__ __forceinline__ void spread(const f32x4 (&acc)[TA][4], int first, flo
     for (int j = 0; j < 4; ++j)
 #pragma unroll
       for (int q = 0; q < 4; ++q)
-        v64[at64(i * 16 + (lane >> 4) * 4 + q, j * 16 + (lane & 15))] = acc[first + i][j][q] * (kUnscale * kUnscale);
+        v64[at64(i * 16 + (lane >> 4) * 4 + q, j * 16 + (lane & 15))] = acc[first + i][j][q];
 }
 
 // Tiles of 16 TA WM x 64 WN, a wave 16 TA x 64 of them.  A slab is one step of both operands, both terms; it goes to LDS by
@@ -465,24 +595,36 @@ __device__ __forceinline__ void triangle_of(int item, int n, int* it, int* jt) {
   *it = band + item, *jt = band + j;
 }
 
+// d_i for the X that this step makes, from d_i^2 A_ii and 1 / d_i of this one.
+__device__ __forceinline__ float next_power(float diagonal, float inverse) {
+  return power_for(fminf(sqrtf(diagonal) * inverse * kGrowth, kMost), kRowTop);
+}
+
 // A 64 x 64 part of A (MUON_A: the values themselves) or B (MUON_B: b A + c times the values) at (i0, j0), and at (j0, i0) where
-// that is another place: fragments f0 .. f1.
+// that is another place: fragments f0 .. f1.  The values carry the powers of row and column; that of the contraction goes.
 template <int WHAT>
-__device__ __forceinline__ void put_symmetric(const MuonTensor& t, const float* v64, int i0, int j0, bool both, int f0, int f1) {
-  if (max(i0, j0) >= t.mt * kPad) return;
+__device__ __forceinline__ void put_symmetric(const MuonBatch& b, const MuonTensor& t, const float* v64, int i0, int j0, bool both, int f0, int f1) {
+  if (max(i0, j0) >= t.small) return;
   uint4* const dst = WHAT == MUON_A ? mat_a(t) : mat_b(t);
-  const int steps = t.mt * (kPad / 32);
-  const auto polynomial = [&](float (&v)[8], int64_t word) {
+  const int steps = t.mt * (kPad / 32), lane = threadIdx.x & 63;
+  const float* const inverse = inv_d(t, b.turn);
+  const auto polynomial = [&](float (&v)[8], int64_t word, const float* by) {
+    times8(v, by);
     if (WHAT == MUON_A) return;
     float a8[8];
     join8(mat_a(t), a_term(t), word, a8);
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = fmaf(kC, v[e], kB * a8[e]);
   };
+  if (WHAT == MUON_A && i0 == j0 && f0 == 0)
+    inv_d(t, b.turn ^ 1)[i0 + lane] = inverse_power(next_power(v64[at64(lane, lane)], inverse[i0 + lane]));
 #pragma unroll 2
   for (int f = f0; f < f1; ++f) {
-    put_fragment<false>(v64, dst, a_term(t), word_of(i0, j0, steps), steps, f, polynomial);
-    if (both) put_fragment<true>(v64, dst, a_term(t), word_of(j0, i0, steps), steps, f, polynomial);
+    put_fragment<false>(v64, dst, a_term(t), word_of(i0, j0, steps), steps, f,
+                        [&](float (&v)[8], int64_t word, int, int k) { polynomial(v, word, inverse + j0 + k); });
+    if (both)
+      put_fragment<true>(v64, dst, a_term(t), word_of(j0, i0, steps), steps, f,
+                         [&](float (&v)[8], int64_t word, int, int k) { polynomial(v, word, inverse + i0 + k); });
   }
 }
 
@@ -501,7 +643,7 @@ __global__ __launch_bounds__(TILE::THREADS, 2) void muon_square_kernel(MuonBatch
   Operand y = x;
   y.row_tile = jt * (TILE::BM / 16);
   TILE::run(x, y, (depth + 31) / 32, smem16, [&](const float* v64, int i1, int j1, int f0, int f1) {
-    put_symmetric<WHAT>(t, v64, it * TILE::BM + i1, jt * TILE::BN + j1, it != jt, f0, f1);
+    put_symmetric<WHAT>(b, t, v64, it * TILE::BM + i1, jt * TILE::BN + j1, it != jt, f0, f1);
   });
 }
 
@@ -547,20 +689,39 @@ __global__ __launch_bounds__(FewTile::THREADS) void muon_join_kernel(MuonBatch b
   int it, jt;
   triangle_of(tile, (t.small + 63) / 64, &it, &jt);
   const int wave = threadIdx.x >> 6;
-  put_symmetric<MUON_A>(t, v64, it * 64, jt * 64, it != jt, wave, wave + 1);
+  put_symmetric<MUON_A>(b, t, v64, it * 64, jt * 64, it != jt, wave, wave + 1);
 }
 
 // X' of a 64 x 64 part at (i0, j0) to where the next step finds it; after the last one: the result, or the weights moved by it.
-// Fragments f0 .. f1 are this wave's.  COLS: X is read by columns too.
+// Fragments f0 .. f1 are this wave's.  COLS: X is read by columns too.  d, e: the powers that X' has in the part's row, and column,
+// `lane`.
 template <bool LAST, bool COLS = true>
-__device__ __forceinline__ void put_next(const MuonBatch& b, const MuonTensor& t, const float* v64, int i0, int j0, int f0, int f1) {
+__device__ __forceinline__ void put_next(const MuonBatch& b, const MuonTensor& t, const float* v64, int i0, int j0, int f0, int f1,
+                                         float d, float e) {
   const int lane = threadIdx.x & 63;
   const int steps_n = t.nt * (kPad / 32), steps_m = t.mt * (kPad / 32);
   if constexpr (!LAST) {
+    uint32_t largest = 0;  // of column `lane`, in the rows of the wave's fragments
 #pragma unroll 2
     for (int f = f0; f < f1; ++f) {
-      put_fragment<false>(v64, x_rows(t), x_term(t), word_of(i0, j0, steps_n), steps_n, f, AsIs());
-      if (COLS) put_fragment<true>(v64, x_cols(t, b.turn ^ 1), x_term(t), word_of(j0, i0, steps_m), steps_m, f, AsIs());
+      put_fragment<false>(v64, x_rows(t), x_term(t), word_of(i0, j0, steps_n), steps_n, f,
+                          [&](float (&v)[8], int64_t, int row, int) { times8(v, __shfl(d, row)); });
+      if (COLS)
+        put_fragment<true>(v64, x_cols(t, b.turn ^ 1), x_term(t), word_of(j0, i0, steps_m), steps_m, f,
+                           [&](float (&v)[8], int64_t, int col, int) {  // sixteen columns, four lanes each
+                             uint32_t most = 0;
+#pragma unroll
+                             for (int n = 0; n < 8; ++n) most = max(most, magnitude(v[n]));
+                             most = max(most, (uint32_t)__shfl_xor((int)most, 16));
+                             most = max(most, (uint32_t)__shfl_xor((int)most, 32));
+                             if (lane >> 4 == f >> 1) largest = max(largest, most);
+                             times8(v, __shfl(e, col));
+                           });
+    }
+    if (COLS) {
+      if (lane >> 4 >= f0 >> 1 && lane >> 4 <= (f1 - 1) >> 1)
+        atomicMax(col_most(t, (b.third + 1) % 3) + j0 + lane, largest);
+      if (i0 == 0 && f0 == 0) inv_e(t, b.turn ^ 1)[j0 + lane] = inverse_power(e), col_most(t, (b.third + 2) % 3)[j0 + lane] = 0;
     }
   } else {
     const float step = b.lr * t.factor;
@@ -592,30 +753,36 @@ __device__ __forceinline__ void put_next(const MuonBatch& b, const MuonTensor& t
   }
 }
 
-// X <- a X + B X of such a part, given B X.  Waves that share a part all come here.
+// X <- a X + B X of such a part, given d_i e_j B X.  Waves that share a part all come here.
 template <bool LAST>
 __device__ __forceinline__ void put_applied(const MuonBatch& b, const MuonTensor& t, float* v64, int i0, int j0, int f0, int f1) {
-  const bool inside = i0 < t.mt * kPad && j0 < t.nt * kPad;  // (the same for all waves that share a part)
   const int lane = threadIdx.x & 63;
-  const int steps_n = t.nt * (kPad / 32);
-  const int64_t by_rows = word_of(i0, j0, steps_n);
+  const bool inside = i0 < t.small && j0 < t.large;  // (the same for all waves that share a part)
+  float d = 0.f, e = 0.f;
   if (inside) {
-#pragma unroll 2
-    for (int f = f0; f < f1; ++f) {  // a X, from X by rows (whose place the same lanes write below)
-      const int row = (f >> 1) * 16 + (lane & 15), k = (f & 1) * 32 + (lane >> 4) * 8;
-      float v[8];
-      join8(x_rows(t), x_term(t), by_rows + ((int64_t)(f >> 1) * steps_n + (f & 1)) * 64 + lane, v);
-#pragma unroll
-      for (int e = 0; e < 8; e += 4) {
-        float4* const p = reinterpret_cast<float4*>(v64 + at64(row, k + e));
-        const float4 u = *p;
-        *p = make_float4(fmaf(kA, v[e], u.x), fmaf(kA, v[e + 1], u.y), fmaf(kA, v[e + 2], u.z), fmaf(kA, v[e + 3], u.w));
-      }
+    if (!LAST) {
+      d = inverse_power(inv_d(t, b.turn ^ 1)[i0 + lane]);
+      const float bound = __uint_as_float(col_most(t, b.third)[j0 + lane]) * (kGrowth * sqrtf((float)t.small));
+      e = power_for(fminf(bound, kMost), kColTop);
+    }
+    float4* const x = x_floats(t, i0, j0);
+    const float *const by_row = inv_d(t, b.turn) + i0, *const by_col = inv_e(t, b.turn) + j0;
+#pragma unroll 4
+    for (int n = f0 * 2; n < f1 * 2; ++n) {
+      const int p = n * 64 + lane;
+      const float row = by_row[row_at(p)];
+      const float4 col = *reinterpret_cast<const float4*>(by_col + col_at(p)), v = x[p];
+      float4* const at = reinterpret_cast<float4*>(v64) + p;
+      float4 u = *at;
+      u.x = fmaf(kA, v.x, u.x * row * col.x), u.y = fmaf(kA, v.y, u.y * row * col.y);
+      u.z = fmaf(kA, v.z, u.z * row * col.z), u.w = fmaf(kA, v.w, u.w * row * col.w);
+      *at = u;
+      if (!LAST) x[p] = u;
     }
   }
   if (f1 - f0 < 8) __syncthreads();  // (a part of several waves)
   else wave_sync();
-  if (inside) put_next<LAST>(b, t, v64, i0, j0, f0, f1);
+  if (inside) put_next<LAST>(b, t, v64, i0, j0, f0, f1, d, e);
 }
 
 template <typename TILE, bool LAST>
@@ -646,7 +813,8 @@ __global__ __launch_bounds__(512) void muon_small_kernel(MuonBatch b) {
   const int j0 = (blockIdx.x - b.first[at_tensor]) * 64;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int rt = (wave >> 1) * 16, ct = (wave & 1) * 32, in = lane & 15, k4 = lane >> 4;  // rows, columns of the wave's tiles
-  float4* const kept = x_floats(t, j0 / 64) + threadIdx.x;
+  float4* const kept = x_floats(t, 0, j0) + threadIdx.x;
+  const float* const inverse = inv_d(t, b.turn);
   const float4* const from = reinterpret_cast<const float4*>(b.shares) + (int64_t)t.share0 * 1024 + threadIdx.x;
   const float4 x[2] = {kept[0], kept[512]};
   float4 v[2] = {from[0], from[512]};
@@ -658,11 +826,14 @@ __global__ __launch_bounds__(512) void muon_small_kernel(MuonBatch b) {
       v[h].x += u.x, v[h].y += u.y, v[h].z += u.z, v[h].w += u.w;
     }
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    reinterpret_cast<float4*>(v64)[h * 512 + threadIdx.x] = v[h];
-    reinterpret_cast<float4*>(x64)[h * 512 + threadIdx.x] = x[h];
+  for (int h = 0; h < 2; ++h) {  // d_i A_ij
+    const int p = h * 512 + threadIdx.x;
+    const float4 by = *reinterpret_cast<const float4*>(inverse + col_at(p));
+    reinterpret_cast<float4*>(v64)[p] = make_float4(v[h].x * by.x, v[h].y * by.y, v[h].z * by.z, v[h].w * by.w);
+    reinterpret_cast<float4*>(x64)[p] = x[h];
   }
   __syncthreads();
+  const float diagonal = v64[at64(lane, lane)], by = inverse[lane];
   // v_mfma_f32_16x16x4_f32: lane l holds row l % 16 of one operand, column l % 16 of the other, contraction l / 16
   const auto product = [&](auto column, f32x4 (&acc)[2]) {  // two halves of the sum at once
     f32x4 part[2][2] = {};
@@ -680,15 +851,17 @@ __global__ __launch_bounds__(512) void muon_small_kernel(MuonBatch b) {
     for (int c = 0; c < 2; ++c) acc[c] = part[0][c] + part[1][c];
   };
   f32x4 acc[2];
-  product([&](int k, int j) { return v64[at64(j, k)]; }, acc);
+  product([&](int k, int j) { return v64[at64(j, k)]; }, acc);  // d_i d_j A^2
   __syncthreads();
 #pragma unroll
-  for (int c = 0; c < 2; ++c)
+  for (int c = 0; c < 2; ++c) {
+    const float by_col = inverse[ct + c * 16 + in];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {  // B in A's place: every value is one lane's own
+    for (int q = 0; q < 4; ++q) {  // d_i B in A's place: every value is one lane's own
       float* const at = v64 + at64(rt + 4 * k4 + q, ct + c * 16 + in);
-      *at = fmaf(kC, acc[c][q], kB * *at);
+      *at = fmaf(kC, acc[c][q] * by_col, kB * *at);
     }
+  }
   __syncthreads();
   product([&](int k, int j) { return x64[at64(k, j)]; }, acc);
   __syncthreads();
@@ -697,14 +870,16 @@ __global__ __launch_bounds__(512) void muon_small_kernel(MuonBatch b) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const int at = at64(rt + 4 * k4 + q, ct + c * 16 + in);
-      v64[at] = fmaf(kA, x64[at], acc[c][q]);
+      v64[at] = fmaf(kA, x64[at], acc[c][q] * inverse[rt + 4 * k4 + q]);
     }
   __syncthreads();
   if (!LAST) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) kept[h * 512] = reinterpret_cast<const float4*>(v64)[h * 512 + threadIdx.x];
   }
-  put_next<LAST, false>(b, t, v64, 0, j0, wave, wave + 1);
+  const float d = next_power(diagonal * inverse_power(by), by);
+  if (!LAST && j0 == 0 && wave == 0) inv_d(t, b.turn ^ 1)[lane] = inverse_power(d);
+  put_next<LAST, false>(b, t, v64, 0, j0, wave, wave + 1, d, 0.f);
 }
 
 // ---- launches -----------------------------------------------------------------------------------------------------------
@@ -712,7 +887,10 @@ static void lay_out(MuonTensor* t) {
   t->tall = t->rows > t->cols;
   t->small = std::min(t->rows, t->cols), t->large = std::max(t->rows, t->cols);
   t->mt = (int)ceil_div(t->small, kPad), t->nt = (int)ceil_div(t->large, kPad);
-  t->norm_blocks = (int)std::min<int64_t>(kNormBlocks, ceil_div((int64_t)t->rows * t->cols, 8 * kThreads));
+  t->pm = (int)ceil_div(t->small, 64), t->pn = (int)ceil_div(t->large, 64);
+  // groups of parts that a block of muon_moment_kernel takes: a block of muon_begin_kernel reads what all of a row, and all of a
+  // column, have seen
+  t->gm = std::min(t->pm, 32), t->gn = std::min(t->pn, std::max(32, 256 / t->gm));
 }
 
 // At the start of the workspace: the shares.
@@ -832,11 +1010,11 @@ vcnn_status launch_muon(const MuonTensor* tensors, int count, float lr, float mo
   }
   b.small = 1;  // a step is two launches then (64 x 800: five steps 76 us, with three launches each 107)
   for (int t = 0; t < b.tensors; ++t) b.small = b.small && b.t[t].small <= 64;
-  const auto norm_blocks = [](const MuonTensor& t) { return t.norm_blocks; };
-  const auto parts = [](const MuonTensor& t) { return ceil_div(t.small, 64) * ceil_div(t.large, 64); };
-  if (vcnn_status s = launch_phase("muon moment", muon_moment_kernel, &b, kThreads, 0, st, norm_blocks)) return s;
+  const auto groups = [](const MuonTensor& t) { return t.gm * t.gn; };
+  const auto parts = [](const MuonTensor& t) { return (int64_t)t.pm * t.pn; };
+  if (vcnn_status s = launch_phase("muon moment", muon_moment_kernel, &b, kThreads, 0, st, groups)) return s;
   if (vcnn_status s = launch_phase("muon begin", muon_begin_kernel, &b, kThreads, 0, st, parts)) return s;
-  for (int i = 0; i < steps; ++i, b.turn ^= 1) {
+  for (int i = 0; i < steps; ++i, b.turn ^= 1, b.third = (b.third + 1) % 3) {
     if (b.small) {
       const auto columns = [](const MuonTensor& t) { return ceil_div(t.large, 64); };
       if (vcnn_status s = launch_shares(&b, b.tensors, 8, 16, st)) return s;

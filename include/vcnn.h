@@ -252,7 +252,8 @@ vcnn_status vcnn_sgd_update_multi(int32_t tensors, const size_t* counts, float* 
  * the residual's addition before it:
  *     h = x + residual (rounded to dtype),   rstd[r] = 1 / sqrt(mean_c h[r][c]^2 + eps),   y[r][c] = h[r][c] * rstd[r] * gain[c]
  * x, residual, h, y follow dtype; gain [cols] and rstd [rows] are float; sums are float (double where the squares leave its
- * range, and between the groups of rows of more than 16384 elements).  residual may be NULL: then h is x, and the argument h is not used.  rstd may be NULL; vcnn_rmsnorm_bwd needs it.
+ * range, and between the groups of rows of more than 16384 elements).  residual may be NULL: then h is x, and the argument h is
+ * not used.  rstd may be NULL; vcnn_rmsnorm_bwd needs it.
  * eps must be positive and finite, cols at most 2^30.  h may be x or residual itself (an update of the residual stream in place), y may be x
  * where h is not; nothing else may overlap.  A row with an infinity or NaN gives what the formula gives, in that row alone. */
 vcnn_status vcnn_rmsnorm_fwd(int32_t dtype, int32_t rows, int32_t cols, float eps, const void* x, const void* residual,
@@ -280,8 +281,9 @@ vcnn_status vcnn_quant_rows_i8(int32_t dtype, int32_t rows, int32_t cols, const 
  *     y[b][o] = act(bias[o] + xscale[b] * wscale[o] * sum_i xq[b][i] * wq[o][i])
  * with xq [batch][in_f], wq [out_f][in_f] int8 and a float scale per row of either (vcnn_rmsnorm_fwd_i8, vcnn_quant_rows_i8, or
  * the caller's own); bias is float and may be NULL; y [batch][out_f] follows dtype.  The sums are exact; a scale of NaN gives
- * NaN.  in_f is at most 131071 (sums of 32 bits; VCNN_ERR_UNSUPPORTED), out_f at most 2^26.  Rows may start at any byte; in_f a multiple of 16 and
- * 16-byte aligned operands are faster with more than 64 samples.  workspace: vcnn_fc_i8_workspace_bytes (0 for most
+ * NaN.  in_f is at most 131071 (sums of 32 bits; VCNN_ERR_UNSUPPORTED), out_f at most 2^26.  Rows may start at any byte; in_f a
+ * multiple of 16 and 16-byte aligned operands are faster with more than 32 samples (with at most 2^25 weights 64, with 2^20 128).
+ * workspace: vcnn_fc_i8_workspace_bytes (0 for most
  * layers) divides the sums of layers with few tiles over more of the chip; with less of it, or none (NULL, 0), the call
  * gives the same bits more slowly. */
 vcnn_status vcnn_fc_i8_workspace_bytes(int32_t batch, int32_t in_f, int32_t out_f, size_t* bytes);

@@ -7,12 +7,11 @@
 // Three kernels.  One or two samples: dot products of whole rows (i8_dot_kernel; 4096 -> 16384 in 11.9 us with the call's own,
 // the next kernel 15.1).  Up to 32, or 128 where the layer is small: the weights are read once and nothing of them is reused,
 // so a block owns 16 outputs, its eight waves take every eighth 128 bytes of the rows and feed the matrix cores from global
-// memory, all operands of four such steps in flight at once (i8_rows_kernel; 48 samples 4096 -> 4096 in 12 us, one round of
-// loads).  More: tiles of 256 x 256 or 128 x 128 from slabs of 64 bytes of both operands in LDS (i8_tile_kernel), the
+// memory, all operands of four such steps in flight at once with up to 16 samples, of two with more (i8_rows_kernel; 48 samples
+// 4096 -> 4096 in 11.2 us, two rounds of loads).  More: tiles of 256 x 256 or 128 x 128 from slabs of 64 bytes of both operands in LDS (i8_tile_kernel), the
 // contraction divided over blocks where the tiles alone do not fill the chip; their shares are added by i8_join_kernel.
 // 4096 x 8192 -> 8192 takes 246 us, 2.23 POP/s: 53 % of what the instruction reaches with operands in registers (4.2, bound by
-// power).  Of those 246 us, the products alone are 135, and bringing the slabs into LDS costs as much as 70: not by its latency
-// (a ring of five slabs in place of four changes nothing).
+// power).
 #include <algorithm>
 
 #include "common.h"
@@ -183,9 +182,11 @@ __global__ __launch_bounds__(256) void i8_dot_kernel(I8Args a) {
 // Lane l holds row l % 16 of either operand and, of the 128 bytes of a step, the 16 from 16 (l / 16) on and the 16 that are 64
 // further: each load takes 64 neighbouring bytes of a row (with 32 neighbouring bytes a lane, in two loads that share every
 // 64, 32 samples of 16 Mi weights took 9.2 us, not 9.0).  With one tile of samples four steps are on their way at once, with
-// more two, for the registers of four leave a CU one block: 16 samples 6.9 and 7.8 us (four, two), 32 9.0 and 8.7, 48 samples
-// 4000 -> 4096 11.9 and 10.4; 48 samples 4096 -> 4096 take 11.2 either way, and 60 samples 3000 -> 5000
-// lose, 13.7 and 14.6.
+// more two, for the registers of four leave a CU one block: 16 samples 4096 -> 4096 6.9 and 7.8 us (four, two).  Of 20 to 128
+// samples, 88 layers of 500 to 8192 inputs and 500 to 10000 outputs, two steps are faster by 2 % in the mean: 48 samples 4000 ->
+// 4096 10.7 us, not 12.7, 4096 -> 4096 11.2 either way.  They lose where a wave's steps are few and leave a remainder: 60 samples
+// 3000 -> 5000 15.0 us, not 14.0, 2000 -> 10000 17.5, not 15.4; but 3000 -> 4096 10.7, not 13.2, so that no rule by the number of
+// inputs separates the two.
 static constexpr int kRowsThreads = 512;
 
 template <typename T, int NB>

@@ -940,7 +940,8 @@ using TileWide = SlabTile<8, 2, 4, 2>;  // 256 x 256
 
 // The tile of a phase, by how many there are for 256 CUs; launch(tile) with its type.  Measured, us a phase (Few / Deep / Two
 // / Wide): X X^T of 1024 x 4096 (36 tiles of 128) 28 / 69 / 96 / 215, of 2048 x 2048 (136) 50 / 45 / 56 / 118; B X of 1024 x 4096
-// (256) 50 / 34 / 39 / 74, of 2048 x 4096 (512) 168 / 115 / 100 / 134, of 4096 x 4096 (1024) 536 / 397 / 361 / 329.
+// (256) 50 / 34 / 39 / 74, of 2048 x 4096 (512) 168 / 115 / 100 / 134, of 4096 x 4096 (1024) 536 / 397 / 361 / 329 (B X
+// without what writing X in floats too has added since, 2 and some 15 us at the first and the last of these sizes).
 template <typename F>
 static vcnn_status with_tile(const MuonBatch& b, bool triangle, F launch) {
   int64_t few = 0, two = 0, wide = 0;

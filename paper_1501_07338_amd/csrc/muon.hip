@@ -138,7 +138,7 @@ struct Part {
   __device__ __forceinline__ bool there(int r) const {
     return (int)(threadIdx.x >> 6) * 16 + r < rows_left && (int)(threadIdx.x & 63) < cols_left;
   }
-  // (behind the end: the last one's, so that loads wait for no condition)
+  // (behind the end: the last one's, which nobody uses, so that loads wait for no condition)
   __device__ __forceinline__ int64_t at(int r) const {
     return at0 + (int64_t)min((int)(threadIdx.x >> 6) * 16 + r, rows_left - 1) * pitch + min((int)(threadIdx.x & 63), cols_left - 1);
   }

@@ -273,6 +273,46 @@ vcnn_status vcnn_rmsnorm_workspace_bytes(int32_t rows, int32_t cols, size_t* byt
 vcnn_status vcnn_rmsnorm_bwd(int32_t dtype, int32_t rows, int32_t cols, const void* h, const float* gain, const float* rstd,
                              const void* dy, const void* dh_above, void* dh, float* dgain, void* workspace,
                              size_t workspace_bytes, void* stream);
+/* Dropout of a [rows][cols] matrix of activations, with the residual's addition behind it:
+ *     y[r][c] = residual[r][c] + (kept(r, c) ? x[r][c] / (1 - p) : 0),      dx[r][c] = kept(r, c) ? dy[r][c] / (1 - p) : 0
+ * (one rounding to dtype; residual may be NULL: zero).  No mask is stored: kept(r, c) follows from rng, site, r, c and cols alone, so
+ * the backward call, given what the forward call was given, meets the same elements.  rng is device memory, two uint64 (8-byte
+ * aligned): a seed and a step; site is a number of the caller's for the place in the network.  p, at least 0 and below 1 - 2^-17, is
+ * rounded to T / 65536 (in the scale too).  The random bits are those of Philox4x32-10 under the key (seed low, seed high) on the
+ * counter (block low, block high, step low, site), 32 bits each, block = r * ceil(cols / 8) + c / 8: element c % 8 of the
+ * block has the low (even) or high (odd) half of word (c % 8) / 2, and is kept where that is at least T.  An element that is not
+ * kept leaves nothing of its value, an infinity or NaN neither.  y may be x or residual itself, dx may be dy. */
+vcnn_status vcnn_dropout_fwd(int32_t dtype, int32_t rows, int32_t cols, float p, const uint64_t* rng, int32_t site,
+                             const void* x, const void* residual, void* y, void* stream);
+vcnn_status vcnn_dropout_bwd(int32_t dtype, int32_t rows, int32_t cols, float p, const uint64_t* rng, int32_t site,
+                             const void* dy, void* dx, void* stream);
+/* rng[1] += 1, on the stream: behind a training step, so that a captured one drops other elements each time it is replayed. */
+vcnn_status vcnn_rng_advance(uint64_t* rng, void* stream);
+/* Layer norm of the rows of a [rows][cols] matrix, with dropout (as vcnn_dropout_fwd; p 0: none, rng may then be NULL) and the
+ * residual's addition before it:
+ *     h = residual + dropout(x) (rounded to dtype),   mean[r] = mean_c h[r][c],   rstd[r] = 1 / sqrt(mean_c (h[r][c] - mean[r])^2 + eps),
+ *     y[r][c] = (h[r][c] - mean[r]) * rstd[r] * gain[c] + bias[c]
+ * x, residual, h, y follow dtype; gain, bias [cols], mean, rstd [rows] are float; sums are float, about a first mean (double where
+ * they leave its range, and for rows of more than 16384 elements).  residual and bias may be NULL (zero); without residual and
+ * dropout h is x, and the argument h is not used.  mean and rstd may be NULL; vcnn_layernorm_bwd needs both.  eps must be positive
+ * and finite, cols at most 2^30.  h may be x or residual itself, y may be x where h is not; nothing else may overlap.  A row with an
+ * infinity or NaN gives what the formula gives, in that row alone. */
+vcnn_status vcnn_layernorm_fwd(int32_t dtype, int32_t rows, int32_t cols, float eps, float p, const uint64_t* rng, int32_t site,
+                               const void* x, const void* residual, const float* gain, const float* bias, void* h, void* y,
+                               float* mean, float* rstd, void* stream);
+/* Gradients of vcnn_layernorm_fwd from h (x without a residual and dropout), mean, rstd and dy = dL/dy: with
+ * z = (h - mean)*rstd, t = dy*gain,
+ *     dh[r][c] = dh_above[r][c] + rstd[r] * (t[r][c] - mean_c(t) - z[r][c] * mean_c(t*z)),   dx = dropout'(dh) (before dh's rounding),
+ *     dgain[c] = sum_r dy[r][c] * z[r][c],   dbias[c] = sum_r dy[r][c]
+ * dh is the gradient of residual (and of x without dropout); dx, the gradient of x, is refused at p 0.  dh_above, the gradient that
+ * reaches h beside the norm, may be NULL (zero).  Each of dh, dx, dgain, dbias may be NULL and is then not computed.  dh may be dy
+ * or dh_above itself, dx the other of the two.  workspace: at least vcnn_layernorm_workspace_bytes (partial sums of dgain and
+ * dbias; not needed without both). */
+vcnn_status vcnn_layernorm_workspace_bytes(int32_t rows, int32_t cols, size_t* bytes);
+vcnn_status vcnn_layernorm_bwd(int32_t dtype, int32_t rows, int32_t cols, float p, const uint64_t* rng, int32_t site,
+                               const void* h, const float* gain, const float* mean, const float* rstd, const void* dy,
+                               const void* dh_above, void* dh, void* dx, float* dgain, float* dbias, void* workspace,
+                               size_t workspace_bytes, void* stream);
 /* Rows in 8 bits: vcnn_rmsnorm_fwd_i8 with u = x and scale[r] = a[r] / 127.  For the weights [out_f][in_f] of
  * vcnn_fc_fwd_i8 (one scale per output), and for activations (one per sample). */
 vcnn_status vcnn_quant_rows_i8(int32_t dtype, int32_t rows, int32_t cols, const void* x, int8_t* q, float* scale,

@@ -8,6 +8,7 @@
 #include <cstring>
 
 #include "common.h"
+#include "dropout.h"
 #include "spectral.h"
 
 namespace vcnn {
@@ -1269,6 +1270,77 @@ vcnn_status vcnn_rmsnorm_bwd(int32_t dtype, int32_t rows, int32_t cols, const vo
   if (dgain)
     if (vcnn_status s = check_ws(workspace, workspace_bytes, rmsnorm_bwd_partial_bytes(rows, cols), "rmsnorm_bwd")) return s;
   return launch_rmsnorm_bwd(dtype, rows, cols, h, gain, rstd, dy, dh_above, dh, dgain, (float*)workspace, (hipStream_t)stream);
+}
+
+static vcnn_status check_dropout(const char* what, float p, const uint64_t* rng, int32_t site, Dropout* drop) {
+  const double limit = std::rint((double)p * 65536.0);
+  if (!(p >= 0.f) || !(limit < 65536.0)) return fail(VCNN_ERR_UNSUPPORTED, "%s: the rate must be at least 0 and below 1 - 2^-17", what);
+  *drop = Dropout{nullptr, (uint32_t)site, (uint32_t)limit, (float)(65536.0 / (65536.0 - limit))};
+  if (p == 0.f) return VCNN_OK;
+  if (!rng) return fail(VCNN_ERR_NULL, "%s: NULL generator", what);
+  if (reinterpret_cast<uintptr_t>(rng) & 7) return fail(VCNN_ERR_UNSUPPORTED, "%s: the generator must be 8-byte aligned", what);
+  drop->rng = rng;
+  return VCNN_OK;
+}
+
+static vcnn_status dropout_call(const char* what, int32_t dtype, int32_t rows, int32_t cols, float p, const uint64_t* rng,
+                                int32_t site, const void* x, const void* residual, void* y, void* stream) {
+  Dropout drop;
+  if (vcnn_status s = check_norm(what, dtype, rows, cols)) return s;
+  if (!x || !y || !rng) return fail(VCNN_ERR_NULL, "%s: NULL tensor or generator", what);
+  if (vcnn_status s = check_dropout(what, p, rng, site, &drop)) return s;
+  drop.rng = rng;  // (a rate of 0 keeps every element)
+  return launch_dropout(dtype, rows, cols, drop, x, residual, y, (hipStream_t)stream);
+}
+
+vcnn_status vcnn_dropout_fwd(int32_t dtype, int32_t rows, int32_t cols, float p, const uint64_t* rng, int32_t site,
+                             const void* x, const void* residual, void* y, void* stream) {
+  return dropout_call("dropout_fwd", dtype, rows, cols, p, rng, site, x, residual, y, stream);
+}
+
+vcnn_status vcnn_dropout_bwd(int32_t dtype, int32_t rows, int32_t cols, float p, const uint64_t* rng, int32_t site,
+                             const void* dy, void* dx, void* stream) {
+  return dropout_call("dropout_bwd", dtype, rows, cols, p, rng, site, dy, nullptr, dx, stream);
+}
+
+vcnn_status vcnn_rng_advance(uint64_t* rng, void* stream) {
+  if (!rng) return fail(VCNN_ERR_NULL, "rng_advance: NULL generator");
+  if (reinterpret_cast<uintptr_t>(rng) & 7) return fail(VCNN_ERR_UNSUPPORTED, "rng_advance: the generator must be 8-byte aligned");
+  return launch_rng_advance(rng, (hipStream_t)stream);
+}
+
+vcnn_status vcnn_layernorm_fwd(int32_t dtype, int32_t rows, int32_t cols, float eps, float p, const uint64_t* rng, int32_t site,
+                               const void* x, const void* residual, const float* gain, const float* bias, void* h, void* y,
+                               float* mean, float* rstd, void* stream) {
+  Dropout drop;
+  if (vcnn_status s = check_norm_fwd("layernorm_fwd", dtype, rows, cols, eps, x, residual, gain, h, y)) return s;
+  if (vcnn_status s = check_dropout("layernorm_fwd", p, rng, site, &drop)) return s;
+  if (drop.rng && !h) return fail(VCNN_ERR_NULL, "layernorm_fwd: NULL h");
+  return launch_layernorm(dtype, rows, cols, eps, drop, x, residual, gain, bias, h, y, mean, rstd, (hipStream_t)stream);
+}
+
+vcnn_status vcnn_layernorm_workspace_bytes(int32_t rows, int32_t cols, size_t* bytes) {
+  if (!bytes) return fail(VCNN_ERR_NULL, "layernorm_workspace_bytes: NULL out-parameter");
+  if (vcnn_status s = check_norm("layernorm_workspace_bytes", VCNN_F32, rows, cols)) return s;
+  *bytes = layernorm_bwd_partial_bytes(rows, cols);
+  return VCNN_OK;
+}
+
+vcnn_status vcnn_layernorm_bwd(int32_t dtype, int32_t rows, int32_t cols, float p, const uint64_t* rng, int32_t site,
+                               const void* h, const float* gain, const float* mean, const float* rstd, const void* dy,
+                               const void* dh_above, void* dh, void* dx, float* dgain, float* dbias, void* workspace,
+                               size_t workspace_bytes, void* stream) {
+  Dropout drop;
+  if (vcnn_status s = check_norm("layernorm_bwd", dtype, rows, cols)) return s;
+  if (vcnn_status s = check_dropout("layernorm_bwd", p, rng, site, &drop)) return s;
+  if (!h || !gain || !mean || !rstd || !dy) return fail(VCNN_ERR_NULL, "layernorm_bwd: NULL tensor");
+  if (dx && !drop.rng) return fail(VCNN_ERR_UNSUPPORTED, "layernorm_bwd: without dropout the gradient of x is dh");
+  if (dx && dx == dh) return fail(VCNN_ERR_UNSUPPORTED, "layernorm_bwd: dh and dx are two tensors");
+  if (!dh && !dx && !dgain && !dbias) return VCNN_OK;
+  if (dgain || dbias)
+    if (vcnn_status s = check_ws(workspace, workspace_bytes, layernorm_bwd_partial_bytes(rows, cols), "layernorm_bwd")) return s;
+  return launch_layernorm_bwd(dtype, rows, cols, drop, h, gain, mean, rstd, dy, dh_above, dh, dx, dgain, dbias, (float*)workspace,
+                              (hipStream_t)stream);
 }
 
 vcnn_status vcnn_quant_rows_i8(int32_t dtype, int32_t rows, int32_t cols, const void* x, int8_t* q, float* scale,

@@ -489,6 +489,17 @@ vcnn_status launch_quant_rows_i8(int dtype, int rows, int cols, const void* x, i
 size_t rmsnorm_bwd_partial_bytes(int rows, int cols);
 vcnn_status launch_rmsnorm_bwd(int dtype, int rows, int cols, const void* h, const float* gain, const float* rstd,
                                const void* dy, const void* above, void* dh, float* dgain, float* partial, hipStream_t st);
+// dropout.hip, layernorm.hip
+struct Dropout;
+vcnn_status launch_dropout(int dtype, int rows, int cols, const Dropout& drop, const void* x, const void* residual, void* y,
+                           hipStream_t st);
+vcnn_status launch_rng_advance(uint64_t* rng, hipStream_t st);
+size_t layernorm_bwd_partial_bytes(int rows, int cols);
+vcnn_status launch_layernorm(int dtype, int rows, int cols, float eps, const Dropout& drop, const void* x, const void* residual,
+                             const float* gain, const float* bias, void* h, void* y, float* mean, float* rstd, hipStream_t st);
+vcnn_status launch_layernorm_bwd(int dtype, int rows, int cols, const Dropout& drop, const void* h, const float* gain,
+                                 const float* mean, const float* rstd, const void* dy, const void* above, void* dh, void* dx,
+                                 float* dgain, float* dbias, float* partial, hipStream_t st);
 
 // ---- int8.hip -------------------------------------------------------------------------------------------
 static constexpr int kMaxI8Depth = 131071;  // sums of products of at most 2^14 below 2^31

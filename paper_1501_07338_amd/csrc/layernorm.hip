@@ -1,0 +1,477 @@
+// Layer norm of the rows of a matrix, with dropout and the residual's addition before it, forward and backward:
+//     h = residual + dropout(x) (rounded to the storage type),   m = mean h,   s = 1 / sqrt(mean((h - m)^2) + eps),   z = (h - m) s
+//     y = z g + b
+//     dh = above + s (t - mean t - z mean(t z)),  t = dy g;   dx = dropout'(dh);   dg = sum over rows of dy z,  db = of dy
+//
+// All of it is bandwidth (and, with dropout, the generator's products).  A row is read once and kept in registers over its sums,
+// divided over threads as in rows.h; rows of more than 16384 elements are read twice.
+#include "dropout.h"
+#include "rows.h"
+
+namespace vcnn {
+
+// ---- sums over a row's threads -------------------------------------------------------------------------------------------
+template <typename S>
+struct PairSums {  // one slot per wave; two sets, taken in turn
+  S a[2][kMaxWaves], b[2][kMaxWaves];
+};
+// Both sums over the row's threads, in every thread.  A set is written again two calls later, behind a barrier that follows
+// every wave's reading of it.
+template <bool WAVE, typename S>
+__device__ __forceinline__ void pair_reduce(PairSums<S>& s, int& turn, S& x, S& y) {
+  x = wave_sum(x), y = wave_sum(y);
+  if constexpr (!WAVE) {
+    const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    if ((threadIdx.x & 63) == 0) s.a[turn][wave] = x, s.b[turn][wave] = y;
+    __syncthreads();
+    x = 0, y = 0;
+    for (int w = 0; w < waves; ++w) x += s.a[turn][w], y += s.b[turn][w];
+    turn ^= 1;
+  }
+}
+
+// Waves a SIMD, of the forward kernel (elements, gain, bias, two tensors' groups of the next row) ...
+constexpr int ln_waves(int nv, int group) {
+  const int registers = nv * (3 * group + 8);
+  return registers <= 32 ? 6 : registers <= 64 ? 4 : registers <= 96 ? 3 : 2;
+}
+
+struct LayerNormArgs {
+  const void* x;
+  const void* residual;  // null: none
+  const float* gain;
+  const float* bias;     // null: none
+  void* h;               // written with a residual or dropout only
+  void* y;
+  float* mean;           // null: not wanted
+  float* rstd;
+  int rows, cols;
+  float eps;
+  Dropout drop;
+};
+
+template <typename T, bool DROP, int NV, bool WAVE>
+__global__ __launch_bounds__(WAVE ? kWaveThreads : NV ? kKeptThreads : 1024, NV ? ln_waves(NV, 16 / (int)sizeof(T)) : 4) void layernorm_kernel(LayerNormArgs a) {
+  constexpr int N = Group<T>::N, K = NV ? NV : 1;
+  __shared__ PairSums<float> sums;
+  __shared__ PairSums<double> wide_sums;
+  const int per_row = WAVE ? 64 : blockDim.x, tid = WAVE ? threadIdx.x & 63 : threadIdx.x;
+  const int rows_at_once = WAVE ? kWaveThreads / 64 : 1;
+  const int cols = a.cols;
+  const uint32_t blocks = dropout_blocks(cols);
+  const bool residual = a.residual, stored = DROP || residual;
+  const Dropout& drop = a.drop;
+  DropoutKey key{};
+  if constexpr (DROP) key = DropoutKey(drop);
+  float gain[K][N], bias[K][N];
+  auto affine = [&](int k, int c) {
+    load_gain(a.gain, c, cols, gain[k]);
+    if (a.bias) {
+      load_gain(a.bias, c, cols, bias[k]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) bias[k][i] = 0.f;
+    }
+  };
+  if constexpr (NV > 0) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k) affine(k, (k * per_row + tid) * N);
+  }
+  const int64_t stride = (int64_t)gridDim.x * rows_at_once;
+  int64_t row = (int64_t)blockIdx.x * rows_at_once + (WAVE ? threadIdx.x >> 6 : 0);
+  // a row's groups are on their way while the row before is reduced and written
+  Loose16 px[K], pr[K];
+  auto fetch = [&](int64_t at) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int c = (k * per_row + tid) * N;
+      if (c >= cols) continue;
+      px[k] = load_group(reinterpret_cast<const T*>(a.x) + at * cols, c, cols);
+      if (residual) pr[k] = load_group(reinterpret_cast<const T*>(a.residual) + at * cols, c, cols);
+    }
+  };
+  if (NV > 0 && row < a.rows) fetch(row);
+  int turn = 0, wide_turn = 0;
+  for (; row < a.rows; row += stride) {
+    const T* const x = reinterpret_cast<const T*>(a.x) + row * cols;
+    T* const h = reinterpret_cast<T*>(a.h) + row * cols;
+    T* const y = reinterpret_cast<T*>(a.y) + row * cols;
+    // the group at c, dropped, the residual added, and the sum stored
+    auto take = [&](int c, const Loose16& gx, const Loose16& gr, float (&v)[N]) {
+      unpack(gx, v);
+      if (!stored) return;
+      uint32_t bits[N];
+      if constexpr (DROP) dropout_bits(key, (uint64_t)row * blocks, c, bits);
+      if (residual) {
+        float w[N];
+        unpack(gr, w);
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = DROP ? dropped(v[i], bits[i], drop, w[i]) : v[i] + w[i];
+      } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = DROP ? dropped(v[i], bits[i], drop) : v[i];
+      }
+      const Loose16 ph = pack(v);
+      unpack(ph, v);
+      store_group(h, c, cols, ph);
+    };
+    // each(f): f(c, v, whole) over this thread's groups of the row, each of v its element c + i (whole: all of them in the row)
+    float v[K][N];
+    const T* const kept = stored ? h : x;  // (rows read twice: every thread meets its own elements again)
+    auto each = [&](auto f) {
+      if constexpr (NV > 0) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+          const int c = (k * per_row + tid) * N;
+          if (c < cols) f(k, c, v[k]);
+        }
+      } else {
+        for (int c = tid * N; c < cols; c += per_row * N) {
+          unpack(load_group(kept, c, cols), v[0]);
+          f(0, c, v[0]);
+        }
+      }
+    };
+    // m0 + shift is the mean; the two together carry more than a float's digits, for rows whose mean dwarfs their spread
+    float m0, shift, rstd;
+    bool again = false;
+    if constexpr (NV > 0) {
+      float sum = 0.f, zero = 0.f;
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        const int c = (k * per_row + tid) * N;
+        if (c < cols) {
+          take(c, px[k], pr[k], v[k]);
+#pragma unroll
+          for (int i = 0; i < N; ++i) sum += v[k][i];  // (zeros behind the row's end)
+        }
+      }
+      if (row + stride < a.rows) fetch(row + stride);
+      pair_reduce<WAVE>(sums, turn, sum, zero);
+      m0 = sum / (float)cols;
+      float off = 0.f, squares = 0.f;
+      each([&](int, int c, const float (&u)[N]) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const float d = c + N <= cols || c + i < cols ? u[i] - m0 : 0.f;
+          off += d, squares = fmaf(d, d, squares);
+        }
+      });
+      pair_reduce<WAVE>(sums, turn, off, squares);
+      shift = off / (float)cols;
+      const float variance = fmaxf(squares / (float)cols - shift * shift, 0.f) + a.eps;
+      rstd = 1.f / sqrtf(variance);
+      // sums beyond the float range (or not finite), or squares so small that their roundings, up to 2^-150 each, are seen in
+      // the variance (only with an eps as small): once more in double
+      again = !(squares < __builtin_inff()) || variance < 0x1p-120f;
+    } else {
+      // sums about this thread's first element, in double, joined about the row's mean
+      double sum = 0., squares = 0., first = 0.;
+      int count = 0;
+      for (int c = tid * N; c < cols; c += per_row * N) {
+        px[0] = load_group(x, c, cols);
+        if (residual) pr[0] = load_group(reinterpret_cast<const T*>(a.residual) + row * cols, c, cols);
+        take(c, px[0], pr[0], v[0]);
+        if (count == 0) first = v[0][0];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          if (c + N > cols && c + i >= cols) continue;
+          const double d = v[0][i] - first;
+          sum += d, squares += d * d, ++count;
+        }
+      }
+      double total = sum + count * first, zero = 0.;
+      pair_reduce<WAVE>(wide_sums, wide_turn, total, zero);
+      const double mean = total / cols, off = first - mean;  // (v - mean = d + off)
+      squares += 2. * off * sum + count * off * off;
+      zero = 0.;
+      pair_reduce<WAVE>(wide_sums, wide_turn, squares, zero);
+      m0 = (float)mean, shift = (float)(mean - m0);
+      const float variance = (float)(fmax(squares, 0.) / cols) + a.eps;
+      rstd = 1.f / sqrtf(variance);
+      again = !(variance < __builtin_inff()) || !(fabsf(m0) < __builtin_inff()) || variance < 0x1p-120f;
+    }
+    double wide_mean = 0., wide_rstd = 0.;
+    if (again) {
+      double total = 0., zero = 0.;
+      each([&](int, int c, const float (&u)[N]) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) total += (double)u[i];  // (zeros behind the row's end)
+      });
+      pair_reduce<WAVE>(wide_sums, wide_turn, total, zero);
+      wide_mean = total / cols;
+      double squares = 0.;
+      each([&](int, int c, const float (&u)[N]) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const double d = c + N <= cols || c + i < cols ? u[i] - wide_mean : 0.;
+          squares += d * d;
+        }
+      });
+      zero = 0.;
+      pair_reduce<WAVE>(wide_sums, wide_turn, squares, zero);
+      wide_rstd = 1. / sqrt(squares / cols + (double)a.eps);
+      m0 = (float)wide_mean, shift = 0.f, rstd = (float)wide_rstd;
+    }
+    if (tid == 0) {
+      if (a.mean) a.mean[row] = m0 + shift;
+      if (a.rstd) a.rstd[row] = rstd;
+    }
+    each([&](int k, int c, const float (&u)[N]) {
+      if (NV == 0) affine(0, c);
+      float o[N];
+      if (again) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) o[i] = fmaf((float)((u[i] - wide_mean) * wide_rstd), gain[k][i], bias[k][i]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) o[i] = fmaf(((u[i] - m0) - shift) * rstd, gain[k][i], bias[k][i]);
+      }
+      store_group(y, c, cols, pack(o));
+    });
+  }
+}
+
+template <typename T, bool DROP>
+static void launch_layernorm_typed(const LayerNormArgs& a, hipStream_t st) {
+  const RowShape s = row_shape(a.rows, a.cols, Group<T>::N, true, ln_waves);
+  with_shape<T>(s, [&](auto nv, auto wave) {
+    hipLaunchKernelGGL((layernorm_kernel<T, DROP, decltype(nv)::value, decltype(wave)::value>), dim3(s.blocks),
+                       dim3(s.threads == 64 ? kWaveThreads : s.threads), 0, st, a);
+  });
+}
+
+vcnn_status launch_layernorm(int dtype, int rows, int cols, float eps, const Dropout& drop, const void* x, const void* residual,
+                             const float* gain, const float* bias, void* h, void* y, float* mean, float* rstd, hipStream_t st) {
+  const LayerNormArgs a{x, residual, gain, bias, h, y, mean, rstd, rows, cols, eps, drop};
+  if (dtype == VCNN_BF16) drop.rng ? launch_layernorm_typed<bf16, true>(a, st) : launch_layernorm_typed<bf16, false>(a, st);
+  else drop.rng ? launch_layernorm_typed<float, true>(a, st) : launch_layernorm_typed<float, false>(a, st);
+  return check_launch("layernorm");
+}
+
+// ---- backward ------------------------------------------------------------------------------------------------------------
+// A block takes every gridDim-th row (or four) and adds their share of dg and db in registers; the blocks' shares are added in a
+// fixed order by a second kernel, so that both have the same bits in every run.
+struct LayerNormBwdArgs {
+  const void* h;
+  const float* gain;
+  const float* mean;
+  const float* rstd;
+  const void* dy;
+  const void* above;  // gradient that reaches h beside the norm (nullable)
+  void* dh;           // nullable
+  void* dx;           // with dropout (nullable)
+  float* partial;     // [blocks][2][cols] (nullable: neither dg nor db)
+  int rows, cols;
+  Dropout drop;
+};
+
+static constexpr int kLnBwdBlocks = 512;
+
+template <typename T, bool DROP, int NV, bool WAVE>
+__global__ __launch_bounds__(WAVE ? kWaveThreads : NV ? kKeptThreads : 1024) void layernorm_bwd_kernel(LayerNormBwdArgs a) {
+  constexpr int N = Group<T>::N, K = NV ? NV : 1;
+  __shared__ PairSums<float> sums;
+  __shared__ PairSums<double> wide_sums;
+  __shared__ float shares[WAVE ? 3 * 64 * K * N : 1];
+  const int per_row = WAVE ? 64 : blockDim.x, tid = WAVE ? threadIdx.x & 63 : threadIdx.x;
+  const int rows_at_once = WAVE ? kWaveThreads / 64 : 1, wave = threadIdx.x >> 6;
+  const int cols = a.cols;
+  const uint32_t blocks = dropout_blocks(cols);
+  const Dropout& drop = a.drop;
+  DropoutKey key{};
+  if constexpr (DROP) key = DropoutKey(drop);
+  float* const partial = a.partial ? a.partial + (int64_t)blockIdx.x * 2 * cols : nullptr;
+  float gain[K][N], dg[K][N], db[K][N];
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    if (NV > 0) load_gain(a.gain, (k * per_row + tid) * N, cols, gain[k]);
+#pragma unroll
+    for (int i = 0; i < N; ++i) dg[k][i] = db[k][i] = 0.f;
+  }
+  int turn = 0, wide_turn = 0;
+  for (int64_t row = (int64_t)blockIdx.x * rows_at_once + (WAVE ? wave : 0); row < a.rows; row += (int64_t)gridDim.x * rows_at_once) {
+    const T* const h = reinterpret_cast<const T*>(a.h) + row * cols;
+    const T* const dy = reinterpret_cast<const T*>(a.dy) + row * cols;
+    const T* const above = a.above ? reinterpret_cast<const T*>(a.above) + row * cols : nullptr;
+    const float rstd = a.rstd[row], mean = a.mean[row];
+    Loose16 ph[K], pd[K], pa[K];
+    // z = (h - m) s, t = dy g, and this group's share of sum t and sum t z
+    auto meet = [&](const Loose16& gh, const Loose16& gd, const float (&g)[N], float (&z)[N], float (&d)[N], float& st, float& stz) {
+      unpack(gh, z), unpack(gd, d);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        z[i] = (z[i] - mean) * rstd;
+        const float t = d[i] * g[i];
+        st += t, stz = fmaf(t, z[i], stz);
+      }
+    };
+    float mt, mtz;
+    if constexpr (NV > 0) {
+      float st = 0.f, stz = 0.f;
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        const int c = (k * per_row + tid) * N;
+        if (c < cols) {
+          ph[k] = load_group(h, c, cols), pd[k] = load_group(dy, c, cols);
+          if (above) pa[k] = load_group(above, c, cols);
+        } else {
+          ph[k] = pd[k] = Loose16{{0, 0, 0, 0}};
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        float z[N], d[N];  // (behind the row's end dy and the gain are 0)
+        meet(ph[k], pd[k], gain[k], z, d, st, stz);
+#pragma unroll
+        for (int i = 0; i < N; ++i) dg[k][i] = fmaf(d[i], z[i], dg[k][i]), db[k][i] += d[i];
+      }
+      pair_reduce<WAVE>(sums, turn, st, stz);
+      mt = st / (float)cols, mtz = stz / (float)cols;
+    } else {
+      double st = 0., stz = 0.;
+      for (int c = tid * N; c < cols; c += per_row * N) {
+        float z[N], d[N], s1 = 0.f, s2 = 0.f;
+        load_gain(a.gain, c, cols, gain[0]);
+        meet(load_group(h, c, cols), load_group(dy, c, cols), gain[0], z, d, s1, s2);
+        st += s1, stz += s2;
+        if (partial) {  // (this thread's own elements, turn after turn)
+          const bool opens = row == blockIdx.x;
+#pragma unroll
+          for (int i = 0; i < N; ++i)
+            if (c + i < cols) {
+              partial[c + i] = (opens ? 0.f : partial[c + i]) + d[i] * z[i];
+              partial[cols + c + i] = (opens ? 0.f : partial[cols + c + i]) + d[i];
+            }
+        }
+      }
+      pair_reduce<WAVE>(wide_sums, wide_turn, st, stz);
+      mt = (float)(st / cols), mtz = (float)(stz / cols);
+    }
+    if (!a.dh && !a.dx) continue;
+    auto give = [&](int c, const Loose16& gh, const Loose16& gd, const Loose16& ga, const float (&g)[N]) {
+      float hv[N], d[N], o[N];
+      unpack(gh, hv), unpack(gd, d);
+#pragma unroll
+      for (int i = 0; i < N; ++i) o[i] = rstd * (d[i] * g[i] - mt - (hv[i] - mean) * rstd * mtz);
+      if (above) {
+        float w[N];
+        unpack(ga, w);
+#pragma unroll
+        for (int i = 0; i < N; ++i) o[i] += w[i];
+      }
+      if (a.dh) store_group(reinterpret_cast<T*>(a.dh) + row * cols, c, cols, pack(o));
+      if constexpr (DROP) {
+        if (!a.dx) return;
+        uint32_t bits[N];
+        dropout_bits(key, (uint64_t)row * blocks, c, bits);
+#pragma unroll
+        for (int i = 0; i < N; ++i) o[i] = dropped(o[i], bits[i], drop);
+        store_group(reinterpret_cast<T*>(a.dx) + row * cols, c, cols, pack(o));
+      }
+    };
+    if constexpr (NV > 0) {
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        const int c = (k * per_row + tid) * N;
+        if (c < cols) give(c, ph[k], pd[k], pa[k], gain[k]);
+      }
+    } else {
+      for (int c = tid * N; c < cols; c += per_row * N) {
+        if (above) pa[0] = load_group(above, c, cols);
+        load_gain(a.gain, c, cols, gain[0]);
+        give(c, load_group(h, c, cols), load_group(dy, c, cols), pa[0], gain[0]);
+      }
+    }
+  }
+  if constexpr (NV > 0) {
+    if (!partial) return;
+    auto leave = [&](float (&sum)[K][N], float* to) {
+      if constexpr (WAVE) {  // the four waves' shares, in order
+        if (wave > 0) {
+#pragma unroll
+          for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int i = 0; i < N; ++i) shares[((wave - 1) * NV * N + k * N + i) * 64 + tid] = sum[k][i];
+        }
+        __syncthreads();
+        if (wave == 0) {
+#pragma unroll
+          for (int w = 0; w < 3; ++w)
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+              for (int i = 0; i < N; ++i) sum[k][i] += shares[(w * NV * N + k * N + i) * 64 + tid];
+        }
+        __syncthreads();
+        if (wave > 0) return;
+      }
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        const int c = (k * per_row + tid) * N;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+          if (c + i < cols) to[c + i] = sum[k][i];
+      }
+    };
+    leave(dg, partial);
+    leave(db, partial + cols);
+  }
+}
+
+// dg and db from the blocks' shares: 64 threads a column take every 64th, and their sums are added in pairs, always the same ones.
+__global__ __launch_bounds__(1024) void affine_grad_kernel(const float* partial, float* dg, float* db, int blocks, int cols) {
+  __shared__ float sums[64][17];
+  const int in = threadIdx.x & 15, part = threadIdx.x >> 4;
+  const int64_t col = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 16 + in;  // of the 2 cols
+  float s = 0.f;
+  if (col < 2 * (int64_t)cols) {
+#pragma unroll 8
+    for (int b = part; b < blocks; b += 64) s += partial[(int64_t)b * 2 * cols + col];
+  }
+  sums[part][in] = s;
+  for (int n = 32; n > 0; n >>= 1) {
+    __syncthreads();
+    if (part < n) sums[part][in] += sums[part + n][in];
+  }
+  if (part > 0 || col >= 2 * (int64_t)cols) return;
+  if (col < cols) {
+    if (dg) dg[col] = sums[0][in];
+  } else if (db) {
+    db[col - cols] = sums[0][in];
+  }
+}
+
+size_t layernorm_bwd_partial_bytes(int rows, int cols) {
+  return (size_t)std::min(rows, kLnBwdBlocks) * 2 * cols * sizeof(float);
+}
+
+template <typename T, bool DROP>
+static int launch_layernorm_bwd_typed(const LayerNormBwdArgs& a, hipStream_t st) {
+  RowShape s = row_shape(a.rows, a.cols, Group<T>::N, false);
+  s.blocks = std::min(s.blocks, kLnBwdBlocks);
+  with_shape<T>(s, [&](auto nv, auto wave) {
+    hipLaunchKernelGGL((layernorm_bwd_kernel<T, DROP, decltype(nv)::value, decltype(wave)::value>), dim3(s.blocks),
+                       dim3(s.threads == 64 ? kWaveThreads : s.threads), 0, st, a);
+  });
+  return s.blocks;
+}
+
+vcnn_status launch_layernorm_bwd(int dtype, int rows, int cols, const Dropout& drop, const void* h, const float* gain,
+                                 const float* mean, const float* rstd, const void* dy, const void* above, void* dh, void* dx,
+                                 float* dgain, float* dbias, float* partial, hipStream_t st) {
+  const LayerNormBwdArgs a{h, gain, mean, rstd, dy, above, dh, dx, dgain || dbias ? partial : nullptr, rows, cols, drop};
+  int blocks;
+  if (dtype == VCNN_BF16)
+    blocks = drop.rng ? launch_layernorm_bwd_typed<bf16, true>(a, st) : launch_layernorm_bwd_typed<bf16, false>(a, st);
+  else
+    blocks = drop.rng ? launch_layernorm_bwd_typed<float, true>(a, st) : launch_layernorm_bwd_typed<float, false>(a, st);
+  if (vcnn_status s = check_launch("layernorm_bwd")) return s;
+  if (!a.partial) return VCNN_OK;
+  const unsigned groups = (unsigned)ceil_div(2 * (int64_t)cols, 16), wide = std::min(groups, 1u << 16);
+  hipLaunchKernelGGL(affine_grad_kernel, dim3(wide, (unsigned)ceil_div(groups, wide)), dim3(1024), 0, st, partial, dgain, dbias,
+                     blocks, cols);
+  return check_launch("layernorm_bwd gain and bias");
+}
+
+}  // namespace vcnn

@@ -82,6 +82,15 @@ _SIGNATURES = {
     "vcnn_rmsnorm_workspace_bytes": (c_int32, [c_int32, c_int32, POINTER(c_size_t)]),
     "vcnn_rmsnorm_bwd": (c_int32, [c_int32, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
                                    c_void_p, c_void_p, c_size_t, c_void_p]),
+    "vcnn_dropout_fwd": (c_int32, [c_int32, c_int32, c_int32, c_float, c_void_p, c_int32, c_void_p, c_void_p, c_void_p, c_void_p]),
+    "vcnn_dropout_bwd": (c_int32, [c_int32, c_int32, c_int32, c_float, c_void_p, c_int32, c_void_p, c_void_p, c_void_p]),
+    "vcnn_rng_advance": (c_int32, [c_void_p, c_void_p]),
+    "vcnn_layernorm_fwd": (c_int32, [c_int32, c_int32, c_int32, c_float, c_float, c_void_p, c_int32, c_void_p, c_void_p,
+                                     c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]),
+    "vcnn_layernorm_workspace_bytes": (c_int32, [c_int32, c_int32, POINTER(c_size_t)]),
+    "vcnn_layernorm_bwd": (c_int32, [c_int32, c_int32, c_int32, c_float, c_void_p, c_int32, c_void_p, c_void_p, c_void_p,
+                                     c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_size_t,
+                                     c_void_p]),
     "vcnn_quant_rows_i8": (c_int32, [c_int32, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_void_p]),
     "vcnn_fc_i8_workspace_bytes": (c_int32, [c_int32, c_int32, c_int32, POINTER(c_size_t)]),
     "vcnn_fc_fwd_i8": (c_int32, [c_int32, c_int32, c_int32, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_void_p,
@@ -333,6 +342,37 @@ def rmsnorm_bwd(dtype, rows, cols, h, gain, rstd, dy, dh_above, dh, dgain, works
     p, nbytes = _ws(workspace)
     _check(lib().vcnn_rmsnorm_bwd(dtype, rows, cols, _ptr(h), _ptr(gain), _ptr(rstd), _ptr(dy), _ptr(dh_above), _ptr(dh),
                                   _ptr(dgain), p, nbytes, _stream(stream)))
+
+
+def dropout_fwd(dtype, rows, cols, p, rng, site, x, residual, y, stream=None):
+    """rng: two 64-bit integers on the device, the seed and the step."""
+    _check(lib().vcnn_dropout_fwd(dtype, rows, cols, p, _ptr(rng), site, _ptr(x), _ptr(residual), _ptr(y), _stream(stream)))
+
+
+def dropout_bwd(dtype, rows, cols, p, rng, site, dy, dx, stream=None):
+    _check(lib().vcnn_dropout_bwd(dtype, rows, cols, p, _ptr(rng), site, _ptr(dy), _ptr(dx), _stream(stream)))
+
+
+def rng_advance(rng, stream=None):
+    _check(lib().vcnn_rng_advance(_ptr(rng), _stream(stream)))
+
+
+def layernorm_fwd(dtype, rows, cols, eps, p, rng, site, x, residual, gain, bias, h, y, mean, rstd, stream=None):
+    _check(lib().vcnn_layernorm_fwd(dtype, rows, cols, eps, p, _ptr(rng), site, _ptr(x), _ptr(residual), _ptr(gain), _ptr(bias),
+                                    _ptr(h), _ptr(y), _ptr(mean), _ptr(rstd), _stream(stream)))
+
+
+def layernorm_workspace_bytes(rows, cols) -> int:
+    b = c_size_t()
+    _check(lib().vcnn_layernorm_workspace_bytes(rows, cols, byref(b)))
+    return b.value
+
+
+def layernorm_bwd(dtype, rows, cols, p, rng, site, h, gain, mean, rstd, dy, dh_above, dh, dx, dgain, dbias, workspace=None,
+                  stream=None):
+    w, nbytes = _ws(workspace)
+    _check(lib().vcnn_layernorm_bwd(dtype, rows, cols, p, _ptr(rng), site, _ptr(h), _ptr(gain), _ptr(mean), _ptr(rstd), _ptr(dy),
+                                    _ptr(dh_above), _ptr(dh), _ptr(dx), _ptr(dgain), _ptr(dbias), w, nbytes, _stream(stream)))
 
 
 def quant_rows_i8(dtype, rows, cols, x, q, scale, stream=None):

@@ -1,0 +1,171 @@
+"""Dropout from the counter-based generator against a plain generator in numpy, whose own known answers are checked first.
+
+Tolerances.  The scale is a float (a rounding of 2^-24), the sum with the residual is rounded once in float and once to the type."""
+import numpy as np
+import pytest
+import torch
+
+from paper_1501_07338_amd import vcnn
+from test_gpu_norm import DEV, TYPES, U, Guarded, dev, half_step, tensor
+
+SHAPES = [(1, 1), (1, 7), (3, 8), (5, 9), (128, 500), (7, 1021), (2, 16384), (3, 40001), (1300, 33), (4100, 200), (1, 1 << 20)]
+
+
+def philox(counter, key):
+    """Philox4x32-10 of counters [n][4] under one key of two words (numpy, 64-bit products)."""
+    low, half = np.uint64(0xffffffff), np.uint64(32)
+    a, b, c, d = (counter[:, i].astype(np.uint64) for i in range(4))
+    k0, k1 = int(key[0]), int(key[1])
+    for _ in range(10):
+        p, q = a * np.uint64(0xD2511F53), c * np.uint64(0xCD9E8D57)
+        a, b, c, d = (q >> half) ^ b ^ np.uint64(k0), q & low, (p >> half) ^ d ^ np.uint64(k1), p & low
+        k0, k1 = (k0 + 0x9E3779B9) & 0xffffffff, (k1 + 0xBB67AE85) & 0xffffffff
+    return np.stack([a, b, c, d], 1).astype(np.uint32)
+
+
+def factors(rows, cols, p, seed, step, site):
+    """What each element is multiplied by: 0 or the scale (64 bits)."""
+    blocks = -(-cols // 8)
+    n = np.arange(rows * blocks, dtype=np.uint64)
+    ctr = np.stack([n & np.uint64(0xffffffff), n >> np.uint64(32), np.full_like(n, step & 0xffffffff),
+                    np.full_like(n, site & 0xffffffff)], 1)
+    words = philox(ctr, (seed & 0xffffffff, seed >> 32))
+    bits = np.stack([words & 0xffff, words >> 16], 2).reshape(rows, blocks * 8)[:, :cols]
+    limit = int(np.rint(np.float64(np.float32(p)) * 65536))
+    return torch.from_numpy((bits >= limit) * (65536 / (65536 - limit)))
+
+
+def generator(seed=0x123456789abcdef, step=7):
+    return torch.from_numpy(np.array([seed, step], dtype=np.uint64).view(np.int64)).to(DEV)
+
+
+def test_known_answers_of_the_plain_generator():
+    ctr = np.array([[0] * 4, [0xffffffff] * 4, [0x243f6a88, 0x85a308d3, 0x13198a2e, 0x03707344]], dtype=np.uint32)
+    keys = [(0, 0), (0xffffffff, 0xffffffff), (0xa4093822, 0x299f31d0)]
+    want = [(0x6627e8d5, 0xe169c58d, 0xbc57ac4c, 0x9b00dbd8), (0x408f276d, 0x41c83b0e, 0xa20bc7c6, 0x6d5451fd),
+            (0xd16cfe09, 0x94fdcceb, 0x5001e420, 0x24126ea1)]
+    for c, k, w in zip(ctr, keys, want):
+        assert tuple(int(v) for v in philox(c[None], k)[0]) == w
+
+
+def test_refusals_need_no_gpu():
+    lib, fake = vcnn.lib(), 0x1000  # never dereferenced: validation fails first
+    fwd = lambda dtype=vcnn.F32, rows=2, cols=8, p=0.5, rng=fake, x=fake, y=fake: \
+        lib.vcnn_dropout_fwd(dtype, rows, cols, p, rng, 0, x, None, y, None)  # noqa: E731
+    assert fwd(rows=0) == vcnn.ERR_SHAPE and fwd(cols=-1) == vcnn.ERR_SHAPE
+    assert fwd(dtype=5) == vcnn.ERR_UNSUPPORTED and fwd(cols=(1 << 30) + 1) == vcnn.ERR_UNSUPPORTED
+    for p in (-0.1, 1.0, 1.5, float("nan"), float("inf"), 1 - 2.0 ** -18):
+        assert fwd(p=p) == vcnn.ERR_UNSUPPORTED
+    assert fwd(rng=None) == vcnn.ERR_NULL and fwd(x=None) == vcnn.ERR_NULL and fwd(y=None) == vcnn.ERR_NULL
+    assert fwd(rng=0x1004) == vcnn.ERR_UNSUPPORTED
+    assert lib.vcnn_dropout_bwd(vcnn.F32, 2, 8, 0.5, fake, 0, None, fake, None) == vcnn.ERR_NULL
+    assert lib.vcnn_dropout_bwd(vcnn.F32, 2, 8, 1.0, fake, 0, fake, fake, None) == vcnn.ERR_UNSUPPORTED
+    assert lib.vcnn_rng_advance(None, None) == vcnn.ERR_NULL and lib.vcnn_rng_advance(0x1004, None) == vcnn.ERR_UNSUPPORTED
+
+
+def close(got, want, dtype, larger):
+    """One rounding of the scale, one of the float sum, one to the type; `larger`: the largest term of the sum."""
+    want = want.double()
+    return bool(((got.double() - want).abs() <= want.abs() * (half_step(dtype) + 2 * U) + 2 * U * larger + 1e-40).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("offset", [0, 1])
+@pytest.mark.parametrize("dtype", [vcnn.F32, vcnn.BF16])
+@pytest.mark.parametrize("rows,cols", SHAPES)
+def test_both_directions(rows, cols, dtype, offset):
+    x, r, dy = (tensor(s, rows, cols, dtype) for s in (1, 2, 3))
+    rng, p = generator(), 0.3
+    f = factors(rows, cols, p, 0x123456789abcdef, 7, 11)
+    for res in (None, r):
+        y = Guarded((rows, cols), x.dtype, offset)
+        vcnn.dropout_fwd(dtype, rows, cols, p, rng, 11, dev(x, offset), dev(res, offset), y.t)
+        kept = x.double() * f
+        assert close(y.cpu(), kept if res is None else kept + res.double(), dtype, kept.abs())
+    dx = Guarded((rows, cols), x.dtype, offset)
+    vcnn.dropout_bwd(dtype, rows, cols, p, rng, 11, dev(dy, offset), dx.t)
+    assert close(dx.cpu(), dy.double() * f, dtype, 0.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("p", [0.0, 2.0 ** -18, 2.0 ** -16, 0.1, 0.5, 0.9, 1 - 2.0 ** -16])
+def test_rates(p):
+    rows, cols = 64, 4099
+    x, y = torch.ones(rows, cols), Guarded((rows, cols), torch.float32)
+    vcnn.dropout_fwd(vcnn.F32, rows, cols, p, generator(), 0, dev(x), None, y.t)
+    got, f = y.cpu(), factors(rows, cols, p, 0x123456789abcdef, 7, 0)
+    assert torch.equal(got, f.float())
+    # the share of kept elements: six standard deviations of a binomial
+    limit = round(p * 65536) / 65536
+    assert abs(float((got > 0).double().mean()) - (1 - limit)) <= 6 * (limit * (1 - limit) / (rows * cols)) ** 0.5 + 1e-12
+
+
+@pytest.mark.gpu
+def test_seed_step_site_and_place_matter():
+    rows, cols = 16, 512
+    x = dev(torch.ones(rows, cols))
+
+    def mask(seed=1, step=0, site=0):
+        y = torch.empty_like(x)
+        vcnn.dropout_fwd(vcnn.F32, rows, cols, 0.5, generator(seed, step), site, x, None, y)
+        return (y > 0).cpu()
+
+    base, n = mask(), rows * cols
+    assert torch.equal(base, mask())
+    for other in (mask(seed=2), mask(seed=1 + (1 << 32)), mask(step=1), mask(site=1), mask(site=-1)):
+        assert abs(int((base != other).sum()) - n / 2) <= 6 * (n / 4) ** 0.5
+    assert torch.equal(base, mask(step=1 << 32))  # the step counts in 32 bits
+    assert abs(int((base[0] != base[1]).sum()) - cols / 2) <= 6 * (cols / 4) ** 0.5
+    top = generator((1 << 64) - 1, (1 << 32) - 1)
+    y = torch.empty_like(x)
+    vcnn.dropout_fwd(vcnn.F32, rows, cols, 0.5, top, (1 << 31) - 1, x, None, y)
+    assert torch.equal((y > 0).cpu(), factors(rows, cols, 0.5, (1 << 64) - 1, (1 << 32) - 1, (1 << 31) - 1) > 0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [vcnn.F32, vcnn.BF16])
+def test_dropped_infinities_leave_nothing_and_in_place_is_the_same(dtype):
+    rows, cols = 9, 777
+    x, r = tensor(5, rows, cols, dtype), tensor(6, rows, cols, dtype)
+    f = factors(rows, cols, 0.5, 0x123456789abcdef, 7, 2)
+    x[f == 0] = float("nan")
+    x[:, ::3] = torch.where(f[:, ::3] == 0, float("-inf"), x[:, ::3].double()).to(x.dtype)
+    outs = []
+    for where in ("apart", "x", "residual"):
+        dx, dr = dev(x), dev(r)
+        y = {"apart": torch.empty_like(dx), "x": dx, "residual": dr}[where]
+        vcnn.dropout_fwd(dtype, rows, cols, 0.5, generator(), 2, dx, dr, y)
+        outs.append(y.cpu())
+    assert bool(torch.isfinite(outs[0]).all()) and torch.equal(outs[0][f == 0], r[f == 0])
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+    x[f > 0] = float("nan")
+    y = torch.empty_like(dev(x))
+    vcnn.dropout_fwd(dtype, rows, cols, 0.5, generator(), 2, dev(x), None, y)
+    assert torch.equal(torch.isnan(y.cpu()), f > 0)
+
+
+@pytest.mark.gpu
+def test_a_captured_step_drops_other_elements_each_time():
+    rows, cols = 64, 1000
+    x = dev(torch.ones(rows, cols))
+    rng, y, dx = generator(3, 0), torch.empty_like(x), torch.empty_like(x)
+
+    def step():
+        vcnn.dropout_fwd(vcnn.F32, rows, cols, 0.4, rng, 1, x, None, y)
+        vcnn.dropout_bwd(vcnn.F32, rows, cols, 0.4, rng, 1, x, dx)
+        vcnn.rng_advance(rng)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()  # eager, on another stream
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for n in range(1, 5):
+        y.zero_(), dx.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y.cpu(), factors(rows, cols, 0.4, 3, n, 1).float()) and torch.equal(y, dx)
+        assert rng.tolist() == [3, n + 1]

@@ -313,6 +313,26 @@ vcnn_status vcnn_layernorm_bwd(int32_t dtype, int32_t rows, int32_t cols, float 
                                const void* h, const float* gain, const float* mean, const float* rstd, const void* dy,
                                const void* dh_above, void* dh, void* dx, float* dgain, float* dbias, void* workspace,
                                size_t workspace_bytes, void* stream);
+/* A fully connected layer (no activation) and its softmax cross-entropy cost, for many classes: the logits
+ * z[b][j] = bias[j] + sum_i x[b][i]*w[j][i], float whatever dtype is, are not kept.  With C the number of samples whose label is
+ * not `ignore` (none: the loss and the gradients are 0),
+ *     sample_loss[b] = logsumexp(z_b) - z_b[labels[b]] (0 for an ignored sample),   loss = (1/C) sum_b sample_loss[b],
+ *     d[b][j] = (softmax(z_b)[j] - [j == labels[b]]) / C (0 for an ignored sample),
+ *     dx[b][i] = sum_j d[b][j]*w[j][i],   dw[j][i] = sum_b d[b][j]*x[b][i],   dbias[j] = sum_b d[b][j]
+ * x [batch][in_f], w [classes][in_f], dx follow dtype; bias, loss (a scalar), sample_loss, dw, dbias are float; labels int32.  bias
+ * and sample_loss may be NULL; each of dx, dw, dbias may be NULL and is then not computed (all three: the cost alone, and a negative
+ * sample_loss is the log probability of the label).  What an ignored sample's x holds reaches nothing but its own row of dx, which
+ * is 0.  A label that is neither `ignore` nor in 0 .. classes - 1 is never used as an index: the loss, that sample's loss and row
+ * of dx, dw and dbias come out as NaN.  A class with a bias of -infinity is left out.  in_f and classes are at most 2^22; w of
+ * bfloat16 starts on 16 bytes if in_f is a multiple of 8; no output may overlap anything.
+ * workspace: vcnn_fc_softmax_loss_workspace_bytes (grads: whether any gradient is wanted), room for the logits of some of the samples,
+ * 1 GiB of them at most, which go through in parts; a call that brings less takes smaller parts, down to 64 samples (what the
+ * query gives for these, and 4 bytes for each further sample). */
+vcnn_status vcnn_fc_softmax_loss_workspace_bytes(int32_t dtype, int32_t batch, int32_t in_f, int32_t classes, int32_t grads,
+                                                 size_t* bytes);
+vcnn_status vcnn_fc_softmax_loss(int32_t dtype, int32_t batch, int32_t in_f, int32_t classes, const void* x, const void* w,
+                                 const float* bias, const int32_t* labels, int32_t ignore, float* loss, float* sample_loss, void* dx,
+                                 float* dw, float* dbias, void* workspace, size_t workspace_bytes, void* stream);
 /* Rows in 8 bits: vcnn_rmsnorm_fwd_i8 with u = x and scale[r] = a[r] / 127.  For the weights [out_f][in_f] of
  * vcnn_fc_fwd_i8 (one scale per output), and for activations (one per sample). */
 vcnn_status vcnn_quant_rows_i8(int32_t dtype, int32_t rows, int32_t cols, const void* x, int8_t* q, float* scale,

@@ -1343,6 +1343,42 @@ vcnn_status vcnn_layernorm_bwd(int32_t dtype, int32_t rows, int32_t cols, float 
                               (hipStream_t)stream);
 }
 
+static vcnn_status check_fc_softmax(int32_t dtype, int32_t batch, int32_t in_f, int32_t classes) {
+  if (batch <= 0 || in_f <= 0 || classes <= 0)
+    return fail(VCNN_ERR_SHAPE, "fc_softmax_loss: non-positive dimension (batch=%d in=%d classes=%d)", batch, in_f, classes);
+  if (vcnn_status s = check_dtype(dtype, "fc_softmax_loss")) return s;
+  if (in_f > 1 << 22 || classes > 1 << 22 || (int64_t)in_f * classes > (int64_t)1 << 38)
+    return fail(VCNN_ERR_UNSUPPORTED, "fc_softmax_loss: problem too large (in=%d classes=%d)", in_f, classes);
+  return VCNN_OK;
+}
+
+vcnn_status vcnn_fc_softmax_loss_workspace_bytes(int32_t dtype, int32_t batch, int32_t in_f, int32_t classes, int32_t grads,
+                                                 size_t* bytes) {
+  if (!bytes) return fail(VCNN_ERR_NULL, "fc_softmax_loss_workspace_bytes: NULL out-parameter");
+  if (vcnn_status s = check_fc_softmax(dtype, batch, in_f, classes)) return s;
+  *bytes = dtype == VCNN_BF16 ? fc_softmax_loss_workspace(batch, in_f, classes, grads != 0)
+                              : fc_softmax_loss_workspace_f32(batch, in_f, classes, grads != 0);
+  return VCNN_OK;
+}
+
+vcnn_status vcnn_fc_softmax_loss(int32_t dtype, int32_t batch, int32_t in_f, int32_t classes, const void* x, const void* w,
+                                 const float* bias, const int32_t* labels, int32_t ignore, float* loss, float* sample_loss, void* dx,
+                                 float* dw, float* dbias, void* workspace, size_t workspace_bytes, void* stream) {
+  if (vcnn_status s = check_fc_softmax(dtype, batch, in_f, classes)) return s;
+  if (!x || !w || !labels || !loss) return fail(VCNN_ERR_NULL, "fc_softmax_loss: NULL tensor");
+  const bool grads = dx || dw || dbias;
+  if (dtype == VCNN_BF16 && in_f % 8 == 0 && (reinterpret_cast<uintptr_t>(w) & 15))
+    return fail(VCNN_ERR_UNSUPPORTED, "fc_softmax_loss: w must be 16-byte aligned");
+  const size_t least = dtype == VCNN_BF16 ? fc_softmax_loss_least_workspace(batch, in_f, classes, grads)
+                                          : fc_softmax_loss_least_workspace_f32(batch, in_f, classes, grads);
+  if (vcnn_status s = check_ws(workspace, workspace_bytes, least, "fc_softmax_loss")) return s;
+  if (dtype == VCNN_BF16)
+    return launch_fc_softmax_loss_bf16(batch, in_f, classes, x, w, bias, labels, ignore, loss, sample_loss, dx, dw, dbias, workspace,
+                                       workspace_bytes, (hipStream_t)stream);
+  return launch_fc_softmax_loss_f32(batch, in_f, classes, (const float*)x, (const float*)w, bias, labels, ignore, loss, sample_loss,
+                                    (float*)dx, dw, dbias, workspace, workspace_bytes, (hipStream_t)stream);
+}
+
 vcnn_status vcnn_quant_rows_i8(int32_t dtype, int32_t rows, int32_t cols, const void* x, int8_t* q, float* scale,
                                void* stream) {
   if (vcnn_status s = check_norm("quant_rows_i8", dtype, rows, cols)) return s;

@@ -1,0 +1,204 @@
+// A matrix product of 16-bit operands with float sums on the matrix cores, for the products of a layer with many outputs:
+//     out[b][a] = sum over k of  A(a, k) B(b, k)
+// Each operand lies in memory as rows that run along k, or as rows of k that run along a (or b): the second kind is turned round
+// on its way from LDS to the registers (ds_read_b64_tr_b16: sixteen lanes read four rows of sixteen elements, and each gets a
+// column of four), so that no transposed copy is ever written.  An operand may come in planes, a high and a low term in turn
+// for every 64 elements, and a product then runs over several pairs of planes into the same sums.
+#pragma once
+#include <type_traits>
+
+#include "bf16_core.h"
+#include "common.h"
+
+namespace vcnn {
+
+struct Operand16 {
+  const char* base;
+  int64_t pitch;  // bytes from row to row
+  int count;      // rows along k: how many; rows of k: groups of eight elements in each
+};
+
+struct ProductArgs {
+  Operand16 a, b;
+  int k;                // contraction steps (rows along k: up to the next multiple of 8 there are zeros)
+  int segments;         // pairs of planes
+  int plane_a[3], plane_b[3];
+  int tiles_a, tiles_b;
+  int slabs_per_split;  // of segments * ceil(k / 32)
+};
+
+// BA x BB outputs by waves of 16 TA x 16 TB.
+template <int BA_, int BB_, int TA_, int TB_>
+struct ProductTile {
+  static constexpr int BA = BA_, BB = BB_, TA = TA_, TB = TB_, RING = 4;
+  static constexpr int WA = BA / (16 * TA), WB = BB / (16 * TB), THREADS = WA * WB * 64;
+  static constexpr int WORDS = (BA + BB) * 4;  // 16-byte words of a slab of 32 steps
+  static constexpr size_t LDS = (size_t)RING * WORDS * 16;
+  static constexpr int LA = BA * 4 / THREADS, LB = BB * 4 / THREADS;  // words a thread brings of one
+  static_assert(TA % 2 == 0 && LA * THREADS == BA * 4 && LB * THREADS == BB * 4 && LA + LB >= 2, "whole slabs");
+};
+
+__device__ const uint4 kZeroWord = {0, 0, 0, 0};
+
+typedef short short4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) short4_t* LdsShort4;
+
+// One operand's way into LDS and from there to the registers.  R rows of the tile, THREADS threads, L words each.
+//   rows along k: word c (of four) of row r at place 4 r + (c ^ swizzle(r)): sixteen lanes of a read meet all banks (as in int8.hip)
+//   rows of k:    word c (of R / 8) of step k at place R / 8 * k + (c ^ turn(k)): a read of half a wave takes two neighbouring
+//                 words of eight steps 8 g + 0 .. 3 and 8 (g + 1) + 0 .. 3, which turn() sends to different banks
+template <bool ALONG, bool PLANES, int R, int THREADS>
+struct Way {
+  static constexpr int L = R * 4 / THREADS, WPR = R / 8;
+  static_assert(R >= 64 || ALONG, "the banks");
+  __device__ static __forceinline__ int swizzle(int r) {
+    const int h = r >> 2 & 3;
+    return h >> 1 | ((h ^ h >> 1) & 1) << 1;
+  }
+  __device__ static __forceinline__ int turn(int k) {
+    return R >= 128 ? 2 * ((k & 3) | (k >> 3 & 1) << 2) : 2 * ((k >> 1 & 1) | (k >> 3 & 1) << 1);
+  }
+
+  const char* base;
+  int64_t pitch;
+  uint32_t offset[L];
+  int step[L];  // of word i: within a slab, the first contraction step (along: of its eight)
+  __device__ __forceinline__ Way(const Operand16& o, int r0, int tid) : base(o.base), pitch(o.pitch) {
+    if constexpr (ALONG) {
+      base += (int64_t)r0 * pitch;
+#pragma unroll
+      for (int i = 0; i < L; ++i) {
+        const int r = i * (THREADS / 4) + (tid >> 2), c = (tid & 3) ^ swizzle(r);
+        offset[i] = (uint32_t)min(r, o.count - 1 - r0) * (uint32_t)pitch + c * 16;  // rows behind the last: that one again
+        step[i] = c * 8;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < L; ++i) {
+        const int p = i * THREADS + tid, k = p / WPR, c = min(r0 / 8 + ((p % WPR) ^ turn(k)), o.count - 1);
+        offset[i] = (uint32_t)k * (uint32_t)pitch + (uint32_t)(PLANES ? (c >> 3) * 256 + (c & 7) * 16 : c * 16);
+        step[i] = k;
+      }
+    }
+  }
+  // Word i of slab s (32 steps from 32 s on; `left` of them are there) of a plane, to `to` (wave-uniform).
+  __device__ __forceinline__ void stage(int i, int s, int left, int plane, uint4* to) const {
+    const char* from = base;
+    if constexpr (ALONG) from += PLANES ? (int64_t)(s >> 1) * 256 + (s & 1) * 64 : (int64_t)s * 64;
+    else from += (int64_t)s * 32 * pitch;
+    if (PLANES) from += plane * 128;
+    if (left >= 32) load_to_lds16(from, offset[i], to);
+    else load_to_lds16(step[i] < left ? reinterpret_cast<const uint4*>(from + offset[i]) : &kZeroWord, to);
+  }
+  // Row tile at r (of the tile) of the slab at buf: lane l holds row l % 16, steps 8 (l / 16) .. + 8.
+  __device__ static __forceinline__ uint4 fragment(const uint4* buf, int r, int lane) {
+    if constexpr (ALONG) {
+      return buf[r * 4 + (lane & 15) * 4 + ((lane >> 4) ^ swizzle(lane & 15))];
+    } else {
+      const int k = 8 * (lane >> 4) + (lane >> 2 & 3), c = (r / 8 + (lane >> 1 & 1)) ^ turn(k);
+      const char* const at = reinterpret_cast<const char*>(buf + k * WPR + c) + (lane & 1) * 8;
+      const short4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4)at);
+      const short4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4)(at + 4 * WPR * 16));  // (turn(k + 4) == turn(k))
+      const uint2 l = __builtin_bit_cast(uint2, lo), h = __builtin_bit_cast(uint2, hi);
+      return make_uint4(l.x, l.y, h.x, h.y);
+    }
+  }
+};
+
+// Consecutive blocks go to the eight XCDs in turn: each takes a contiguous eighth of the tiles, in patches of eight tiles of b by
+// as many of a as it comes to, so that the blocks at work share what they read in its L2.
+__device__ __forceinline__ void product_tile_of(const ProductArgs& p, int* ta, int* tb) {
+  const int total = p.tiles_a * p.tiles_b, per = total / 8, block = blockIdx.x;
+  const int item = block < per * 8 ? (block % 8) * per + block / 8 : block;
+  const int group = item / (8 * p.tiles_a), in = item - group * 8 * p.tiles_a, wide = min(8, p.tiles_b - group * 8);
+  *ta = in / wide, *tb = group * 8 + in % wide;
+}
+
+// Slabs of 32 steps go to a ring of four by direct loads, three slabs ahead; a wave reads the second half of a step's a-tiles while
+// it multiplies the first, and the first of the next step while it multiplies the second, so that neither the loads nor the barrier
+// (one a slab) leave the matrix cores without operands.  acc[i][j]: lane l has a = 16 i + 4 (l / 16) + q, b = 16 j + l % 16 of the
+// wave's part.
+template <typename TILE, bool F16, bool A_ALONG, bool A_PLANES, bool B_ALONG, bool B_PLANES>
+__device__ __forceinline__ void slab_product(const ProductArgs& p, int a0, int b0, uint4* smem,
+                                             f32x4 (&acc)[TILE::TA][TILE::TB]) {
+  constexpr int TA = TILE::TA, TB = TILE::TB, LA = TILE::LA, LB = TILE::LB, L = LA + LB, R = TILE::RING;
+  using WayA = Way<A_ALONG, A_PLANES, TILE::BA, TILE::THREADS>;
+  using WayB = Way<B_ALONG, B_PLANES, TILE::BB, TILE::THREADS>;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const WayA wa(p.a, a0, tid);
+  const WayB wb(p.b, b0, tid);
+  const int per_plane = (p.k + 31) / 32, first = blockIdx.y * p.slabs_per_split;
+  const int slabs = min(p.slabs_per_split, p.segments * per_plane - first);
+  auto stage = [&](int s, int i) {  // load i of L of slab s; behind the last: zeros
+    const int at = first + s, seg = p.segments == 1 ? 0 : (at >= per_plane) + (at >= 2 * per_plane);
+    const int slab = at - seg * per_plane, left = s < slabs ? p.k - slab * 32 : 0;
+    uint4* const to = smem + (s % R) * TILE::WORDS + i * TILE::THREADS + wave * 64;
+    if (i < LA) wa.stage(i, slab, left, A_PLANES ? p.plane_a[seg] : 0, to);
+    else wb.stage(i - LA, slab, left, B_PLANES ? p.plane_b[seg] : 0, to);
+  };
+#pragma unroll
+  for (int i = 0; i < TA; ++i)
+#pragma unroll
+    for (int j = 0; j < TB; ++j) acc[i][j] = (f32x4){0.f, 0.f, 0.f, 0.f};
+  const int ra = (wave % TILE::WA) * 16 * TA, rb = (wave / TILE::WA) * 16 * TB;
+  constexpr int H = TA / 2;
+  uint4 fa[2][H], fb[2][TB];
+  auto read_a = [&](int s, int h) {
+    const uint4* const buf = smem + (s % R) * TILE::WORDS;
+#pragma unroll
+    for (int i = 0; i < H; ++i) fa[h][i] = WayA::fragment(buf, ra + (h * H + i) * 16, lane);
+  };
+  auto read_b = [&](int s, int n) {
+    const uint4* const buf = smem + (s % R) * TILE::WORDS + TILE::BA * 4;
+#pragma unroll
+    for (int j = 0; j < TB; ++j) fb[n][j] = WayB::fragment(buf, rb + j * 16, lane);
+  };
+  // The products of half h, loads l0 .. l1 of slab s among them: a load waits its turn behind those of the other waves, and the
+  // matrix cores are not to wait with it.
+  auto multiply = [&](int h, int n, int s, int l0, int l1) {
+    const int every = H * TB / (l1 - l0);
+#pragma unroll
+    for (int m = 0; m < H * TB; ++m) {
+      const int i = m / TB, j = m % TB;
+      if constexpr (F16) acc[h * H + i][j] = mfma_f16(fa[h][i], fb[n][j], acc[h * H + i][j]);
+      else acc[h * H + i][j] = mfma_bf16(fa[h][i], fb[n][j], acc[h * H + i][j]);
+      if (m % every == every / 2 && l0 + m / every < l1) {
+        __builtin_amdgcn_sched_barrier(0);
+        stage(s, l0 + m / every);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  };
+  constexpr auto all_but = [](int n) { return 0x0F70 | (n & 15) | n >> 4 << 14; };  // vmcnt(n)
+  static_assert((R - 2) * L < 64, "the counts fit");
+#pragma unroll
+  for (int s = 0; s < R - 1; ++s)
+#pragma unroll
+    for (int i = 0; i < L; ++i) stage(s, i);
+  __builtin_amdgcn_s_waitcnt(all_but((R - 2) * L));
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  read_b(0, 0), read_a(0, 0);
+  auto step = [&](int s, int n) {
+    // slab s + 1 is there, for everyone; slab s - 1 has been read by everyone
+    __builtin_amdgcn_s_waitcnt(all_but((R - 3) * L));
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    read_a(s, 1);
+    __builtin_amdgcn_sched_barrier(0);
+    multiply(0, n, s + R - 1, 0, L / 2);
+    __builtin_amdgcn_sched_barrier(0);
+    read_b(s + 1, n ^ 1), read_a(s + 1, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    multiply(1, n, s + R - 1, L / 2, L);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  for (int s = 0; s < slabs; s += 2) {
+    step(s, 0);
+    step(s + 1, 1);
+  }
+  __builtin_amdgcn_s_waitcnt(0x0070);  // nothing more is on its way to LDS, or from it
+  __syncthreads();
+}
+
+}  // namespace vcnn

@@ -91,6 +91,9 @@ _SIGNATURES = {
     "vcnn_layernorm_bwd": (c_int32, [c_int32, c_int32, c_int32, c_float, c_void_p, c_int32, c_void_p, c_void_p, c_void_p,
                                      c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_size_t,
                                      c_void_p]),
+    "vcnn_fc_softmax_loss_workspace_bytes": (c_int32, [c_int32, c_int32, c_int32, c_int32, c_int32, POINTER(c_size_t)]),
+    "vcnn_fc_softmax_loss": (c_int32, [c_int32, c_int32, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_void_p, c_int32,
+                                       c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
     "vcnn_quant_rows_i8": (c_int32, [c_int32, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_void_p]),
     "vcnn_fc_i8_workspace_bytes": (c_int32, [c_int32, c_int32, c_int32, POINTER(c_size_t)]),
     "vcnn_fc_fwd_i8": (c_int32, [c_int32, c_int32, c_int32, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_void_p,
@@ -373,6 +376,19 @@ def layernorm_bwd(dtype, rows, cols, p, rng, site, h, gain, mean, rstd, dy, dh_a
     w, nbytes = _ws(workspace)
     _check(lib().vcnn_layernorm_bwd(dtype, rows, cols, p, _ptr(rng), site, _ptr(h), _ptr(gain), _ptr(mean), _ptr(rstd), _ptr(dy),
                                     _ptr(dh_above), _ptr(dh), _ptr(dx), _ptr(dgain), _ptr(dbias), w, nbytes, _stream(stream)))
+
+
+def fc_softmax_loss_workspace_bytes(dtype, batch, in_f, classes, grads) -> int:
+    b = c_size_t()
+    _check(lib().vcnn_fc_softmax_loss_workspace_bytes(dtype, batch, in_f, classes, int(grads), byref(b)))
+    return b.value
+
+
+def fc_softmax_loss(dtype, batch, in_f, classes, x, w, bias, labels, ignore, loss, sample_loss, dx, dw, dbias, workspace,
+                    stream=None):
+    p, nbytes = _ws(workspace)
+    _check(lib().vcnn_fc_softmax_loss(dtype, batch, in_f, classes, _ptr(x), _ptr(w), _ptr(bias), _ptr(labels), ignore, _ptr(loss),
+                                      _ptr(sample_loss), _ptr(dx), _ptr(dw), _ptr(dbias), p, nbytes, _stream(stream)))
 
 
 def quant_rows_i8(dtype, rows, cols, x, q, scale, stream=None):

@@ -1356,8 +1356,7 @@ vcnn_status vcnn_fc_softmax_loss_workspace_bytes(int32_t dtype, int32_t batch, i
                                                  size_t* bytes) {
   if (!bytes) return fail(VCNN_ERR_NULL, "fc_softmax_loss_workspace_bytes: NULL out-parameter");
   if (vcnn_status s = check_fc_softmax(dtype, batch, in_f, classes)) return s;
-  *bytes = dtype == VCNN_BF16 ? fc_softmax_loss_workspace(batch, in_f, classes, grads != 0)
-                              : fc_softmax_loss_workspace_f32(batch, in_f, classes, grads != 0);
+  *bytes = fc_softmax_loss_workspace(dtype, batch, in_f, classes, grads != 0);
   return VCNN_OK;
 }
 
@@ -1369,14 +1368,10 @@ vcnn_status vcnn_fc_softmax_loss(int32_t dtype, int32_t batch, int32_t in_f, int
   const bool grads = dx || dw || dbias;
   if (dtype == VCNN_BF16 && in_f % 8 == 0 && (reinterpret_cast<uintptr_t>(w) & 15))
     return fail(VCNN_ERR_UNSUPPORTED, "fc_softmax_loss: w must be 16-byte aligned");
-  const size_t least = dtype == VCNN_BF16 ? fc_softmax_loss_least_workspace(batch, in_f, classes, grads)
-                                          : fc_softmax_loss_least_workspace_f32(batch, in_f, classes, grads);
-  if (vcnn_status s = check_ws(workspace, workspace_bytes, least, "fc_softmax_loss")) return s;
-  if (dtype == VCNN_BF16)
-    return launch_fc_softmax_loss_bf16(batch, in_f, classes, x, w, bias, labels, ignore, loss, sample_loss, dx, dw, dbias, workspace,
-                                       workspace_bytes, (hipStream_t)stream);
-  return launch_fc_softmax_loss_f32(batch, in_f, classes, (const float*)x, (const float*)w, bias, labels, ignore, loss, sample_loss,
-                                    (float*)dx, dw, dbias, workspace, workspace_bytes, (hipStream_t)stream);
+  if (vcnn_status s = check_ws(workspace, workspace_bytes, fc_softmax_loss_least_workspace(dtype, batch, in_f, classes, grads), "fc_softmax_loss"))
+    return s;
+  return launch_fc_softmax_loss(dtype, batch, in_f, classes, x, w, bias, labels, ignore, loss, sample_loss, dx, dw, dbias, workspace,
+                                workspace_bytes, (hipStream_t)stream);
 }
 
 vcnn_status vcnn_quant_rows_i8(int32_t dtype, int32_t rows, int32_t cols, const void* x, int8_t* q, float* scale,

@@ -490,16 +490,11 @@ size_t rmsnorm_bwd_partial_bytes(int rows, int cols);
 vcnn_status launch_rmsnorm_bwd(int dtype, int rows, int cols, const void* h, const float* gain, const float* rstd,
                                const void* dy, const void* above, void* dh, float* dgain, float* partial, hipStream_t st);
 // fc_softmax.hip: with gradients (any of dx, dw, dbias) or without
-size_t fc_softmax_loss_workspace(int batch, int in_f, int classes, bool grads);
-size_t fc_softmax_loss_least_workspace(int batch, int in_f, int classes, bool grads);
-size_t fc_softmax_loss_workspace_f32(int batch, int in_f, int classes, bool grads);
-size_t fc_softmax_loss_least_workspace_f32(int batch, int in_f, int classes, bool grads);
-vcnn_status launch_fc_softmax_loss_bf16(int batch, int in_f, int classes, const void* x, const void* w, const float* bias,
-                                        const int32_t* labels, int ignore, float* loss, float* sample_loss, void* dx, float* dw,
-                                        float* dbias, void* workspace, size_t bytes, hipStream_t st);
-vcnn_status launch_fc_softmax_loss_f32(int batch, int in_f, int classes, const float* x, const float* w, const float* bias,
-                                       const int32_t* labels, int ignore, float* loss, float* sample_loss, float* dx, float* dw,
-                                       float* dbias, void* workspace, size_t bytes, hipStream_t st);
+size_t fc_softmax_loss_workspace(int dtype, int batch, int in_f, int classes, bool grads);
+size_t fc_softmax_loss_least_workspace(int dtype, int batch, int in_f, int classes, bool grads);
+vcnn_status launch_fc_softmax_loss(int dtype, int batch, int in_f, int classes, const void* x, const void* w, const float* bias,
+                                   const int32_t* labels, int ignore, float* loss, float* sample_loss, void* dx, float* dw,
+                                   float* dbias, void* workspace, size_t bytes, hipStream_t st);
 // dropout.hip, layernorm.hip
 struct Dropout;
 vcnn_status launch_dropout(int dtype, int rows, int cols, const Dropout& drop, const void* x, const void* residual, void* y,

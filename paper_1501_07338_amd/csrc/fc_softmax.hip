@@ -7,6 +7,11 @@
 // and a low bfloat16 term of the difference, and two products make dx and dw from it.  Without gradients z is not stored at all.
 //   d in two terms: dw is float, and one bfloat16 term alone would leave 2^-9 of each element in it (the two leave 2^-18).  dx is
 //   bfloat16 itself and takes the high term alone.
+//   float: x, w and d in two half-precision terms each (22 bits), products high x high, high x low and low x high, three
+//   where the float instruction would take sixteen.  x and w are scaled by a power of two a row so that its largest element comes to
+//   2^14 .. 2^15, but by at most 2^8 more than the row with the largest element of all, and d by 2^14 and the inverse of what its
+//   sample's and its class's rows were scaled by beyond that.  What falls below 2^-24 in half precision is lost: 2^-39 of a row's
+//   largest element, and 2^-39 of 1 in an element of d, 2^-23 at the worst (where a float keeps 2^-24 of p - 1).
 #include <algorithm>
 
 #include "rows.h"
@@ -16,31 +21,36 @@ namespace vcnn {
 
 static constexpr int kThreads = 256;
 
-struct LossMeta {  // at the head of the workspace
-  float inverse;   // 1 / C, 0 if no sample counts
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+
+struct LossMeta {     // at the head of the workspace
+  float inverse;      // 1 / C, 0 if no sample counts
+  uint32_t most[2];   // float: the largest finite magnitude in this part's x, and in w (as bits)
 };
 
 // ---- operands ----------------------------------------------------------------------------------------------------------
+// How many samples count (before the first part), and no largest magnitude yet (x before each).
+__global__ __launch_bounds__(1024) void loss_meta_kernel(const int32_t* labels, int batch, int ignore, int first, LossMeta* meta) {
+  __shared__ int counts[16];
+  if (threadIdx.x == 0) meta->most[0] = 0;
+  if (!first) return;
+  int n = 0;
+  for (int b = threadIdx.x; b < batch; b += 1024) n += labels[b] != ignore;
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) n += __shfl_xor(n, d);
+  if ((threadIdx.x & 63) == 0) counts[threadIdx.x >> 6] = n;
+  __syncthreads();
+  if (threadIdx.x > 0) return;
+  n = 0;
+  for (int w = 0; w < 16; ++w) n += counts[w];
+  meta->inverse = n ? 1.f / (float)n : 0.f, meta->most[1] = 0;
+}
+
 // Rows re-laid with a length of whole groups of eight, the rows of samples that do not count as zeros (whatever they hold must
-// not meet the zeros of d as a NaN).  Block 0 of the first part counts the samples.
+// not meet the zeros of d as a NaN).
 template <typename T>
 __global__ __launch_bounds__(kThreads) void relay_rows_kernel(const T* x, T* to, int64_t rows, int cols, int groups,
-                                                              const int32_t* labels, int ignore, const int32_t* all_labels,
-                                                              int batch, LossMeta* meta) {
-  if (meta && blockIdx.x == 0) {
-    __shared__ int counts[kThreads / 64];
-    int n = 0;
-    for (int b = threadIdx.x; b < batch; b += kThreads) n += all_labels[b] != ignore;
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) n += __shfl_xor(n, d);
-    if ((threadIdx.x & 63) == 0) counts[threadIdx.x >> 6] = n;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      n = 0;
-      for (int w = 0; w < kThreads / 64; ++w) n += counts[w];
-      meta->inverse = n ? 1.f / (float)n : 0.f;
-    }
-  }
+                                                              const int32_t* labels, int ignore) {
   for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < rows * groups; i += (int64_t)gridDim.x * kThreads) {
     const int64_t row = i / groups;
     const int c = (int)(i - row * groups) * 8;
@@ -49,6 +59,87 @@ __global__ __launch_bounds__(kThreads) void relay_rows_kernel(const T* x, T* to,
     *reinterpret_cast<uint4*>(to + i * 8) = make_uint4(v.w[0], v.w[1], v.w[2], v.w[3]);
   }
 }
+
+// Float: the largest finite magnitude of each row (a wave a row) and of all.  Rows of samples that do not count are not looked at.
+__global__ __launch_bounds__(kThreads) void row_most_kernel(const float* x, int64_t rows, int cols, const int32_t* labels, int ignore,
+                                                            uint32_t* row_most, uint32_t* most) {
+  const int lane = threadIdx.x & 63;
+  uint32_t all = 0;
+  for (int64_t row = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6); row < rows; row += (int64_t)gridDim.x * (kThreads / 64)) {
+    uint32_t m = 0;
+    if (!labels || labels[row] != ignore) {
+#pragma unroll 4
+      for (int c = lane * 4; c < cols; c += 256) {
+        const Loose16 v = load_group(x + row * cols, c, cols);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t bits = v.w[i] & 0x7fffffffu;
+          m = max(m, bits < 0x7f800000u ? bits : 0u);
+        }
+      }
+    }
+    m = wave_max(m);
+    if (lane == 0) row_most[row] = m;
+    all = max(all, m);
+  }
+  if (lane == 0 && all) atomicMax(most, all);  // (whatever the order, the same)
+}
+
+// The power of two that brings the largest of all, `bits`, to 2^14 .. 2^15 (kept to where it and its inverse are floats).
+__device__ __forceinline__ int least_power(uint32_t bits) {
+  return bits ? max(-110, min(110, 14 + 127 - (int)max(1u, bits >> 23))) : 0;
+}
+__device__ __forceinline__ float power2(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
+
+__device__ __forceinline__ void split_f16(float v, _Float16* hi, _Float16* lo) {
+  *hi = (_Float16)v;
+  *lo = (_Float16)(v - (float)*hi);
+}
+
+// Rows in two terms: 64 high ones, 64 low ones in turn, zeros behind the row's end; row_most becomes the 2^-(0 .. 8) by which a row
+// is scaled more than the least.
+__global__ __launch_bounds__(kThreads) void relay_planes_kernel(const float* x, char* to, int64_t rows, int cols, int groups,
+                                                                const int32_t* labels, int ignore, float* down, const uint32_t* most) {
+  const uint32_t top = *most;
+  const int least = least_power(top), lane = threadIdx.x & 63;
+  for (int64_t row = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6); row < rows; row += (int64_t)gridDim.x * (kThreads / 64)) {
+    const uint32_t bits = __builtin_amdgcn_readfirstlane(__float_as_uint(down[row]));  // (every lane has read it before lane 0 writes)
+    const int more = bits ? min(8, (int)max(1u, top >> 23) - (int)max(1u, bits >> 23)) : 8;
+    if (lane == 0) down[row] = power2(-more);
+    const float scale = power2(least + more);
+    const bool counts = !labels || labels[row] != ignore;
+    for (int g = lane; g < groups; g += 64) {
+      const int c = g * 8;
+      float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      if (counts) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          if (c + 4 * h < cols) {
+            const Loose16 q = load_group(x + row * cols, c + 4 * h, cols);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[4 * h + i] = __uint_as_float(q.w[i]) * scale;
+          }
+      }
+      f16x8 hi, lo;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        _Float16 a, b;
+        split_f16(v[i], &a, &b);
+        hi[i] = a, lo[i] = b;
+      }
+      char* const at = to + (row * (groups >> 3) + (g >> 3)) * 256 + (g & 7) * 16;
+      *reinterpret_cast<f16x8*>(at) = hi;
+      *reinterpret_cast<f16x8*>(at + 128) = lo;
+    }
+  }
+}
+
+// Logits are compared and summed as powers of two: 2^(z log2 e - m), with log2 e in two terms, so that the rounding of the constant
+// (1.3e-8 of z) is not seen.  The instruction is off by one unit in the last place.
+__device__ __forceinline__ float log2e_times_less(float z, float m) {
+  return fmaf(z, 1.925963033e-8f, fmaf(z, 1.442695022f, -m));
+}
+__device__ __forceinline__ float exp2_of(float t) { return __builtin_amdgcn_exp2f(t); }
 
 // ---- products ------------------------------------------------------------------------------------------------------------
 enum { EPI_LOGITS = 0, EPI_DX = 1, EPI_DW = 2 };
@@ -61,14 +152,20 @@ struct LossProduct {
   int64_t z_pitch;
   const float* bias;     // nullable
   const int32_t* labels;
-  float2* stats;         // [16 TA of classes][rows]: the largest logit, the sum of exponentials about it
+  float2* stats;         // [16 TA of classes][rows]: the largest logit times log2 e, the sum of powers about it
   float* at_label;
   // EPI_DX, EPI_DW
   const LossMeta* meta;
   float* partial;        // [splits][rows][cols] (EPI_DX, shared sums)
   void* out;             // [rows][cols]
   int add;               // EPI_DW: to what is there
+  // float: by how much the rows of a and b (EPI_LOGITS), or that of b, were scaled beyond the least
+  const float* down_a;
+  const float* down_b;
 };
+
+// 2^k of 2^-k.
+__device__ __forceinline__ float inverse_power(float p) { return __uint_as_float(0x7f000000u - __float_as_uint(p)); }
 
 template <typename T>
 __device__ __forceinline__ void store4(T* at, const float (&v)[4], int n) {
@@ -90,17 +187,31 @@ __device__ __forceinline__ void store4(T* at, const float (&v)[4], int n) {
   }
 }
 
-template <typename TILE, int EPI, bool A_ALONG, bool B_ALONG, bool B_PLANES>
-__global__ __launch_bounds__(TILE::THREADS, 2) void loss_product_kernel(LossProduct a) {
+template <typename TILE, int EPI, bool F32, bool A_ALONG, bool B_ALONG, bool B_PLANES>
+__global__ __launch_bounds__(TILE::THREADS, TILE::WAVES_SIMD) void loss_product_kernel(LossProduct a) {
   extern __shared__ uint4 smem16[];
   int ta, tb;
   product_tile_of(a.p, &ta, &tb);
   f32x4 acc[TILE::TA][TILE::TB];
-  slab_product<TILE, false, A_ALONG, false, B_ALONG, B_PLANES>(a.p, ta * TILE::BA, tb * TILE::BB, smem16, acc);
+  slab_product<TILE, F32, A_ALONG, F32, B_ALONG, B_PLANES>(a.p, ta * TILE::BA, tb * TILE::BB, smem16, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int a0 = ta * TILE::BA + (wave % TILE::WA) * 16 * TILE::TA, b0 = tb * TILE::BB + (wave / TILE::WA) * 16 * TILE::TB;
   const int ca = a0 + 4 * (lane >> 4);  // + 16 i + q
   if constexpr (EPI == EPI_LOGITS) {
+    if constexpr (F32) {
+      const float sa = power2(-least_power(a.meta->most[1])), sb = power2(-least_power(a.meta->most[0]));
+      float db[TILE::TB];
+#pragma unroll
+      for (int j = 0; j < TILE::TB; ++j) db[j] = a.down_b[min(b0 + 16 * j + (lane & 15), a.rows - 1)];
+#pragma unroll
+      for (int i = 0; i < TILE::TA; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const float da = a.down_a[min(ca + 16 * i + q, a.cols - 1)] * sa;
+#pragma unroll
+          for (int j = 0; j < TILE::TB; ++j) acc[i][j][q] = acc[i][j][q] * da * (db[j] * sb);
+        }
+    }
 #pragma unroll
     for (int i = 0; i < TILE::TA; ++i) {
       float bias[4] = {0.f, 0.f, 0.f, 0.f};
@@ -125,12 +236,13 @@ __global__ __launch_bounds__(TILE::THREADS, 2) void loss_product_kernel(LossProd
           if (ca + 16 * i + q < a.cols) most = fmaxf(most, acc[i][j][q]);
       most = fmaxf(most, __shfl_xor(most, 16));
       most = fmaxf(most, __shfl_xor(most, 32));
+      most = log2e_times_less(most, 0.f);
       if (most > -__builtin_inff()) {  // (none of these classes is possible: their sum is 0)
 #pragma unroll
         for (int i = 0; i < TILE::TA; ++i)
 #pragma unroll
           for (int q = 0; q < 4; ++q)
-            if (ca + 16 * i + q < a.cols) sum += expf(acc[i][j][q] - most);
+            if (ca + 16 * i + q < a.cols) sum += exp2_of(log2e_times_less(acc[i][j][q], most));
       } else {  // (or all are NaN)
 #pragma unroll
         for (int i = 0; i < TILE::TA; ++i)
@@ -153,10 +265,12 @@ __global__ __launch_bounds__(TILE::THREADS, 2) void loss_product_kernel(LossProd
     }
   } else {
     const float inverse = a.meta->inverse;
+    const float least = F32 ? power2(-14 - least_power(a.meta->most[EPI == EPI_DX ? 1 : 0])) : 1.f;
 #pragma unroll
     for (int j = 0; j < TILE::TB; ++j) {
       const int b = b0 + 16 * j + (lane & 15);
       if (b >= a.rows) continue;
+      const float up = F32 ? inverse_power(a.down_b[b]) : 1.f;
 #pragma unroll
       for (int i = 0; i < TILE::TA; ++i) {
         const int c = ca + 16 * i, n = a.cols - c;
@@ -165,14 +279,14 @@ __global__ __launch_bounds__(TILE::THREADS, 2) void loss_product_kernel(LossProd
         float v[4];
         if (EPI == EPI_DX && a.partial) {
 #pragma unroll
-          for (int q = 0; q < 4; ++q) v[q] = acc[i][j][q];
+          for (int q = 0; q < 4; ++q) v[q] = F32 ? acc[i][j][q] * least * up : acc[i][j][q];
           store4(a.partial + (int64_t)blockIdx.y * a.rows * a.cols + at, v, n);
           continue;
         }
 #pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] = acc[i][j][q] * inverse;
+        for (int q = 0; q < 4; ++q) v[q] = (F32 ? acc[i][j][q] * least * up : acc[i][j][q]) * inverse;
         if constexpr (EPI == EPI_DX) {
-          store4(reinterpret_cast<bf16*>(a.out) + at, v, n);
+          store4(reinterpret_cast<std::conditional_t<F32, float, bf16>*>(a.out) + at, v, n);
         } else {
           float* const out = reinterpret_cast<float*>(a.out) + at;
           if (a.add) {
@@ -188,8 +302,9 @@ __global__ __launch_bounds__(TILE::THREADS, 2) void loss_product_kernel(LossProd
 }
 
 // dx from the shares of its sums, always in the same order.
+template <typename T>
 __global__ __launch_bounds__(kThreads) void loss_join_kernel(const float* partial, int splits, int64_t count, const LossMeta* meta,
-                                                             bf16* out) {
+                                                             T* out) {
   const int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * 4;
   if (i >= count) return;
   const float inverse = meta->inverse;
@@ -205,7 +320,7 @@ __global__ __launch_bounds__(kThreads) void loss_join_kernel(const float* partia
 }
 
 // ---- softmax -------------------------------------------------------------------------------------------------------------
-// lse of sixteen samples from the tiles' maxima and sums, sixteen threads each, joined in a fixed order; what each sample costs.
+// lse (times log2 e) of sixteen samples from the tiles' maxima and sums, sixteen threads each, joined in a fixed order; what each sample costs.
 __global__ __launch_bounds__(kThreads) void loss_rows_kernel(const float2* stats, int tiles, int rows, int classes,
                                                              const int32_t* labels, int ignore, const float* at_label, float* lse,
                                                              float* each) {
@@ -214,7 +329,7 @@ __global__ __launch_bounds__(kThreads) void loss_rows_kernel(const float2* stats
   float most = -__builtin_inff(), sum = 0.f;
   auto meet = [&](float m, float s) {
     const float top = fmaxf(most, m);
-    if (top > -__builtin_inff()) sum = sum * expf(most - top) + s * expf(m - top);
+    if (top > -__builtin_inff()) sum = sum * exp2_of(most - top) + s * exp2_of(m - top);
     else sum += s;  // (nothing yet, or a NaN)
     most = top;
   };
@@ -229,19 +344,26 @@ __global__ __launch_bounds__(kThreads) void loss_rows_kernel(const float2* stats
   __syncthreads();
   if (part > 0 || b >= rows) return;
   for (int p = 1; p < 16; ++p) meet(parts[p][in].x, parts[p][in].y);
-  const float l = most + logf(sum);
+  const float l = most + log2f(sum);
   const int label = labels[b];
-  if (lse) lse[b] = l;
-  each[b] = label == ignore ? 0.f : label < 0 || label >= classes ? __builtin_nanf("") : l - at_label[b];
+  lse[b] = l;
+  each[b] = label == ignore ? 0.f : label < 0 || label >= classes ? __builtin_nanf("")
+                                                                  : -0.693147180559945f * log2e_times_less(at_label[b], l);
 }
 
 // z to d where it stands: 64 floats of a row become 64 high and 64 low terms (the sixteen lanes that read them are of one wave, which
 // has them all before it writes); behind the last class zeros.  Each block leaves its samples' share of dbias.
+template <bool F32>
 __global__ __launch_bounds__(kThreads) void loss_grad_kernel(float* z, int64_t pitch, int rows, int classes, const int32_t* labels,
-                                                             int ignore, const float* lse, float* shares, int64_t share_pitch) {
+                                                             int ignore, const float* lse, const float* down_x, const float* down_w,
+                                                             float* shares, int64_t share_pitch) {
   __shared__ float sums[16][64];
   const int in = threadIdx.x & 15, part = threadIdx.x >> 4, c = blockIdx.x * 64 + in * 4;
-  float total[4] = {0.f, 0.f, 0.f, 0.f};
+  float total[4] = {0.f, 0.f, 0.f, 0.f}, scale[4];
+  if constexpr (F32) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) scale[q] = 0x1p14f * down_w[min(c + q, classes - 1)];
+  }
 #pragma unroll
   for (int n = 0; n < 4; ++n) {
     const int b = blockIdx.y * 64 + n * 16 + part;
@@ -251,24 +373,38 @@ __global__ __launch_bounds__(kThreads) void loss_grad_kernel(float* z, int64_t p
     const float l = lse[b];
     char* const row = reinterpret_cast<char*>(z + b * pitch);
     const float4 v = *reinterpret_cast<const float4*>(row + c * 4);
-    float d[4] = {v.x, v.y, v.z, v.w}, low[4];
-    bf16x2 h[2], r[2];
+    float d[4] = {v.x, v.y, v.z, v.w};
+    uint2 h, r;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      d[q] = expf(d[q] - l) - (c + q == label ? 1.f : 0.f);
+      d[q] = exp2_of(log2e_times_less(d[q], l)) - (c + q == label ? 1.f : 0.f);
       if (bad) d[q] = __builtin_nanf("");
       if (!counts || c + q >= classes) d[q] = 0.f;
       total[q] += d[q];
     }
+    if constexpr (F32) {
+      const float down = down_x[b];
+      f16x4 hi, lo;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      h[i] = __builtin_convertvector((f32x2){d[2 * i], d[2 * i + 1]}, bf16x2);
-      low[2 * i] = d[2 * i] - (float)h[i][0], low[2 * i + 1] = d[2 * i + 1] - (float)h[i][1];
-      r[i] = __builtin_convertvector((f32x2){low[2 * i], low[2 * i + 1]}, bf16x2);
+      for (int q = 0; q < 4; ++q) {
+        _Float16 e, f;
+        split_f16(d[q] * scale[q] * down, &e, &f);
+        hi[q] = e, lo[q] = f;
+      }
+      h = __builtin_bit_cast(uint2, hi), r = __builtin_bit_cast(uint2, lo);
+    } else {
+      bf16x2 hi[2], lo[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        hi[i] = __builtin_convertvector((f32x2){d[2 * i], d[2 * i + 1]}, bf16x2);
+        lo[i] = __builtin_convertvector((f32x2){d[2 * i] - (float)hi[i][0], d[2 * i + 1] - (float)hi[i][1]}, bf16x2);
+      }
+      h = make_uint2(__builtin_bit_cast(uint32_t, hi[0]), __builtin_bit_cast(uint32_t, hi[1]));
+      r = make_uint2(__builtin_bit_cast(uint32_t, lo[0]), __builtin_bit_cast(uint32_t, lo[1]));
     }
     char* const to = row + (int64_t)blockIdx.x * 256 + in * 8;
-    *reinterpret_cast<uint2*>(to) = make_uint2(__builtin_bit_cast(uint32_t, h[0]), __builtin_bit_cast(uint32_t, h[1]));
-    *reinterpret_cast<uint2*>(to + 128) = make_uint2(__builtin_bit_cast(uint32_t, r[0]), __builtin_bit_cast(uint32_t, r[1]));
+    *reinterpret_cast<uint2*>(to) = h;
+    *reinterpret_cast<uint2*>(to + 128) = r;
   }
   if (!shares) return;
 #pragma unroll
@@ -312,35 +448,43 @@ __global__ __launch_bounds__(1024) void loss_mean_kernel(const float* each, cons
 }
 
 // ---- plan ----------------------------------------------------------------------------------------------------------------
-using TileLarge = ProductTile<256, 256, 8, 4>;
-using TileSmall = ProductTile<128, 128, 4, 4>;
+// One plane of each; d in two; both in two.  256 x 256 of the first and 256 x 128 of the others are what the registers of eight waves
+// and a ring in LDS that stays ahead of the memory allow.
+using TileLarge = ProductTile<256, 256, 8, 4, 1, 1, 4>;
+using TileSmall = ProductTile<128, 128, 4, 4, 1, 1, 4>;
+using TileTwo = ProductTile<256, 128, 8, 2, 1, 2, 5>;
+using TileTwoSmall = ProductTile<128, 128, 4, 4, 1, 2, 3>;
+using TileFloat = ProductTile<256, 128, 4, 4, 2, 2, 3>;
 
 struct LossPlan {
   int part;            // samples at once
   int classes_pitch;   // elements of a row of z
-  int groups;          // of eight inputs, of a row
+  int groups;          // of eight inputs, of a row as it is relaid
+  int64_t x_pitch;     // bytes of such a row
   int stat_tiles;      // of classes
-  bool relay_w;
+  bool f32, relay_w;
   int splits, slabs_per_split;  // of dx
   int tile_z, tile_dx, tile_dw;
-  size_t x, w, stats, at_label, lse, each, z, partial, shares, bytes;  // places in the workspace
+  size_t x, w, down_x, down_w, stats, at_label, lse, each, z, partial, shares, bytes;  // places in the workspace
 };
 
 static constexpr int kMostSamples = 1 << 20;  // of a part
 
 static int tile_of(int64_t a, int64_t b) { return ceil_div(a, 256) * ceil_div(b, 256) >= 192 ? 256 : 128; }
 
-static LossPlan loss_plan(int part, int batch, int in_f, int classes, bool grads) {
+static LossPlan loss_plan(bool f32, int part, int batch, int in_f, int classes, bool grads) {
   LossPlan p{};
-  p.part = part;
+  p.f32 = f32, p.part = part;
   p.classes_pitch = (int)ceil_div(classes, 64) * 64;
-  p.groups = (int)ceil_div(in_f, 8);
-  p.relay_w = in_f % 8 != 0;
+  p.groups = f32 ? (int)ceil_div(in_f, 64) * 8 : (int)ceil_div(in_f, 8);
+  p.x_pitch = (int64_t)p.groups * (f32 ? 32 : 16);
+  p.relay_w = f32 || in_f % 8 != 0;
   p.tile_z = tile_of(classes, part), p.tile_dx = tile_of(in_f, part), p.tile_dw = tile_of(in_f, classes);
-  p.stat_tiles = (int)ceil_div(classes, p.tile_z == 256 ? 16 * TileLarge::TA : 16 * TileSmall::TA);
+  p.stat_tiles = (int)ceil_div(classes, 16 * (f32 ? TileFloat::TA : p.tile_z == 256 ? TileLarge::TA : TileSmall::TA));
   const int slabs = (int)ceil_div(classes, 32);
   p.splits = 1, p.slabs_per_split = slabs;
-  const int64_t tiles = ceil_div(in_f, p.tile_dx) * ceil_div(part, p.tile_dx), room = p.tile_dx == 256 ? 256 : 512;
+  const int64_t tiles = f32 ? ceil_div(in_f, TileFloat::BA) * ceil_div(part, TileFloat::BB) : ceil_div(in_f, p.tile_dx) * ceil_div(part, p.tile_dx);
+  const int64_t room = f32 || p.tile_dx == 256 ? 256 : 512;
   if (tiles * 2 <= room) {
     const int want = (int)std::min<int64_t>(room / tiles, std::max(1, slabs / 16));
     p.slabs_per_split = (int)ceil_div(slabs, want), p.splits = (int)ceil_div(slabs, p.slabs_per_split);
@@ -351,8 +495,9 @@ static LossPlan loss_plan(int part, int batch, int in_f, int classes, bool grads
     at += (bytes + 255) & ~(size_t)255;
     return here;
   };
-  p.x = take((size_t)part * p.groups * 16);
-  p.w = take(p.relay_w ? (size_t)classes * p.groups * 16 : 0);
+  p.x = take((size_t)part * p.x_pitch);
+  p.w = take(p.relay_w ? (size_t)classes * p.x_pitch : 0);
+  p.down_x = take(f32 ? (size_t)part * 4 : 0), p.down_w = take(f32 ? (size_t)classes * 4 : 0);
   p.stats = take((size_t)p.stat_tiles * part * 8);
   p.at_label = take((size_t)part * 4), p.lse = take((size_t)part * 4), p.each = take((size_t)batch * 4);
   if (grads) {
@@ -365,109 +510,112 @@ static LossPlan loss_plan(int part, int batch, int in_f, int classes, bool grads
 }
 
 // The samples in equal parts of whole tiles, the fewest that keep a part's logits (without gradients: its statistics) within `most`.
-static LossPlan loss_plan_within(size_t most, int batch, int in_f, int classes, bool grads) {
-  const LossPlan one = loss_plan(64, 64, in_f, classes, grads);
-  const size_t row = (size_t)one.groups * 16 + (grads ? (size_t)one.classes_pitch * 4 : (size_t)one.stat_tiles * 8);
+static LossPlan loss_plan_within(bool f32, size_t most, int batch, int in_f, int classes, bool grads) {
+  const LossPlan one = loss_plan(f32, 64, 64, in_f, classes, grads);
+  const size_t row = grads ? (size_t)one.classes_pitch * 4 : (size_t)one.x_pitch + (size_t)one.stat_tiles * 8;
   const int64_t fit = std::max<int64_t>(64, std::min<int64_t>((int64_t)(most / row), kMostSamples) / 64 * 64), parts = ceil_div(batch, fit);
   int64_t part = ceil_div(batch, parts);
   if (parts > 1) part = std::min(fit, ceil_div(part, part > 256 ? 256 : 64) * (part > 256 ? 256 : 64));
-  return loss_plan((int)part, batch, in_f, classes, grads);
+  return loss_plan(f32, (int)part, batch, in_f, classes, grads);
 }
+static constexpr size_t kMostLogits = (size_t)1 << 30;  // bytes of a part's
 
-size_t fc_softmax_loss_workspace(int batch, int in_f, int classes, bool grads) {
-  return loss_plan_within((size_t)1 << 30, batch, in_f, classes, grads).bytes;
-}
-size_t fc_softmax_loss_least_workspace(int batch, int in_f, int classes, bool grads) {
-  return std::min(loss_plan(std::min(batch, 64), batch, in_f, classes, grads).bytes, fc_softmax_loss_workspace(batch, in_f, classes, grads));
-}
-
-template <typename TILE, int EPI, bool A_ALONG, bool B_ALONG, bool B_PLANES>
+template <typename TILE, int EPI, bool F32, bool A_ALONG, bool B_ALONG, bool B_PLANES>
 static vcnn_status launch_product(LossProduct a, int splits, hipStream_t st) {
   a.p.tiles_a = (int)ceil_div(a.cols, TILE::BA), a.p.tiles_b = (int)ceil_div(a.rows, TILE::BB);
-  const auto kernel = loss_product_kernel<TILE, EPI, A_ALONG, B_ALONG, B_PLANES>;
+  const auto kernel = loss_product_kernel<TILE, EPI, F32, A_ALONG, B_ALONG, B_PLANES>;
   (void)hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)TILE::LDS);
   hipLaunchKernelGGL(kernel, dim3((unsigned)(a.p.tiles_a * a.p.tiles_b), (unsigned)splits), dim3(TILE::THREADS), TILE::LDS, st, a);
   return check_launch("fc_softmax_loss product");
 }
-template <int EPI, bool A_ALONG, bool B_ALONG, bool B_PLANES>
-static vcnn_status launch_product(int tile, const LossProduct& a, int splits, hipStream_t st) {
-  return tile == 256 ? launch_product<TileLarge, EPI, A_ALONG, B_ALONG, B_PLANES>(a, splits, st)
-                     : launch_product<TileSmall, EPI, A_ALONG, B_ALONG, B_PLANES>(a, splits, st);
+// A_ALONG, B_ALONG: how the operands lie.  Of d both planes are read for dw, and in float all planes of all.
+template <int EPI, bool A_ALONG, bool B_ALONG>
+static vcnn_status launch_product(bool f32, int tile, const LossProduct& a, int splits, hipStream_t st) {
+  if (f32) return launch_product<TileFloat, EPI, true, A_ALONG, B_ALONG, true>(a, splits, st);
+  using Large = std::conditional_t<EPI == EPI_DW, TileTwo, TileLarge>;
+  using Small = std::conditional_t<EPI == EPI_DW, TileTwoSmall, TileSmall>;
+  return tile == 256 ? launch_product<Large, EPI, false, A_ALONG, B_ALONG, EPI != EPI_LOGITS>(a, splits, st)
+                     : launch_product<Small, EPI, false, A_ALONG, B_ALONG, EPI != EPI_LOGITS>(a, splits, st);
 }
 
-template <typename T>
-static vcnn_status relay(const T* x, T* to, int64_t rows, int cols, int groups, const int32_t* labels, int ignore,
-                         const int32_t* all_labels, int batch, LossMeta* meta, hipStream_t st) {
-  const int64_t blocks = std::min<int64_t>(ceil_div(rows * groups, kThreads), 256 * 16);
-  hipLaunchKernelGGL(relay_rows_kernel<T>, dim3((unsigned)blocks), dim3(kThreads), 0, st, x, to, rows, cols, groups, labels, ignore,
-                     all_labels, batch, meta);
+// x or w of T as the products read it.
+static vcnn_status relay(const bf16* x, char* to, const LossPlan& p, int64_t rows, int cols, const int32_t* labels, int ignore, float*,
+                         const uint32_t*, hipStream_t st) {
+  hipLaunchKernelGGL(relay_rows_kernel<bf16>, dim3((unsigned)std::min<int64_t>(ceil_div(rows * p.groups, kThreads), 256 * 16)),
+                     dim3(kThreads), 0, st, x, (bf16*)to, rows, cols, p.groups, labels, ignore);
+  return check_launch("fc_softmax_loss relay");
+}
+static vcnn_status relay(const float* x, char* to, const LossPlan& p, int64_t rows, int cols, const int32_t* labels, int ignore,
+                         float* down, uint32_t* most, hipStream_t st) {
+  const dim3 grid((unsigned)std::min<int64_t>(ceil_div(rows, kThreads / 64), 256 * 8));
+  hipLaunchKernelGGL(row_most_kernel, grid, dim3(kThreads), 0, st, x, rows, cols, labels, ignore, (uint32_t*)down, most);
+  hipLaunchKernelGGL(relay_planes_kernel, grid, dim3(kThreads), 0, st, x, to, rows, cols, p.groups, labels, ignore, down, most);
   return check_launch("fc_softmax_loss relay");
 }
 
-vcnn_status launch_fc_softmax_loss_bf16(int batch, int in_f, int classes, const void* x, const void* w, const float* bias,
-                                        const int32_t* labels, int ignore, float* loss, float* sample_loss, void* dx, float* dw,
-                                        float* dbias, void* workspace, size_t bytes, hipStream_t st) {
+template <typename T>
+static vcnn_status loss_products(LossPlan p, int batch, int in_f, int classes, const T* x, const T* w, const float* bias,
+                                 const int32_t* labels, int ignore, float* loss, float* sample_loss, T* dx, float* dw, float* dbias,
+                                 void* workspace, hipStream_t st) {
+  constexpr bool F32 = sizeof(T) == 4;
   const bool grads = dx || dw || dbias;
-  LossPlan p = loss_plan_within((size_t)1 << 30, batch, in_f, classes, grads);
-  for (size_t most = (size_t)1 << 30; p.bytes > bytes; most /= 2) {
-    if (most < 256) {
-      p = loss_plan(std::min(batch, 64), batch, in_f, classes, grads);
-      break;
-    }
-    p = loss_plan_within(most, batch, in_f, classes, grads);
-  }
   char* const ws = (char*)workspace;
   LossMeta* const meta = (LossMeta*)ws;
   float* const each = sample_loss ? sample_loss : (float*)(ws + p.each);
   float* const lse = (float*)(ws + p.lse);
   float* const z = grads ? (float*)(ws + p.z) : nullptr;
-  const bf16* weights = (const bf16*)w;
-  if (p.relay_w) {
-    weights = (const bf16*)(ws + p.w);
-    if (vcnn_status s = relay((const bf16*)w, (bf16*)(ws + p.w), classes, in_f, p.groups, nullptr, 0, nullptr, 0, nullptr, st)) return s;
-  }
-  const int64_t x_pitch = (int64_t)p.groups * 16, z_pitch = (int64_t)p.classes_pitch * 4;
+  float* const down_x = F32 ? (float*)(ws + p.down_x) : nullptr;
+  float* const down_w = F32 ? (float*)(ws + p.down_w) : nullptr;
+  char* const xs = ws + p.x;
+  const char* weights = (const char*)w;
   for (int64_t b0 = 0; b0 < batch; b0 += p.part) {
     const int rows = (int)std::min<int64_t>(p.part, batch - b0);
     const int32_t* const lab = labels + b0;
-    bf16* const xs = (bf16*)(ws + p.x);
-    if (vcnn_status s = relay((const bf16*)x + b0 * in_f, xs, rows, in_f, p.groups, grads ? lab : nullptr, ignore, labels, batch,
-                              b0 == 0 ? meta : nullptr, st))
-      return s;
+    if (grads || F32) {
+      hipLaunchKernelGGL(loss_meta_kernel, dim3(1), dim3(1024), 0, st, labels, batch, ignore, b0 == 0, meta);
+      if (vcnn_status s = check_launch("fc_softmax_loss count")) return s;
+    }
+    if (b0 == 0 && p.relay_w) {
+      weights = ws + p.w;
+      if (vcnn_status s = relay(w, ws + p.w, p, classes, in_f, nullptr, 0, down_w, &meta->most[1], st)) return s;
+    }
+    if (vcnn_status s = relay(x + b0 * in_f, xs, p, rows, in_f, grads || F32 ? lab : nullptr, ignore, down_x, &meta->most[0], st)) return s;
     LossProduct l{};
-    l.p.a = {(const char*)weights, x_pitch, classes}, l.p.b = {(const char*)xs, x_pitch, rows};
-    l.p.k = p.groups * 8, l.p.segments = 1, l.p.slabs_per_split = (int)ceil_div(l.p.k, 32);
+    l.p.a = {weights, p.x_pitch, classes}, l.p.b = {xs, p.x_pitch, rows};
+    l.p.k = F32 ? in_f : p.groups * 8, l.p.slabs_per_split = (int)ceil_div(l.p.k, 32);
     l.rows = rows, l.cols = classes, l.z = z, l.z_pitch = p.classes_pitch, l.bias = bias, l.labels = lab;
     l.stats = (float2*)(ws + p.stats), l.at_label = (float*)(ws + p.at_label);
-    if (vcnn_status s = launch_product<EPI_LOGITS, true, true, false>(p.tile_z, l, 1, st)) return s;
+    l.meta = meta, l.down_a = down_w, l.down_b = down_x;
+    if (vcnn_status s = launch_product<EPI_LOGITS, true, true>(F32, p.tile_z, l, 1, st)) return s;
     hipLaunchKernelGGL(loss_rows_kernel, dim3((unsigned)ceil_div(rows, 16)), dim3(kThreads), 0, st, l.stats, p.stat_tiles, rows, classes,
                        lab, ignore, l.at_label, lse, each + b0);
     if (vcnn_status s = check_launch("fc_softmax_loss rows")) return s;
     if (!grads) continue;
     float* const shares = dbias ? (float*)(ws + p.shares) : nullptr;
-    hipLaunchKernelGGL(loss_grad_kernel, dim3((unsigned)(p.classes_pitch / 64), (unsigned)ceil_div(rows, 64)), dim3(kThreads), 0, st, z,
-                       p.classes_pitch, rows, classes, lab, ignore, lse, shares, p.classes_pitch);
+    hipLaunchKernelGGL(loss_grad_kernel<F32>, dim3((unsigned)(p.classes_pitch / 64), (unsigned)ceil_div(rows, 64)), dim3(kThreads), 0, st, z,
+                       p.classes_pitch, rows, classes, lab, ignore, lse, down_x, down_w, shares, p.classes_pitch);
     if (vcnn_status s = check_launch("fc_softmax_loss gradient")) return s;
+    const int64_t z_pitch = (int64_t)p.classes_pitch * 4;
     if (dx) {
       LossProduct g{};
-      g.p.a = {(const char*)weights, x_pitch, p.groups}, g.p.b = {(const char*)z, z_pitch, rows};
-      g.p.k = classes, g.p.segments = 1, g.p.slabs_per_split = p.slabs_per_split;
-      g.rows = rows, g.cols = in_f, g.meta = meta, g.out = (bf16*)dx + b0 * in_f;
+      g.p.a = {weights, p.x_pitch, p.groups}, g.p.b = {(const char*)z, z_pitch, rows};
+      g.p.k = classes, g.p.slabs_per_split = p.slabs_per_split;
+      g.rows = rows, g.cols = in_f, g.meta = meta, g.out = dx + b0 * in_f, g.down_b = down_x;
       g.partial = p.splits > 1 ? (float*)(ws + p.partial) : nullptr;
-      if (vcnn_status s = launch_product<EPI_DX, false, true, true>(p.tile_dx, g, p.splits, st)) return s;
+      if (vcnn_status s = launch_product<EPI_DX, false, true>(F32, p.tile_dx, g, p.splits, st)) return s;
       if (p.splits > 1) {
         const int64_t count = (int64_t)rows * in_f;
-        hipLaunchKernelGGL(loss_join_kernel, dim3((unsigned)ceil_div(count, 4 * kThreads)), dim3(kThreads), 0, st, g.partial, p.splits,
-                           count, meta, (bf16*)g.out);
+        hipLaunchKernelGGL(loss_join_kernel<T>, dim3((unsigned)ceil_div(count, 4 * kThreads)), dim3(kThreads), 0, st, g.partial, p.splits,
+                           count, meta, (T*)g.out);
         if (vcnn_status s = check_launch("fc_softmax_loss join")) return s;
       }
     }
     if (dw) {
       LossProduct g{};
-      g.p.a = {(const char*)xs, x_pitch, p.groups}, g.p.b = {(const char*)z, z_pitch, p.classes_pitch / 8};
-      g.p.k = rows, g.p.segments = 2, g.p.plane_b[1] = 1, g.p.slabs_per_split = 2 * (int)ceil_div(rows, 32);
-      g.rows = classes, g.cols = in_f, g.meta = meta, g.out = dw, g.add = b0 > 0;
-      if (vcnn_status s = launch_product<EPI_DW, false, false, true>(p.tile_dw, g, 1, st)) return s;
+      g.p.a = {xs, p.x_pitch, p.groups}, g.p.b = {(const char*)z, z_pitch, p.classes_pitch / 8};
+      g.p.k = rows, g.p.slabs_per_split = (int)ceil_div(rows, 32);
+      g.rows = classes, g.cols = in_f, g.meta = meta, g.out = dw, g.add = b0 > 0, g.down_b = down_w;
+      if (vcnn_status s = launch_product<EPI_DW, false, false>(F32, p.tile_dw, g, 1, st)) return s;
     }
     if (dbias) {
       hipLaunchKernelGGL(loss_bias_kernel, dim3((unsigned)ceil_div(classes, kThreads)), dim3(kThreads), 0, st, shares, p.classes_pitch,
@@ -479,8 +627,8 @@ vcnn_status launch_fc_softmax_loss_bf16(int batch, int in_f, int classes, const 
   return check_launch("fc_softmax_loss mean");
 }
 
-// ---- float ---------------------------------------------------------------------------------------------------------------
-// The samples that count, and x with zeros for the others.
+// ---- small float layers --------------------------------------------------------------------------------------------------
+// x with zeros for the samples that do not count.
 __global__ __launch_bounds__(kThreads) void loss_float_rows_kernel(const float* x, float* to, int64_t count, int cols,
                                                                    const int32_t* labels, int ignore) {
   for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < count; i += (int64_t)gridDim.x * kThreads)
@@ -489,7 +637,7 @@ __global__ __launch_bounds__(kThreads) void loss_float_rows_kernel(const float* 
 
 // A block a sample: z to d / C where it stands, and what the sample costs.
 __global__ __launch_bounds__(kThreads) void loss_float_kernel(float* z, int classes, const int32_t* labels, int ignore,
-                                                              const int32_t* all_labels, int batch, int grads, float* each) {
+                                                              int batch, int grads, float* each) {
   __shared__ float parts[kThreads / 64];
   __shared__ int counts[kThreads / 64];
   const int b = blockIdx.x, label = labels[b];
@@ -501,7 +649,7 @@ __global__ __launch_bounds__(kThreads) void loss_float_kernel(float* z, int clas
   for (int d = 32; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
   int n = 0;
   if (grads) {
-    for (int i = threadIdx.x; i < batch; i += kThreads) n += all_labels[i] != ignore;
+    for (int i = threadIdx.x; i < batch; i += kThreads) n += labels[i] != ignore;
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) n += __shfl_xor(n, d);
   }
@@ -531,12 +679,10 @@ __global__ __launch_bounds__(kThreads) void loss_float_kernel(float* z, int clas
 }
 
 struct LossFloatPlan {
-  int part;
-  size_t x, z, each, dw, dbias, bytes;
+  size_t x, z, each, bytes;
 };
-static LossFloatPlan loss_float_plan(int64_t part, int batch, int in_f, int classes, bool grads) {
+static LossFloatPlan loss_float_plan(int batch, int in_f, int classes, bool grads) {
   LossFloatPlan p{};
-  p.part = (int)part;
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t here = at;
@@ -544,65 +690,72 @@ static LossFloatPlan loss_float_plan(int64_t part, int batch, int in_f, int clas
     return here;
   };
   p.each = take((size_t)batch * 4);
-  p.z = take((size_t)part * classes * 4);
-  if (grads) {
-    p.x = take((size_t)part * in_f * 4);
-    p.dw = take((size_t)classes * in_f * 4), p.dbias = take((size_t)classes * 4);  // (of a part behind the first)
-  }
+  p.z = take((size_t)batch * classes * 4);
+  p.x = take(grads ? (size_t)batch * in_f * 4 : 0);
   p.bytes = at;
   return p;
 }
-static LossFloatPlan loss_float_plan_within(size_t most, int batch, int in_f, int classes, bool grads) {
-  const int64_t fit = std::max<int64_t>(64, std::min<int64_t>((int64_t)(most / ((size_t)classes * 4)), kMostSamples) / 64 * 64);
-  return loss_float_plan(std::min<int64_t>(batch, ceil_div(ceil_div(batch, ceil_div(batch, fit)), 64) * 64), batch, in_f, classes, grads);
-}
-size_t fc_softmax_loss_workspace_f32(int batch, int in_f, int classes, bool grads) {
-  return loss_float_plan_within((size_t)1 << 30, batch, in_f, classes, grads).bytes;
-}
-size_t fc_softmax_loss_least_workspace_f32(int batch, int in_f, int classes, bool grads) {
-  return std::min(loss_float_plan(std::min(batch, 64), batch, in_f, classes, grads).bytes, fc_softmax_loss_workspace_f32(batch, in_f, classes, grads));
+
+// Small float layers by the float products, whole: d is made of finished logits there.
+static bool loss_is_small(int64_t batch, int64_t in_f, int64_t classes, bool grads) {
+  return batch * classes <= (int64_t)1 << 24 && batch * in_f * classes <= (int64_t)1 << 27;
 }
 
-vcnn_status launch_fc_softmax_loss_f32(int batch, int in_f, int classes, const float* x, const float* w, const float* bias,
-                                       const int32_t* labels, int ignore, float* loss, float* sample_loss, float* dx, float* dw,
-                                       float* dbias, void* workspace, size_t bytes, hipStream_t st) {
+static vcnn_status loss_float(int batch, int in_f, int classes, const float* x, const float* w, const float* bias,
+                              const int32_t* labels, int ignore, float* loss, float* sample_loss, float* dx, float* dw, float* dbias,
+                              void* workspace, hipStream_t st) {
   const bool grads = dx || dw || dbias;
-  LossFloatPlan p = loss_float_plan_within((size_t)1 << 30, batch, in_f, classes, grads);
-  for (size_t most = (size_t)1 << 30; p.bytes > bytes; most /= 2) {
-    p = most < 256 ? loss_float_plan(std::min(batch, 64), batch, in_f, classes, grads)
-                   : loss_float_plan_within(most, batch, in_f, classes, grads);
-    if (most < 256) break;
-  }
+  const LossFloatPlan p = loss_float_plan(batch, in_f, classes, grads);
   char* const ws = (char*)workspace;
   float* const each = sample_loss ? sample_loss : (float*)(ws + p.each);
   float* const z = (float*)(ws + p.z);
-  for (int64_t b0 = 0; b0 < batch; b0 += p.part) {
-    const int rows = (int)std::min<int64_t>(p.part, batch - b0);
-    const int32_t* const lab = labels + b0;
-    const float* xs = x + b0 * in_f;
-    if (vcnn_status s = vcnn_fc_fwd(VCNN_F32, rows, in_f, classes, VCNN_ACT_NONE, xs, w, bias, z, st)) return s;
-    hipLaunchKernelGGL(loss_float_kernel, dim3((unsigned)rows), dim3(kThreads), 0, st, z, classes, lab, ignore, labels, batch, (int)grads,
-                       each + b0);
-    if (vcnn_status s = check_launch("fc_softmax_loss rows")) return s;
-    if (!grads) continue;
-    if (dw) {
-      const int64_t count = (int64_t)rows * in_f;
-      hipLaunchKernelGGL(loss_float_rows_kernel, dim3((unsigned)std::min<int64_t>(ceil_div(count, kThreads), 256 * 16)), dim3(kThreads),
-                         0, st, xs, (float*)(ws + p.x), count, in_f, lab, ignore);
-      if (vcnn_status s = check_launch("fc_softmax_loss rows of x")) return s;
-      xs = (const float*)(ws + p.x);
-    }
-    float* const dw_here = b0 == 0 || !dw ? dw : (float*)(ws + p.dw);
-    float* const db_here = b0 == 0 || !dbias ? dbias : (float*)(ws + p.dbias);
-    if (vcnn_status s = vcnn_fc_bwd(VCNN_F32, rows, in_f, classes, xs, w, z, dw_here, db_here, dx ? dx + b0 * in_f : nullptr, st)) return s;
-    if (b0 == 0) continue;
-    if (dw)
-      if (vcnn_status s = launch_sgd_f32((size_t)classes * in_f, -1.f, dw, dw_here, st)) return s;
-    if (dbias)
-      if (vcnn_status s = launch_sgd_f32((size_t)classes, -1.f, dbias, db_here, st)) return s;
+  if (vcnn_status s = vcnn_fc_fwd(VCNN_F32, batch, in_f, classes, VCNN_ACT_NONE, x, w, bias, z, st)) return s;
+  hipLaunchKernelGGL(loss_float_kernel, dim3((unsigned)batch), dim3(kThreads), 0, st, z, classes, labels, ignore, batch, (int)grads, each);
+  if (vcnn_status s = check_launch("fc_softmax_loss rows")) return s;
+  if (dw) {
+    const int64_t count = (int64_t)batch * in_f;
+    hipLaunchKernelGGL(loss_float_rows_kernel, dim3((unsigned)std::min<int64_t>(ceil_div(count, kThreads), 256 * 16)), dim3(kThreads),
+                       0, st, x, (float*)(ws + p.x), count, in_f, labels, ignore);
+    if (vcnn_status s = check_launch("fc_softmax_loss rows of x")) return s;
+    x = (const float*)(ws + p.x);
   }
+  if (grads)
+    if (vcnn_status s = vcnn_fc_bwd(VCNN_F32, batch, in_f, classes, x, w, z, dw, dbias, dx, st)) return s;
   hipLaunchKernelGGL(loss_mean_kernel, dim3(1), dim3(1024), 0, st, each, labels, ignore, batch, loss);
   return check_launch("fc_softmax_loss mean");
+}
+
+// ---- entry ---------------------------------------------------------------------------------------------------------------
+size_t fc_softmax_loss_workspace(int dtype, int batch, int in_f, int classes, bool grads) {
+  const bool f32 = dtype == VCNN_F32;
+  if (f32 && loss_is_small(batch, in_f, classes, grads))  // (enough for small parts by the other products, too)
+    return std::max(loss_float_plan(batch, in_f, classes, grads).bytes, loss_plan(f32, std::min(batch, 64), batch, in_f, classes, grads).bytes);
+  return loss_plan_within(f32, kMostLogits, batch, in_f, classes, grads).bytes;
+}
+size_t fc_softmax_loss_least_workspace(int dtype, int batch, int in_f, int classes, bool grads) {
+  const bool f32 = dtype == VCNN_F32;
+  const size_t whole = fc_softmax_loss_workspace(dtype, batch, in_f, classes, grads);
+  return std::min(whole, loss_plan(f32, std::min(batch, 64), batch, in_f, classes, grads).bytes);
+}
+
+vcnn_status launch_fc_softmax_loss(int dtype, int batch, int in_f, int classes, const void* x, const void* w, const float* bias,
+                                   const int32_t* labels, int ignore, float* loss, float* sample_loss, void* dx, float* dw,
+                                   float* dbias, void* workspace, size_t bytes, hipStream_t st) {
+  const bool grads = dx || dw || dbias, f32 = dtype == VCNN_F32;
+  if (f32 && loss_is_small(batch, in_f, classes, grads) && bytes >= loss_float_plan(batch, in_f, classes, grads).bytes)
+    return loss_float(batch, in_f, classes, (const float*)x, (const float*)w, bias, labels, ignore, loss, sample_loss, (float*)dx, dw,
+                      dbias, workspace, st);
+  LossPlan p = loss_plan_within(f32, kMostLogits, batch, in_f, classes, grads);
+  for (size_t most = kMostLogits / 2; p.bytes > bytes; most /= 2) {
+    const bool last = most < 256;
+    p = last ? loss_plan(f32, std::min(batch, 64), batch, in_f, classes, grads) : loss_plan_within(f32, most, batch, in_f, classes, grads);
+    if (last) break;
+  }
+  if (f32)
+    return loss_products(p, batch, in_f, classes, (const float*)x, (const float*)w, bias, labels, ignore, loss, sample_loss, (float*)dx, dw,
+                         dbias, workspace, st);
+  return loss_products(p, batch, in_f, classes, (const bf16*)x, (const bf16*)w, bias, labels, ignore, loss, sample_loss, (bf16*)dx, dw,
+                       dbias, workspace, st);
 }
 
 }  // namespace vcnn

@@ -21,21 +21,23 @@ struct Operand16 {
 struct ProductArgs {
   Operand16 a, b;
   int k;                // contraction steps (rows along k: up to the next multiple of 8 there are zeros)
-  int segments;         // pairs of planes
-  int plane_a[3], plane_b[3];
   int tiles_a, tiles_b;
-  int slabs_per_split;  // of segments * ceil(k / 32)
+  int slabs_per_split;  // of ceil(k / 32)
 };
 
-// BA x BB outputs by waves of 16 TA x 16 TB.
-template <int BA_, int BB_, int TA_, int TB_>
+// BA x BB outputs by waves of 16 TA x 16 TB, from PA and PB planes of the operands: high x high, and the products of a low term
+// with the other's high one.  RING slabs in LDS.
+template <int BA_, int BB_, int TA_, int TB_, int PA_, int PB_, int RING_>
 struct ProductTile {
-  static constexpr int BA = BA_, BB = BB_, TA = TA_, TB = TB_, RING = 4;
-  static constexpr int WA = BA / (16 * TA), WB = BB / (16 * TB), THREADS = WA * WB * 64;
-  static constexpr int WORDS = (BA + BB) * 4;  // 16-byte words of a slab of 32 steps
+  static constexpr int BA = BA_, BB = BB_, TA = TA_, TB = TB_, PA = PA_, PB = PB_, RING = RING_;
+  static constexpr int WA = BA / (16 * TA), WB = BB / (16 * TB), WAVES = WA * WB, THREADS = WAVES * 64;
+  static constexpr int WORDS = (PA * BA + PB * BB) * 4;  // 16-byte words of a slab of 32 steps
   static constexpr size_t LDS = (size_t)RING * WORDS * 16;
-  static constexpr int LA = BA * 4 / THREADS, LB = BB * 4 / THREADS;  // words a thread brings of one
-  static_assert(TA % 2 == 0 && LA * THREADS == BA * 4 && LB * THREADS == BB * 4 && LA + LB >= 2, "whole slabs");
+  static constexpr int BLOCKS = 160 * 1024 / LDS >= 2 && THREADS <= 256 ? 2 : 1;   // a CU's
+  static constexpr int WAVES_SIMD = BLOCKS * WAVES / 4;
+  static constexpr int LA = BA * 4 / THREADS, LB = BB * 4 / THREADS;  // words a thread brings of a plane
+  static constexpr int LOADS = PA * LA + PB * LB;
+  static_assert(TA % 2 == 0 && LA * THREADS == BA * 4 && LB * THREADS == BB * 4, "whole slabs");
 };
 
 __device__ const uint4 kZeroWord = {0, 0, 0, 0};
@@ -81,14 +83,17 @@ struct Way {
       }
     }
   }
-  // Word i of slab s (32 steps from 32 s on; `left` of them are there) of a plane, to `to` (wave-uniform).
-  __device__ __forceinline__ void stage(int i, int s, int left, int plane, uint4* to) const {
-    const char* from = base;
-    if constexpr (ALONG) from += PLANES ? (int64_t)(s >> 1) * 256 + (s & 1) * 64 : (int64_t)s * 64;
-    else from += (int64_t)s * 32 * pitch;
-    if (PLANES) from += plane * 128;
-    if (left >= 32) load_to_lds16(from, offset[i], to);
-    else load_to_lds16(step[i] < left ? reinterpret_cast<const uint4*>(from + offset[i]) : &kZeroWord, to);
+  // Word i of a plane of slab s (32 steps from 32 s on) to `to` (wave-uniform).
+  __device__ __forceinline__ const char* from(int s, int plane) const {
+    int64_t at;
+    if constexpr (ALONG) at = PLANES ? (int64_t)(s >> 1) * 256 + (s & 1) * 64 + plane * 128 : (int64_t)s * 64;
+    else at = (int64_t)s * 32 * pitch + plane * 128;
+    return base + at;
+  }
+  __device__ __forceinline__ void stage(int i, int s, int plane, uint4* to) const { load_to_lds16(from(s, plane), offset[i], to); }
+  // Only `left` of the 32 steps are there: zeros for the others.
+  __device__ __forceinline__ void stage(int i, int s, int plane, int left, uint4* to) const {
+    load_to_lds16(step[i] < left ? reinterpret_cast<const uint4*>(from(s, plane) + offset[i]) : &kZeroWord, to);
   }
   // Row tile at r (of the tile) of the slab at buf: lane l holds row l % 16, steps 8 (l / 16) .. + 8.
   __device__ static __forceinline__ uint4 fragment(const uint4* buf, int r, int lane) {
@@ -114,27 +119,35 @@ __device__ __forceinline__ void product_tile_of(const ProductArgs& p, int* ta, i
   *ta = in / wide, *tb = group * 8 + in % wide;
 }
 
-// Slabs of 32 steps go to a ring of four by direct loads, three slabs ahead; a wave reads the second half of a step's a-tiles while
-// it multiplies the first, and the first of the next step while it multiplies the second, so that neither the loads nor the barrier
+// Slabs of 32 steps go to a ring by direct loads, RING - 1 slabs ahead; a wave reads the second half of a step's a-tiles while it
+// multiplies the first, and the first of the next step while it multiplies the second, so that neither the loads nor the barrier
 // (one a slab) leave the matrix cores without operands.  acc[i][j]: lane l has a = 16 i + 4 (l / 16) + q, b = 16 j + l % 16 of the
 // wave's part.
 template <typename TILE, bool F16, bool A_ALONG, bool A_PLANES, bool B_ALONG, bool B_PLANES>
 __device__ __forceinline__ void slab_product(const ProductArgs& p, int a0, int b0, uint4* smem,
                                              f32x4 (&acc)[TILE::TA][TILE::TB]) {
-  constexpr int TA = TILE::TA, TB = TILE::TB, LA = TILE::LA, LB = TILE::LB, L = LA + LB, R = TILE::RING;
+  constexpr int TA = TILE::TA, TB = TILE::TB, PA = TILE::PA, PB = TILE::PB, LA = TILE::LA, LB = TILE::LB, L = TILE::LOADS;
+  constexpr int R = TILE::RING;
   using WayA = Way<A_ALONG, A_PLANES, TILE::BA, TILE::THREADS>;
   using WayB = Way<B_ALONG, B_PLANES, TILE::BB, TILE::THREADS>;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const WayA wa(p.a, a0, tid);
   const WayB wb(p.b, b0, tid);
-  const int per_plane = (p.k + 31) / 32, first = blockIdx.y * p.slabs_per_split;
-  const int slabs = min(p.slabs_per_split, p.segments * per_plane - first);
-  auto stage = [&](int s, int i) {  // load i of L of slab s; behind the last: zeros
-    const int at = first + s, seg = p.segments == 1 ? 0 : (at >= per_plane) + (at >= 2 * per_plane);
-    const int slab = at - seg * per_plane, left = s < slabs ? p.k - slab * 32 : 0;
-    uint4* const to = smem + (s % R) * TILE::WORDS + i * TILE::THREADS + wave * 64;
-    if (i < LA) wa.stage(i, slab, left, A_PLANES ? p.plane_a[seg] : 0, to);
-    else wb.stage(i - LA, slab, left, B_PLANES ? p.plane_b[seg] : 0, to);
+  const int first = blockIdx.y * p.slabs_per_split;
+  const int slabs = min(p.slabs_per_split, (p.k + 31) / 32 - first), whole = min(slabs, p.k / 32 - first);
+  // load i of L of slab s, to its place `slot` in the ring; WHOLE: it is known to have 32 steps (otherwise, and behind the last, zeros for what there is not)
+  auto stage = [&](int s, int slot, int i, auto is_whole) {
+    constexpr bool WHOLE = decltype(is_whole)::value;
+    uint4* const to = smem + slot * TILE::WORDS + i * TILE::THREADS + wave * 64;
+    const int left = WHOLE ? 32 : s < slabs ? p.k - (first + s) * 32 : 0;
+    if (i < PA * LA) {
+      if constexpr (WHOLE) wa.stage(i % LA, first + s, i / LA, to);
+      else wa.stage(i % LA, first + s, i / LA, left, to);
+    } else {
+      const int n = i - PA * LA;
+      if constexpr (WHOLE) wb.stage(n % LB, first + s, n / LB, to);
+      else wb.stage(n % LB, first + s, n / LB, left, to);
+    }
   };
 #pragma unroll
   for (int i = 0; i < TA; ++i)
@@ -142,60 +155,78 @@ __device__ __forceinline__ void slab_product(const ProductArgs& p, int a0, int b
     for (int j = 0; j < TB; ++j) acc[i][j] = (f32x4){0.f, 0.f, 0.f, 0.f};
   const int ra = (wave % TILE::WA) * 16 * TA, rb = (wave / TILE::WA) * 16 * TB;
   constexpr int H = TA / 2;
-  uint4 fa[2][H], fb[2][TB];
-  auto read_a = [&](int s, int h) {
-    const uint4* const buf = smem + (s % R) * TILE::WORDS;
+  // fa: [half][term]; fb: the high terms of this step and the next, and the low ones of this step
+  uint4 fa[2][PA][H], fb[2][TB], fl[TB];
+  auto read_a = [&](int slot, int h) {
+    const uint4* const buf = smem + slot * TILE::WORDS;
 #pragma unroll
-    for (int i = 0; i < H; ++i) fa[h][i] = WayA::fragment(buf, ra + (h * H + i) * 16, lane);
-  };
-  auto read_b = [&](int s, int n) {
-    const uint4* const buf = smem + (s % R) * TILE::WORDS + TILE::BA * 4;
+    for (int t = 0; t < PA; ++t)
 #pragma unroll
-    for (int j = 0; j < TB; ++j) fb[n][j] = WayB::fragment(buf, rb + j * 16, lane);
+      for (int i = 0; i < H; ++i) fa[h][t][i] = WayA::fragment(buf + t * TILE::BA * 4, ra + (h * H + i) * 16, lane);
   };
-  // The products of half h, loads l0 .. l1 of slab s among them: a load waits its turn behind those of the other waves, and the
-  // matrix cores are not to wait with it.
-  auto multiply = [&](int h, int n, int s, int l0, int l1) {
-    const int every = H * TB / (l1 - l0);
+  auto read_b = [&](int slot, uint4 (&to)[TB], int t) {
+    const uint4* const buf = smem + slot * TILE::WORDS + (PA * TILE::BA + t * TILE::BB) * 4;
+#pragma unroll
+    for (int j = 0; j < TB; ++j) to[j] = WayB::fragment(buf, rb + j * 16, lane);
+  };
+  // The products of half h: term t of a with `with`.  Loads of slab s, every L / (2 PAIRS) such products one, stand among them: a
+  // load waits its turn behind those of the other waves, and the matrix cores are not to wait with it.
+  constexpr int PAIRS = PA == 2 && PB == 2 ? 3 : PA * PB;
+  auto multiply = [&](int h, int t, const uint4 (&with)[TB], int s, int slot, int turn, auto is_whole) {
+    const int l0 = L * turn / (2 * PAIRS), l1 = L * (turn + 1) / (2 * PAIRS), every = H * TB / (l1 > l0 ? l1 - l0 : 1);
 #pragma unroll
     for (int m = 0; m < H * TB; ++m) {
       const int i = m / TB, j = m % TB;
-      if constexpr (F16) acc[h * H + i][j] = mfma_f16(fa[h][i], fb[n][j], acc[h * H + i][j]);
-      else acc[h * H + i][j] = mfma_bf16(fa[h][i], fb[n][j], acc[h * H + i][j]);
+      if constexpr (F16) acc[h * H + i][j] = mfma_f16(fa[h][t][i], with[j], acc[h * H + i][j]);
+      else acc[h * H + i][j] = mfma_bf16(fa[h][t][i], with[j], acc[h * H + i][j]);
       if (m % every == every / 2 && l0 + m / every < l1) {
         __builtin_amdgcn_sched_barrier(0);
-        stage(s, l0 + m / every);
+        stage(s, slot, l0 + m / every, is_whole);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
+    __builtin_amdgcn_sched_barrier(0);
   };
   constexpr auto all_but = [](int n) { return 0x0F70 | (n & 15) | n >> 4 << 14; };  // vmcnt(n)
   static_assert((R - 2) * L < 64, "the counts fit");
 #pragma unroll
   for (int s = 0; s < R - 1; ++s)
 #pragma unroll
-    for (int i = 0; i < L; ++i) stage(s, i);
+    for (int i = 0; i < L; ++i) stage(s, s, i, std::false_type());
   __builtin_amdgcn_s_waitcnt(all_but((R - 2) * L));
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
-  read_b(0, 0), read_a(0, 0);
-  auto step = [&](int s, int n) {
+  read_b(0, fb[0], 0), read_a(0, 0);
+  __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): so that the loop's own waits need not count what came before it
+  int here = 0;  // the slab's place
+  auto step = [&](int s, int n, auto is_whole) {
+    const int next = here + 1 == R ? 0 : here + 1, last = here == 0 ? R - 1 : here - 1;
     // slab s + 1 is there, for everyone; slab s - 1 has been read by everyone
     __builtin_amdgcn_s_waitcnt(all_but((R - 3) * L));
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    read_a(s, 1);
+    int turn = 0;
+    if constexpr (PB == 2) read_b(here, fl, 1);
+    read_a(here, 1);
     __builtin_amdgcn_sched_barrier(0);
-    multiply(0, n, s + R - 1, 0, L / 2);
+    multiply(0, 0, fb[n], s + R - 1, last, turn++, is_whole);
+    if constexpr (PA == 2) multiply(0, 1, fb[n], s + R - 1, last, turn++, is_whole);
+    if constexpr (PB == 2) multiply(0, 0, fl, s + R - 1, last, turn++, is_whole);
+    read_b(next, fb[n ^ 1], 0), read_a(next, 0);
     __builtin_amdgcn_sched_barrier(0);
-    read_b(s + 1, n ^ 1), read_a(s + 1, 0);
-    __builtin_amdgcn_sched_barrier(0);
-    multiply(1, n, s + R - 1, L / 2, L);
-    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (PB == 2) multiply(1, 0, fl, s + R - 1, last, turn++, is_whole);
+    if constexpr (PA == 2) multiply(1, 1, fb[n], s + R - 1, last, turn++, is_whole);
+    multiply(1, 0, fb[n], s + R - 1, last, turn++, is_whole);
+    here = next;
   };
-  for (int s = 0; s < slabs; s += 2) {
-    step(s, 0);
-    step(s + 1, 1);
+  int s = 0;
+  for (; s + R < whole; s += 2) {
+    step(s, 0, std::true_type());
+    step(s + 1, 1, std::true_type());
+  }
+  for (; s < slabs; s += 2) {
+    step(s, 0, std::false_type());
+    step(s + 1, 1, std::false_type());
   }
   __builtin_amdgcn_s_waitcnt(0x0070);  // nothing more is on its way to LDS, or from it
   __syncthreads();

@@ -1366,7 +1366,7 @@ vcnn_status vcnn_fc_softmax_loss(int32_t dtype, int32_t batch, int32_t in_f, int
   if (vcnn_status s = check_fc_softmax(dtype, batch, in_f, classes)) return s;
   if (!x || !w || !labels || !loss) return fail(VCNN_ERR_NULL, "fc_softmax_loss: NULL tensor");
   const bool grads = dx || dw || dbias;
-  if (dtype == VCNN_BF16 && in_f % 8 == 0 && (reinterpret_cast<uintptr_t>(w) & 15))
+  if (dtype == VCNN_BF16 && in_f % 8 == 0 && (reinterpret_cast<uintptr_t>(w) & 15))  // (read where it stands)
     return fail(VCNN_ERR_UNSUPPORTED, "fc_softmax_loss: w must be 16-byte aligned");
   if (vcnn_status s = check_ws(workspace, workspace_bytes, fc_softmax_loss_least_workspace(dtype, batch, in_f, classes, grads), "fc_softmax_loss"))
     return s;

@@ -3,7 +3,7 @@
 //     d = softmax(z) - onehot(label) (0 for samples that do not count),   dx = d w / C,   dw = d^T x / C,   dbias = sum_r d_r / C
 //
 // The samples go through in parts.  A part's logits are made once (z, float), by a product whose tiles leave the largest logit of
-// each sample and its sum of exponentials beside them; these are joined to lse; one pass turns z where it stands into d, a high
+// each sample and its sum of exponentials beside them; these are joined; one pass turns z where it stands into d, a high
 // and a low bfloat16 term of the difference, and two products make dx and dw from it.  Without gradients z is not stored at all.
 //   d in two terms: dw is float, and one bfloat16 term alone would leave 2^-9 of each element in it (the two leave 2^-18).  dx is
 //   bfloat16 itself and takes the high term alone.
@@ -82,7 +82,14 @@ __global__ __launch_bounds__(kThreads) void row_most_kernel(const float* x, int6
     if (lane == 0) row_most[row] = m;
     all = max(all, m);
   }
-  if (lane == 0 && all) atomicMax(most, all);  // (whatever the order, the same)
+  // one of a block, and only if it is larger than what is known (2000 of one place take 60 us); whatever the order, the same
+  __shared__ uint32_t tops[kThreads / 64];
+  if (lane == 0) tops[threadIdx.x >> 6] = all;
+  __syncthreads();
+  if (threadIdx.x > 0) return;
+#pragma unroll
+  for (int w = 1; w < kThreads / 64; ++w) all = max(all, tops[w]);
+  if (all > __atomic_load_n(most, __ATOMIC_RELAXED)) atomicMax(most, all);
 }
 
 // The power of two that brings the largest of all, `bits`, to 2^14 .. 2^15 (kept to where it and its inverse are floats).
@@ -134,12 +141,15 @@ __global__ __launch_bounds__(kThreads) void relay_planes_kernel(const float* x, 
   }
 }
 
-// Logits are compared and summed as powers of two: 2^(z log2 e - m), with log2 e in two terms, so that the rounding of the constant
-// (1.3e-8 of z) is not seen.  The instruction is off by one unit in the last place.
-__device__ __forceinline__ float log2e_times_less(float z, float m) {
-  return fmaf(z, 1.925963033e-8f, fmaf(z, 1.442695022f, -m));
+// e^d of a difference d <= 0 of two logits, off by 2^-24 |d| and one unit in the last place.
+__device__ __forceinline__ float exp_of(float d) { return __builtin_amdgcn_exp2f(d * 1.442695041f); }
+
+// Sums of exponentials about a maximum, two as one.
+__device__ __forceinline__ void join(float2& a, float2 b) {
+  const float top = fmaxf(a.x, b.x);
+  a.y = top > -__builtin_inff() ? a.y * exp_of(a.x - top) + b.y * exp_of(b.x - top) : a.y + b.y;  // (nothing yet, or a NaN)
+  a.x = top;
 }
-__device__ __forceinline__ float exp2_of(float t) { return __builtin_amdgcn_exp2f(t); }
 
 // ---- products ------------------------------------------------------------------------------------------------------------
 enum { EPI_LOGITS = 0, EPI_DX = 1, EPI_DW = 2 };
@@ -152,7 +162,7 @@ struct LossProduct {
   int64_t z_pitch;
   const float* bias;     // nullable
   const int32_t* labels;
-  float2* stats;         // [16 TA of classes][rows]: the largest logit times log2 e, the sum of powers about it
+  float2* stats;         // [16 TA of classes][rows]: the largest logit, the sum of exponentials about it
   float* at_label;
   // EPI_DX, EPI_DW
   const LossMeta* meta;
@@ -236,13 +246,12 @@ __global__ __launch_bounds__(TILE::THREADS, TILE::WAVES_SIMD) void loss_product_
           if (ca + 16 * i + q < a.cols) most = fmaxf(most, acc[i][j][q]);
       most = fmaxf(most, __shfl_xor(most, 16));
       most = fmaxf(most, __shfl_xor(most, 32));
-      most = log2e_times_less(most, 0.f);
       if (most > -__builtin_inff()) {  // (none of these classes is possible: their sum is 0)
 #pragma unroll
         for (int i = 0; i < TILE::TA; ++i)
 #pragma unroll
           for (int q = 0; q < 4; ++q)
-            if (ca + 16 * i + q < a.cols) sum += exp2_of(log2e_times_less(acc[i][j][q], most));
+            if (ca + 16 * i + q < a.cols) sum += exp_of(acc[i][j][q] - most);
       } else {  // (or all are NaN)
 #pragma unroll
         for (int i = 0; i < TILE::TA; ++i)
@@ -301,6 +310,86 @@ __global__ __launch_bounds__(TILE::THREADS, TILE::WAVES_SIMD) void loss_product_
   }
 }
 
+// ---- few samples, the cost alone ------------------------------------------------------------------------------------------
+// Bandwidth: w is read once, where it stands.  A wave takes 16 classes and up to 16 NB samples and reads its operands as the matrix
+// instruction wants them, straight into registers: lane l row l % 16, and of every 128 bytes of it the 16 from 16 (l / 16) on and the 16
+// that are 64 further.  (Which steps of the sum a lane holds does not matter as long as it is the same ones of both.)  The eight waves
+// of a block leave one maximum and sum of their 128 classes.
+static constexpr int kFewThreads = 512, kFewClasses = 16 * kFewThreads / 64, kFewRows = 64;
+
+template <typename T, int NB>
+__global__ __launch_bounds__(kFewThreads) void loss_few_kernel(LossProduct a, const T* xs, const T* ws, int in_f) {
+  constexpr int AHEAD = 4, N = 16 / sizeof(T), STEP = 4 * N;  // elements of a load, and of a row's four
+  __shared__ float2 parts[kFewThreads / 64][NB * 16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, at = (lane >> 4) * N;
+  const int c0 = blockIdx.x * kFewClasses + wave * 16;
+  const T* const w = ws + (int64_t)min(c0 + row, a.cols - 1) * in_f;
+  const T* x[NB];
+  f32x4 acc[NB];
+#pragma unroll
+  for (int n = 0; n < NB; ++n) {
+    x[n] = xs + (int64_t)min(n * 16 + row, a.rows - 1) * in_f;
+    acc[n] = (f32x4){0.f, 0.f, 0.f, 0.f};
+  }
+  auto whole_group = [](const T* p) { return *reinterpret_cast<const Loose16*>(p); };
+  auto multiply = [](const Loose16& p, const Loose16& q, f32x4 c) {
+    if constexpr (sizeof(T) == 2) {
+      return mfma_bf16(make_uint4(p.w[0], p.w[1], p.w[2], p.w[3]), make_uint4(q.w[0], q.w[1], q.w[2], q.w[3]), c);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(p.w[i]), __uint_as_float(q.w[i]), c, 0, 0, 0);
+      return c;
+    }
+  };
+  int k = 0;
+  for (; k + AHEAD * 2 * STEP <= in_f; k += AHEAD * 2 * STEP) {
+    Loose16 fw[2 * AHEAD];
+#pragma unroll
+    for (int u = 0; u < 2 * AHEAD; ++u) fw[u] = whole_group(w + k + u * STEP + at);
+#pragma unroll
+    for (int u = 0; u < 2 * AHEAD; ++u)
+#pragma unroll
+      for (int n = 0; n < NB; ++n) acc[n] = multiply(fw[u], whole_group(x[n] + k + u * STEP + at), acc[n]);
+  }
+  for (; k < in_f; k += STEP) {
+    Loose16 fw{{0, 0, 0, 0}};
+    if (k + at < in_f) fw = load_group(w, k + at, in_f);
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+      Loose16 fx{{0, 0, 0, 0}};
+      if (k + at < in_f) fx = load_group(x[n], k + at, in_f);
+      acc[n] = multiply(fw, fx, acc[n]);
+    }
+  }
+  const int c = c0 + 4 * (lane >> 4);
+#pragma unroll
+  for (int n = 0; n < NB; ++n) {
+    const int b = n * 16 + row, label = a.labels[min(b, a.rows - 1)];
+    float most = -__builtin_inff(), sum = 0.f;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if (a.bias) acc[n][q] += a.bias[min(c + q, a.cols - 1)];
+      if (c + q < a.cols) most = fmaxf(most, acc[n][q]);
+      if (b < a.rows && c + q == label && label < a.cols) a.at_label[b] = acc[n][q];
+    }
+    most = fmaxf(most, __shfl_xor(most, 16));
+    most = fmaxf(most, __shfl_xor(most, 32));
+    const float about = most > -__builtin_inff() ? most : 0.f;  // (none is possible, or all are NaN)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (c + q < a.cols) sum += exp_of(acc[n][q] - about);
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    if (lane < 16) parts[wave][b] = make_float2(most, sum);
+  }
+  __syncthreads();
+  if (threadIdx.x >= NB * 16 || threadIdx.x >= a.rows) return;
+  float2 total = parts[0][threadIdx.x];
+#pragma unroll
+  for (int v = 1; v < kFewThreads / 64; ++v) join(total, parts[v][threadIdx.x]);
+  a.stats[(int64_t)blockIdx.x * a.rows + threadIdx.x] = total;
+}
+
 // dx from the shares of its sums, always in the same order.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void loss_join_kernel(const float* partial, int splits, int64_t count, const LossMeta* meta,
@@ -320,42 +409,73 @@ __global__ __launch_bounds__(kThreads) void loss_join_kernel(const float* partia
 }
 
 // ---- softmax -------------------------------------------------------------------------------------------------------------
-// lse (times log2 e) of sixteen samples from the tiles' maxima and sums, sixteen threads each, joined in a fixed order; what each sample costs.
-__global__ __launch_bounds__(kThreads) void loss_rows_kernel(const float2* stats, int tiles, int rows, int classes,
-                                                             const int32_t* labels, int ignore, const float* at_label, float* lse,
-                                                             float* each) {
+// Each sample's largest logit and the inverse of its sum of exponentials, and what it costs.
+struct LossRows {
+  const float2* stats;  // [tiles][rows]
+  int tiles, rows, classes;
+  const int32_t* labels;
+  int ignore;
+  const float* at_label;
+  float2* softmax;      // nullable
+  float* each;
+  float* loss;          // of few samples: their mean
+};
+__device__ __forceinline__ float finish_row(const LossRows& a, int b, float2 total) {
+  const int label = a.labels[b];
+  if (a.softmax) a.softmax[b] = make_float2(total.x, 1.f / total.y);
+  const float cost = label == a.ignore ? 0.f : label < 0 || label >= a.classes ? __builtin_nanf("")
+                                             : (total.x + logf(total.y)) - a.at_label[b];
+  a.each[b] = cost;
+  return cost;
+}
+
+// Sixteen samples a block, sixteen threads each, joined in a fixed order.
+__global__ __launch_bounds__(kThreads) void loss_rows_kernel(LossRows a) {
   __shared__ float2 parts[16][17];
   const int in = threadIdx.x & 15, part = threadIdx.x >> 4, b = blockIdx.x * 16 + in;
-  float most = -__builtin_inff(), sum = 0.f;
-  auto meet = [&](float m, float s) {
-    const float top = fmaxf(most, m);
-    if (top > -__builtin_inff()) sum = sum * exp2_of(most - top) + s * exp2_of(m - top);
-    else sum += s;  // (nothing yet, or a NaN)
-    most = top;
-  };
-  if (b < rows) {
+  float2 total = make_float2(-__builtin_inff(), 0.f);
+  if (b < a.rows) {
 #pragma unroll 4
-    for (int t = part; t < tiles; t += 16) {
-      const float2 v = stats[(int64_t)t * rows + b];
-      meet(v.x, v.y);
-    }
+    for (int t = part; t < a.tiles; t += 16) join(total, a.stats[(int64_t)t * a.rows + b]);
   }
-  parts[part][in] = make_float2(most, sum);
+  parts[part][in] = total;
   __syncthreads();
-  if (part > 0 || b >= rows) return;
-  for (int p = 1; p < 16; ++p) meet(parts[p][in].x, parts[p][in].y);
-  const float l = most + log2f(sum);
-  const int label = labels[b];
-  lse[b] = l;
-  each[b] = label == ignore ? 0.f : label < 0 || label >= classes ? __builtin_nanf("")
-                                                                  : -0.693147180559945f * log2e_times_less(at_label[b], l);
+  if (part > 0 || b >= a.rows) return;
+  for (int p = 1; p < 16; ++p) join(total, parts[p][in]);
+  finish_row(a, b, total);
+}
+
+// Few samples, a wave each, and their mean.
+__global__ __launch_bounds__(1024) void loss_few_rows_kernel(LossRows a) {
+  __shared__ float costs[kFewRows];
+  const int lane = threadIdx.x & 63;
+  for (int b = threadIdx.x >> 6; b < a.rows; b += 16) {
+    float2 total = make_float2(-__builtin_inff(), 0.f);
+#pragma unroll 8
+    for (int t = lane; t < a.tiles; t += 64) join(total, a.stats[(int64_t)t * a.rows + b]);
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) {
+      float2 other = make_float2(__shfl_xor(total.x, d), __shfl_xor(total.y, d));
+      join(total, other);
+    }
+    if (lane == 0) costs[b] = finish_row(a, b, total);
+  }
+  if (!a.loss) return;
+  __syncthreads();
+  if (threadIdx.x >= 64) return;
+  const bool in = lane < a.rows;
+  int n = in && a.labels[lane] != a.ignore;
+  const float s = wave_sum(in ? costs[lane] : 0.f);
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) n += __shfl_xor(n, d);
+  if (lane == 0) *a.loss = n ? s / (float)n : 0.f;
 }
 
 // z to d where it stands: 64 floats of a row become 64 high and 64 low terms (the sixteen lanes that read them are of one wave, which
 // has them all before it writes); behind the last class zeros.  Each block leaves its samples' share of dbias.
 template <bool F32>
 __global__ __launch_bounds__(kThreads) void loss_grad_kernel(float* z, int64_t pitch, int rows, int classes, const int32_t* labels,
-                                                             int ignore, const float* lse, const float* down_x, const float* down_w,
+                                                             int ignore, const float2* softmax, const float* down_x, const float* down_w,
                                                              float* shares, int64_t share_pitch) {
   __shared__ float sums[16][64];
   const int in = threadIdx.x & 15, part = threadIdx.x >> 4, c = blockIdx.x * 64 + in * 4;
@@ -370,14 +490,14 @@ __global__ __launch_bounds__(kThreads) void loss_grad_kernel(float* z, int64_t p
     if (b >= rows) break;
     const int label = labels[b];
     const bool counts = label != ignore, bad = counts && (label < 0 || label >= classes);
-    const float l = lse[b];
+    const float2 about = softmax[b];
     char* const row = reinterpret_cast<char*>(z + b * pitch);
     const float4 v = *reinterpret_cast<const float4*>(row + c * 4);
     float d[4] = {v.x, v.y, v.z, v.w};
     uint2 h, r;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      d[q] = exp2_of(log2e_times_less(d[q], l)) - (c + q == label ? 1.f : 0.f);
+      d[q] = exp_of(d[q] - about.x) * about.y - (c + q == label ? 1.f : 0.f);
       if (bad) d[q] = __builtin_nanf("");
       if (!counts || c + q >= classes) d[q] = 0.f;
       total[q] += d[q];
@@ -462,10 +582,10 @@ struct LossPlan {
   int groups;          // of eight inputs, of a row as it is relaid
   int64_t x_pitch;     // bytes of such a row
   int stat_tiles;      // of classes
-  bool f32, relay_w;
+  bool f32, few, relay_w;
   int splits, slabs_per_split;  // of dx
   int tile_z, tile_dx, tile_dw;
-  size_t x, w, down_x, down_w, stats, at_label, lse, each, z, partial, shares, bytes;  // places in the workspace
+  size_t x, w, down_x, down_w, stats, at_label, softmax, each, z, partial, shares, bytes;  // places in the workspace
 };
 
 static constexpr int kMostSamples = 1 << 20;  // of a part
@@ -478,9 +598,10 @@ static LossPlan loss_plan(bool f32, int part, int batch, int in_f, int classes, 
   p.classes_pitch = (int)ceil_div(classes, 64) * 64;
   p.groups = f32 ? (int)ceil_div(in_f, 64) * 8 : (int)ceil_div(in_f, 8);
   p.x_pitch = (int64_t)p.groups * (f32 ? 32 : 16);
-  p.relay_w = f32 || in_f % 8 != 0;
+  p.few = !grads && part <= kFewRows;
+  p.relay_w = !p.few && (f32 || in_f % 8 != 0);
   p.tile_z = tile_of(classes, part), p.tile_dx = tile_of(in_f, part), p.tile_dw = tile_of(in_f, classes);
-  p.stat_tiles = (int)ceil_div(classes, 16 * (f32 ? TileFloat::TA : p.tile_z == 256 ? TileLarge::TA : TileSmall::TA));
+  p.stat_tiles = (int)ceil_div(classes, p.few ? kFewClasses : 16 * (f32 ? TileFloat::TA : p.tile_z == 256 ? TileLarge::TA : TileSmall::TA));
   const int slabs = (int)ceil_div(classes, 32);
   p.splits = 1, p.slabs_per_split = slabs;
   const int64_t tiles = f32 ? ceil_div(in_f, TileFloat::BA) * ceil_div(part, TileFloat::BB) : ceil_div(in_f, p.tile_dx) * ceil_div(part, p.tile_dx);
@@ -495,11 +616,11 @@ static LossPlan loss_plan(bool f32, int part, int batch, int in_f, int classes, 
     at += (bytes + 255) & ~(size_t)255;
     return here;
   };
-  p.x = take((size_t)part * p.x_pitch);
+  p.x = take(p.few ? 0 : (size_t)part * p.x_pitch);
   p.w = take(p.relay_w ? (size_t)classes * p.x_pitch : 0);
-  p.down_x = take(f32 ? (size_t)part * 4 : 0), p.down_w = take(f32 ? (size_t)classes * 4 : 0);
+  p.down_x = take(f32 && !p.few ? (size_t)part * 4 : 0), p.down_w = take(f32 && !p.few ? (size_t)classes * 4 : 0);
   p.stats = take((size_t)p.stat_tiles * part * 8);
-  p.at_label = take((size_t)part * 4), p.lse = take((size_t)part * 4), p.each = take((size_t)batch * 4);
+  p.at_label = take((size_t)part * 4), p.softmax = take((size_t)part * 8), p.each = take((size_t)batch * 4);
   if (grads) {
     p.z = take((size_t)part * p.classes_pitch * 4);
     p.partial = take(p.splits > 1 ? (size_t)p.splits * part * in_f * 4 : 0);
@@ -511,7 +632,7 @@ static LossPlan loss_plan(bool f32, int part, int batch, int in_f, int classes, 
 
 // The samples in equal parts of whole tiles, the fewest that keep a part's logits (without gradients: its statistics) within `most`.
 static LossPlan loss_plan_within(bool f32, size_t most, int batch, int in_f, int classes, bool grads) {
-  const LossPlan one = loss_plan(f32, 64, 64, in_f, classes, grads);
+  const LossPlan one = loss_plan(f32, 64, batch, in_f, classes, grads);
   const size_t row = grads ? (size_t)one.classes_pitch * 4 : (size_t)one.x_pitch + (size_t)one.stat_tiles * 8;
   const int64_t fit = std::max<int64_t>(64, std::min<int64_t>((int64_t)(most / row), kMostSamples) / 64 * 64), parts = ceil_div(batch, fit);
   int64_t part = ceil_div(batch, parts);
@@ -562,7 +683,7 @@ static vcnn_status loss_products(LossPlan p, int batch, int in_f, int classes, c
   char* const ws = (char*)workspace;
   LossMeta* const meta = (LossMeta*)ws;
   float* const each = sample_loss ? sample_loss : (float*)(ws + p.each);
-  float* const lse = (float*)(ws + p.lse);
+  float2* const softmax = (float2*)(ws + p.softmax);
   float* const z = grads ? (float*)(ws + p.z) : nullptr;
   float* const down_x = F32 ? (float*)(ws + p.down_x) : nullptr;
   float* const down_w = F32 ? (float*)(ws + p.down_w) : nullptr;
@@ -571,7 +692,7 @@ static vcnn_status loss_products(LossPlan p, int batch, int in_f, int classes, c
   for (int64_t b0 = 0; b0 < batch; b0 += p.part) {
     const int rows = (int)std::min<int64_t>(p.part, batch - b0);
     const int32_t* const lab = labels + b0;
-    if (grads || F32) {
+    if (grads || (F32 && !p.few)) {
       hipLaunchKernelGGL(loss_meta_kernel, dim3(1), dim3(1024), 0, st, labels, batch, ignore, b0 == 0, meta);
       if (vcnn_status s = check_launch("fc_softmax_loss count")) return s;
     }
@@ -579,21 +700,30 @@ static vcnn_status loss_products(LossPlan p, int batch, int in_f, int classes, c
       weights = ws + p.w;
       if (vcnn_status s = relay(w, ws + p.w, p, classes, in_f, nullptr, 0, down_w, &meta->most[1], st)) return s;
     }
-    if (vcnn_status s = relay(x + b0 * in_f, xs, p, rows, in_f, grads || F32 ? lab : nullptr, ignore, down_x, &meta->most[0], st)) return s;
+    // (the cost alone reads x where it stands if its rows have whole groups)
+    const bool as_it_is = !F32 && !grads && in_f % 8 == 0 && (reinterpret_cast<uintptr_t>(x) & 15) == 0;
+    if (!as_it_is && !p.few)
+      if (vcnn_status s = relay(x + b0 * in_f, xs, p, rows, in_f, grads || F32 ? lab : nullptr, ignore, down_x, &meta->most[0], st)) return s;
     LossProduct l{};
-    l.p.a = {weights, p.x_pitch, classes}, l.p.b = {xs, p.x_pitch, rows};
+    l.p.a = {weights, p.x_pitch, classes}, l.p.b = {as_it_is ? (const char*)(x + b0 * in_f) : xs, p.x_pitch, rows};
     l.p.k = F32 ? in_f : p.groups * 8, l.p.slabs_per_split = (int)ceil_div(l.p.k, 32);
     l.rows = rows, l.cols = classes, l.z = z, l.z_pitch = p.classes_pitch, l.bias = bias, l.labels = lab;
     l.stats = (float2*)(ws + p.stats), l.at_label = (float*)(ws + p.at_label);
     l.meta = meta, l.down_a = down_w, l.down_b = down_x;
-    if (vcnn_status s = launch_product<EPI_LOGITS, true, true>(F32, p.tile_z, l, 1, st)) return s;
-    hipLaunchKernelGGL(loss_rows_kernel, dim3((unsigned)ceil_div(rows, 16)), dim3(kThreads), 0, st, l.stats, p.stat_tiles, rows, classes,
-                       lab, ignore, l.at_label, lse, each + b0);
+    const dim3 few_grid((unsigned)p.stat_tiles);
+    if (p.few && rows <= 16) hipLaunchKernelGGL((loss_few_kernel<T, 1>), few_grid, dim3(kFewThreads), 0, st, l, x + b0 * in_f, w, in_f);
+    else if (p.few && rows <= 32) hipLaunchKernelGGL((loss_few_kernel<T, 2>), few_grid, dim3(kFewThreads), 0, st, l, x + b0 * in_f, w, in_f);
+    else if (p.few) hipLaunchKernelGGL((loss_few_kernel<T, 4>), few_grid, dim3(kFewThreads), 0, st, l, x + b0 * in_f, w, in_f);
+    else if (vcnn_status s = launch_product<EPI_LOGITS, true, true>(F32, p.tile_z, l, 1, st)) return s;
+    const LossRows r{l.stats, p.stat_tiles, rows, classes, lab, ignore, l.at_label, grads ? softmax : nullptr, each + b0,
+                     batch <= kFewRows ? loss : nullptr};
+    if (rows <= kFewRows) hipLaunchKernelGGL(loss_few_rows_kernel, dim3(1), dim3(1024), 0, st, r);
+    else hipLaunchKernelGGL(loss_rows_kernel, dim3((unsigned)ceil_div(rows, 16)), dim3(kThreads), 0, st, r);
     if (vcnn_status s = check_launch("fc_softmax_loss rows")) return s;
     if (!grads) continue;
     float* const shares = dbias ? (float*)(ws + p.shares) : nullptr;
     hipLaunchKernelGGL(loss_grad_kernel<F32>, dim3((unsigned)(p.classes_pitch / 64), (unsigned)ceil_div(rows, 64)), dim3(kThreads), 0, st, z,
-                       p.classes_pitch, rows, classes, lab, ignore, lse, down_x, down_w, shares, p.classes_pitch);
+                       p.classes_pitch, rows, classes, lab, ignore, softmax, down_x, down_w, shares, p.classes_pitch);
     if (vcnn_status s = check_launch("fc_softmax_loss gradient")) return s;
     const int64_t z_pitch = (int64_t)p.classes_pitch * 4;
     if (dx) {
@@ -623,26 +753,23 @@ static vcnn_status loss_products(LossPlan p, int batch, int in_f, int classes, c
       if (vcnn_status s = check_launch("fc_softmax_loss bias")) return s;
     }
   }
+  if (batch <= kFewRows) return VCNN_OK;
   hipLaunchKernelGGL(loss_mean_kernel, dim3(1), dim3(1024), 0, st, each, labels, ignore, batch, loss);
   return check_launch("fc_softmax_loss mean");
 }
 
 // ---- small float layers --------------------------------------------------------------------------------------------------
-// x with zeros for the samples that do not count.
-__global__ __launch_bounds__(kThreads) void loss_float_rows_kernel(const float* x, float* to, int64_t count, int cols,
-                                                                   const int32_t* labels, int ignore) {
-  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < count; i += (int64_t)gridDim.x * kThreads)
-    to[i] = labels[i / cols] != ignore ? x[i] : 0.f;
-}
-
-// A block a sample: z to d / C where it stands, and what the sample costs.
+// A block a sample: z to d / C where it stands, what the sample costs, and its x, zeros if it does not count (whatever it holds must not
+// meet the zeros of d as a NaN).
 __global__ __launch_bounds__(kThreads) void loss_float_kernel(float* z, int classes, const int32_t* labels, int ignore,
-                                                              int batch, int grads, float* each) {
+                                                              int batch, int grads, float* each, const float* x, float* x_to, int in_f) {
   __shared__ float parts[kThreads / 64];
   __shared__ int counts[kThreads / 64];
   const int b = blockIdx.x, label = labels[b];
   float* const row = z + (int64_t)b * classes;
   const bool counted = label != ignore, good = label >= 0 && label < classes;
+  if (x_to)
+    for (int64_t i = (int64_t)b * in_f + threadIdx.x; i < (int64_t)(b + 1) * in_f; i += kThreads) x_to[i] = counted ? x[i] : 0.f;
   float most = -__builtin_inff();
   for (int c = threadIdx.x; c < classes; c += kThreads) most = fmaxf(most, row[c]);
 #pragma unroll
@@ -698,6 +825,7 @@ static LossFloatPlan loss_float_plan(int batch, int in_f, int classes, bool grad
 
 // Small float layers by the float products, whole: d is made of finished logits there.
 static bool loss_is_small(int64_t batch, int64_t in_f, int64_t classes, bool grads) {
+  if (!grads && batch <= kFewRows) return false;
   return batch * classes <= (int64_t)1 << 24 && batch * in_f * classes <= (int64_t)1 << 27;
 }
 
@@ -710,15 +838,10 @@ static vcnn_status loss_float(int batch, int in_f, int classes, const float* x, 
   float* const each = sample_loss ? sample_loss : (float*)(ws + p.each);
   float* const z = (float*)(ws + p.z);
   if (vcnn_status s = vcnn_fc_fwd(VCNN_F32, batch, in_f, classes, VCNN_ACT_NONE, x, w, bias, z, st)) return s;
-  hipLaunchKernelGGL(loss_float_kernel, dim3((unsigned)batch), dim3(kThreads), 0, st, z, classes, labels, ignore, batch, (int)grads, each);
+  hipLaunchKernelGGL(loss_float_kernel, dim3((unsigned)batch), dim3(kThreads), 0, st, z, classes, labels, ignore, batch, (int)grads, each,
+                     x, dw ? (float*)(ws + p.x) : nullptr, in_f);
   if (vcnn_status s = check_launch("fc_softmax_loss rows")) return s;
-  if (dw) {
-    const int64_t count = (int64_t)batch * in_f;
-    hipLaunchKernelGGL(loss_float_rows_kernel, dim3((unsigned)std::min<int64_t>(ceil_div(count, kThreads), 256 * 16)), dim3(kThreads),
-                       0, st, x, (float*)(ws + p.x), count, in_f, labels, ignore);
-    if (vcnn_status s = check_launch("fc_softmax_loss rows of x")) return s;
-    x = (const float*)(ws + p.x);
-  }
+  if (dw) x = (const float*)(ws + p.x);
   if (grads)
     if (vcnn_status s = vcnn_fc_bwd(VCNN_F32, batch, in_f, classes, x, w, z, dw, dbias, dx, st)) return s;
   hipLaunchKernelGGL(loss_mean_kernel, dim3(1), dim3(1024), 0, st, each, labels, ignore, batch, loss);

@@ -16,7 +16,10 @@ import numpy as np
 import torch
 
 from . import vcnn
-from .workloads import FC, Conv, Net, Norm, Pool
+from .workloads import FC, Conv, Dropout, LayerNorm, Net, Norm, Pool
+
+
+IGNORE = -1  # label of a sample that does not count in a fused cost
 
 
 class TrainStep:
@@ -24,12 +27,15 @@ class TrainStep:
 
     def __init__(self, net: Net, params: list, inputs: dict, device: str = "cuda:0", first_layer_dx: bool = False,
                  dtype: int = vcnn.F32, overlap: bool = True, algos: Optional[dict] = None, fold_conv_act: bool = True,
-                 muon: Optional[dict] = None):
+                 muon: Optional[dict] = None, seed: int = 0, fused_cost: bool = False):
         """algos: {layer index: vcnn.ALGO_*} - convolutions named there are planned and launched under that route
         choice, the others under the process-wide one.  fold_conv_act=False: convolutions store their plain input
         gradient and the ReLU derivative of the layer below is a pass of its own (for comparisons).
         muon: the weight matrices (a convolution's kernels as the rows of one) are moved by vcnn.muon_update_multi, biases
-        and gains by SGD with the net's rate; a dict with any of lr, momentum, nesterov, weight_decay, steps."""
+        and gains by SGD with the net's rate; a dict with any of lr, momentum, nesterov, weight_decay, steps.
+        seed: of the dropout layers' generator, whose step counts the training steps.
+        fused_cost: a softmax network's last layer and cost are one call that keeps no logits and gives their gradients at once
+        (the last entry of acts is then not computed); samples with the label IGNORE do not count."""
         self.net, self.dev, self.dtype = net, torch.device(device), dtype
         self.fold_conv_act = fold_conv_act
         self.algos = dict(algos or {})
@@ -50,9 +56,16 @@ class TrainStep:
             None if p is None else tuple(torch.from_numpy(t).to(self.dev) for t in p) for p in params]
         self.grads = [None if p is None else tuple(torch.empty_like(t) for t in p) for p in self.params]
         # bf16 variant: fp32 master weights plus a bf16 copy refreshed after every update
-        self.params16 = [None if p is None or len(p) == 1 or dtype != vcnn.BF16 else torch.empty(p[0].shape, **act)
-                         for p in self.params]  # (a norm's gain is read as float)
-        self.rstd = {li: torch.empty(net.batch, **f32) for li, L in enumerate(net.layers) if isinstance(L, Norm)}
+        self.params16 = [torch.empty(p[0].shape, **act) if dtype == vcnn.BF16 and self.has_matrix(li) else None
+                         for li, p in enumerate(self.params)]  # (a norm's gain and bias are read as float)
+        self.rstd = {li: torch.empty(net.batch, **f32) for li, L in enumerate(net.layers) if isinstance(L, (Norm, LayerNorm))}
+        self.mean = {li: torch.empty(net.batch, **f32) for li, L in enumerate(net.layers) if isinstance(L, LayerNorm)}
+        self.rng = None  # of the dropout layers: seed, step
+        if any(isinstance(L, Dropout) for L in net.layers):
+            self.rng = torch.tensor([seed, 0], dtype=torch.int64, device=self.dev)
+        self.fused_cost = fused_cost
+        if fused_cost and not (net.loss == "softmax" and isinstance(net.layers[-1], FC) and not net.layers[-1].relu):
+            raise ValueError("a fused cost needs a softmax network that ends in a fully connected layer without an activation")
         self.acts = [self.x] + [torch.empty(s, **act) for s in net.shapes]
         self.dacts = [torch.empty_like(a) for a in self.acts]
         self.argmax = {li: torch.empty(net.shapes[li], dtype=torch.int32, device=self.dev)
@@ -75,6 +88,10 @@ class TrainStep:
                                                 L.stride, dtype=dtype)
             elif isinstance(L, Norm):
                 ws_bytes = max(ws_bytes, vcnn.rmsnorm_workspace_bytes(*self._rows_cols(li)))
+            elif isinstance(L, LayerNorm):
+                ws_bytes = max(ws_bytes, vcnn.layernorm_workspace_bytes(*self._rows_cols(li)))
+            elif fused_cost and li == len(net.layers) - 1:
+                ws_bytes = max(ws_bytes, vcnn.fc_softmax_loss_workspace_bytes(dtype, *self._rows_cols(li), L.out, True))
             if getattr(L, "relu", False):  # gradient w.r.t. the pre-activation, read by both strands
                 self.dpre[li] = torch.empty(net.shapes[li], **act)
             # (a first layer's kernel gradient has no input gradient to overlap with and runs on the main stream)
@@ -91,7 +108,7 @@ class TrainStep:
             self.muon = dict(dict(lr=0.02, momentum=0.95, nesterov=True, weight_decay=0.0, steps=5), **muon)
             if len(self.muon) != 5:
                 raise ValueError(f"unknown settings of the Muon update: {sorted(muon)}")
-            self.momenta = {li: torch.zeros_like(p[0]) for li, p in enumerate(self.params) if p is not None and len(p) == 2}
+            self.momenta = {li: torch.zeros_like(p[0]) for li, p in enumerate(self.params) if self.has_matrix(li)}
             ws_bytes = max(ws_bytes, vcnn.muon_workspace_bytes([m.shape for m in self.momenta.values()]))
         self.workspace = torch.empty(max(ws_bytes, 256), dtype=torch.uint8, device=self.dev)
         self.workspace_side = torch.empty(max(ws_side_bytes, 256), dtype=torch.uint8, device=self.dev)
@@ -99,6 +116,10 @@ class TrainStep:
             self.logits32 = torch.empty(net.out_shape, **f32)
             self.dlogits32 = torch.empty(net.out_shape, **f32)
         self.refresh_weights()
+
+    def has_matrix(self, li):
+        """True if layer li has a weight tensor (kernels or a matrix), rather than a norm's gain, or nothing."""
+        return isinstance(self.net.layers[li], (Conv, FC))
 
     def weights(self, li):
         """The weight tensor the layer kernels read: the fp32 parameters, or their bf16 copy."""
@@ -111,9 +132,10 @@ class TrainStep:
                     vcnn.f32_to_bf16(p[0].numel(), p[0], p16, stream)
 
     def snapshot(self):
-        """Keeps a device copy of the current parameters (and momenta) for restore()."""
+        """Keeps a device copy of the current parameters (and momenta, and dropout's generator) for restore()."""
         self._saved = [None if p is None else tuple(t.clone() for t in p) for p in self.params]
         self._saved_momenta = {li: m.clone() for li, m in self.momenta.items()} if self.muon else {}
+        self._saved_rng = None if self.rng is None else self.rng.clone()
 
     def restore(self, stream=None):
         """Puts the parameters of the last snapshot() back (device-to-device copies, no arithmetic) and refreshes the
@@ -124,6 +146,8 @@ class TrainStep:
                     t.copy_(u, non_blocking=True)
         for li, m in self._saved_momenta.items():
             self.momenta[li].copy_(m, non_blocking=True)
+        if self._saved_rng is not None:
+            self.rng.copy_(self._saved_rng, non_blocking=True)
         self.refresh_weights(stream)
 
     def folds(self, li):
@@ -137,6 +161,16 @@ class TrainStep:
         """Samples, and features of a sample, at the input of layer li."""
         shape = self.net.in_shape(li)
         return shape[0], int(np.prod(shape[1:]))
+
+    def _dropped_before(self, li):
+        """(rate, site, dropout's layer) of the dropout that layer li, a layer norm, takes into its own passes; rate 0: none."""
+        below = self.net.layers[li - 1] if li > 0 else None
+        return (below.p, li - 1, li - 1) if isinstance(below, Dropout) else (0.0, 0, None)
+
+    def _in_next(self, li):
+        """True if layer li is a dropout that the layer norm above it takes into its own passes."""
+        return isinstance(self.net.layers[li], Dropout) and li + 1 < len(self.net.layers) and \
+            isinstance(self.net.layers[li + 1], LayerNorm)
 
     def _routed(self, li, call):
         """call() under the route choice given for layer li (the process-wide choice is put back afterwards)."""
@@ -165,6 +199,16 @@ class TrainStep:
             elif isinstance(L, Norm):
                 vcnn.rmsnorm_fwd(self.dtype, *self._rows_cols(li), L.eps, a_in, None, self.params[li][0], None, a_out,
                                  self.rstd[li], stream)
+            elif isinstance(L, Dropout):
+                if not self._in_next(li):
+                    vcnn.dropout_fwd(self.dtype, *self._rows_cols(li), L.p, self.rng, li, a_in, None, a_out, stream)
+            elif isinstance(L, LayerNorm):
+                p, site, below = self._dropped_before(li)
+                x, h = (a_in, None) if below is None else (self.acts[below], a_in)
+                vcnn.layernorm_fwd(self.dtype, *self._rows_cols(li), L.eps, p, self.rng, site, x, None, *self.params[li], h, a_out,
+                                   self.mean[li], self.rstd[li], stream)
+            elif self.fused_cost and li == len(net.layers) - 1:
+                pass  # (in cost())
             else:
                 w, b = self.weights(li), self.params[li][1]
                 bsz = a_in.shape[0]
@@ -174,7 +218,13 @@ class TrainStep:
     def cost(self, stream=None):
         net, out, dout = self.net, self.acts[-1], self.dacts[-1]
         stream = torch.cuda.current_stream() if stream is None else stream
-        if net.loss == "softmax" and self.dtype == vcnn.BF16:
+        if self.fused_cost:
+            li = len(net.layers) - 1
+            dw, db = self.grads[li]
+            vcnn.fc_softmax_loss(self.dtype, *self._rows_cols(li), net.layers[li].out, self.acts[li], self.weights(li),
+                                 self.params[li][1], self.labels, IGNORE, self.loss, None,
+                                 self.dacts[li] if li > 0 or self.first_layer_dx else None, dw, db, self.workspace, stream)
+        elif net.loss == "softmax" and self.dtype == vcnn.BF16:
             vcnn.bf16_to_f32(out.numel(), out, self.logits32, stream)
             vcnn.softmax_loss(out.shape[0], out.shape[1], self.logits32, self.labels, self.loss, self.dlogits32, stream)
             vcnn.f32_to_bf16(out.numel(), self.dlogits32, dout, stream)
@@ -196,8 +246,10 @@ class TrainStep:
         side = self.side if self.side is not None else main
         joined = True   # nothing on the second stream yet
         folded = False  # the layer above already applied this layer's ReLU derivative and wrote dpre[li]
-        for li in range(len(net.layers) - 1, -1, -1):
+        for li in range(len(net.layers) - (2 if self.fused_cost else 1), -1, -1):
             L = net.layers[li]
+            if self._in_next(li):  # done by the layer norm above
+                continue
             a_in, a_out, d = self.acts[li], self.acts[li + 1], self.dacts[li + 1]
             need_dx = li > 0 or self.first_layer_dx
             if getattr(L, "relu", False):
@@ -216,6 +268,17 @@ class TrainStep:
             if isinstance(L, Norm):
                 vcnn.rmsnorm_bwd(self.dtype, *self._rows_cols(li), a_in, self.params[li][0], self.rstd[li], d, None,
                                  dx_out if need_dx else None, self.grads[li][0], self.workspace, main)
+                continue
+            if isinstance(L, Dropout):
+                if need_dx:
+                    vcnn.dropout_bwd(self.dtype, *self._rows_cols(li), L.p, self.rng, li, d, dx_out, main)
+                continue
+            if isinstance(L, LayerNorm):
+                p, site, below = self._dropped_before(li)
+                need_below = below is not None and (below > 0 or self.first_layer_dx)
+                vcnn.layernorm_bwd(self.dtype, *self._rows_cols(li), p, self.rng, site, a_in, self.params[li][0], self.mean[li],
+                                   self.rstd[li], d, None, dx_out if need_dx else None, self.dacts[below] if need_below else None,
+                                   *self.grads[li], self.workspace, main)
                 continue
             w = self.weights(li)
             dw, db = self.grads[li]
@@ -246,15 +309,17 @@ class TrainStep:
         gs = [t for g in self.grads if g is not None for t in g]
         w16 = None
         if self.dtype == vcnn.BF16:  # the weights' bf16 working copies are refreshed by the same launch
-            w16 = [t for p, h in zip(self.params, self.params16) if p is not None for t in (h, None)[:len(p)]]
+            w16 = [t for p, h in zip(self.params, self.params16) if p is not None for t in (h, None)[:len(p)]]  # (h: None for norms)
         if self.muon is not None:
             o, at = self.muon, list(self.momenta)
             vcnn.muon_update_multi(o["lr"], o["momentum"], o["nesterov"], o["weight_decay"], o["steps"],
                                    [self.params[li][0] for li in at], [self.grads[li][0] for li in at],
                                    [self.momenta[li] for li in at], self.workspace,
                                    None if w16 is None else [self.params16[li] for li in at], stream)
-            rest = [p[-1] for p in self.params if p is not None]  # biases, gains
-            ws, gs, w16 = rest, [g[-1] for g in self.grads if g is not None], None
+            first = [1 if self.has_matrix(li) else 0 for li in range(len(self.params))]
+            ws, gs = ([t for f, p in zip(first, ps) if p is not None for t in p[f:]]  # biases, gains
+                      for ps in (self.params, self.grads))
+            w16 = None
         vcnn.sgd_update_multi(self.net.lr, ws, gs, w16, stream)
 
     def step(self, stream=None):
@@ -262,6 +327,8 @@ class TrainStep:
         self.cost(stream)
         self.backward(stream)
         self.update(stream)
+        if self.rng is not None:
+            vcnn.rng_advance(self.rng, stream)
 
     # ---- HIP graph ---------------------------------------------------------------------------------
     def capture(self):

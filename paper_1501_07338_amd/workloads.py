@@ -44,6 +44,18 @@ class Norm:
     eps: float = 1e-6
 
 
+@dataclass(frozen=True)
+class LayerNorm:
+    """Layer norm of each sample over all its features, with a learned gain and bias per feature."""
+    eps: float = 1e-5
+
+
+@dataclass(frozen=True)
+class Dropout:
+    """Each element of a training step's activations is kept with probability 1 - p and then divided by it."""
+    p: float = 0.5
+
+
 @dataclass
 class Net:
     name: str
@@ -176,7 +188,7 @@ def make_inputs(net: Net) -> dict:
 
 def make_params(net: Net) -> list:
     """He-normal weights (variance 2 / fan-in) and constant biases, one (w, b) pair per parametrised
-    layer (None for pooling layers, a gain of ones for a norm), fp32."""
+    layer (None for pooling and dropout, a gain of ones for a norm, and a bias of zeros beside it for a layer norm), fp32."""
     params = []
     pl = 0
     for li, L in enumerate(net.layers):
@@ -189,8 +201,10 @@ def make_params(net: Net) -> list:
             fan_in = int(np.prod(ishape[1:]))
             wshape = (L.out, fan_in)
             nout = L.out
-        elif isinstance(L, Norm):
-            params.append((np.ones(int(np.prod(ishape[1:])), dtype=np.float32),))
+        elif isinstance(L, (Norm, LayerNorm)):
+            features = int(np.prod(ishape[1:]))
+            both = (np.ones(features, dtype=np.float32), np.zeros(features, dtype=np.float32))
+            params.append(both if isinstance(L, LayerNorm) else both[:1])
             pl += 1
             continue
         else:

@@ -146,3 +146,117 @@ def test_unknown_settings_are_refused():
         dummy = TrainStep.__new__(TrainStep)
         net = normed()
         dummy.__init__(net, wl.make_params(net), inputs_of(net), device="cpu", overlap=False, muon=dict(rate=1.0))
+
+
+# ---- dropout, layer norm and a cost over many classes --------------------------------------------------------------------------
+def dropped(batch=24, classes=1203):
+    return wl.Net("dropped", 10, batch, (1, 14, 14),
+                  [wl.Conv(8, 3, 3, relu=True), wl.Pool(2, 2), wl.Dropout(0.25), wl.FC(96, relu=True), wl.Dropout(0.125),
+                   wl.LayerNorm(), wl.FC(136), wl.LayerNorm(), wl.FC(classes)],
+                  "softmax", classes=classes, lr=0.02)
+
+
+def many_labels(net, ignored):
+    rng = np.random.Generator(np.random.Philox(key=91))
+    labels = rng.integers(0, net.classes, net.batch).astype(np.int32)
+    if ignored:
+        labels[::5] = -1
+    return dict(x=rng.random((net.batch,) + net.in_chw).astype(np.float32), labels=labels)
+
+
+def dropped64(net, params, x, step, seed):
+    from test_gpu_dropout import factors
+    a = x
+    for li, (L, p) in enumerate(zip(net.layers, params)):
+        flat = a.reshape(a.shape[0], -1)
+        if isinstance(L, wl.Dropout):
+            a = (flat * factors(*flat.shape, L.p, seed, step, li)).reshape(a.shape)
+        elif isinstance(L, wl.LayerNorm):
+            a = F.layer_norm(flat, flat.shape[1:], p[0], p[1], L.eps).reshape(a.shape)
+        elif isinstance(L, wl.Pool):
+            a = F.max_pool2d(a, L.win, L.stride)
+        else:
+            a = F.conv2d(a, *p) if isinstance(L, wl.Conv) else F.linear(flat, *p)
+            a = a.relu() if L.relu else a
+    return a
+
+
+def test_shapes_and_parameters_of_dropout_and_layer_norm():
+    net = dropped()
+    assert net.shapes[2] == net.shapes[1] and net.shapes[-1] == (24, 1203)
+    p = wl.make_params(net)
+    assert p[2] is None and p[4] is None and [t.shape for t in p[5]] == [(96,), (96,)]
+    assert np.all(p[5][0] == 1.0) and np.all(p[5][1] == 0.0) and p[6][0].shape == (136, 96)
+
+
+def test_a_fused_cost_needs_its_last_layer():
+    net = wl.Net("squares", 11, 4, (1, 6, 6), [wl.FC(3)], "l2")
+    with pytest.raises(ValueError):
+        TrainStep(net, wl.make_params(net), dict(x=np.zeros((4, 1, 6, 6), np.float32)), device="cpu", overlap=False, fused_cost=True)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fused", [False, True])
+@pytest.mark.parametrize("captured", [False, True])
+@pytest.mark.parametrize("muon", [None, dict(lr=0.0, momentum=0.5)])
+def test_dropout_layer_norm_and_many_classes_against_64_bits(fused, captured, muon):
+    """Three steps, other elements dropped in each.  (muon: biases and gains keep SGD; with a rate of 0 the matrices stay.)"""
+    net, seed = dropped(), 77
+    inputs, params = many_labels(net, fused), wl.make_params(net)
+    ts = TrainStep(net, params, inputs, first_layer_dx=True, seed=seed, fused_cost=fused, muon=muon)
+    ps = [None if p is None else [torch.from_numpy(t).double() for t in p] for p in params]
+    x, labels = torch.from_numpy(inputs["x"]).double(), torch.from_numpy(inputs["labels"]).long()
+    if captured:
+        ts.snapshot()
+        graph = ts.capture()  # (runs a step by itself)
+        torch.cuda.synchronize()
+        ts.restore()
+    for step in range(3):
+        for p in ps:
+            for t in p or ():
+                t.requires_grad_(True)
+        x.requires_grad_(True)
+        loss = F.cross_entropy(dropped64(net, ps, x, step, seed), labels, ignore_index=-1)
+        grads = torch.autograd.grad(loss, [x] + [t for p in ps for t in p or ()])
+        if captured:
+            graph.replay()
+        else:
+            ts.step()
+        torch.cuda.synchronize()
+        assert ts.rng.tolist() == [seed, step + 1]
+        assert abs(float(ts.loss) - float(loss.detach())) <= TOL_F32 * float(loss.detach())
+        got = [ts.dacts[0]] + [t for g in ts.grads if g is not None for t in g]
+        for a, b in zip(got, grads):
+            assert rel_err(a.cpu().numpy(), b.numpy()) <= TOL_F32
+        it = iter(grads[1:])
+        for li, p in enumerate(ps):
+            if p is not None:
+                stay = muon is not None and isinstance(net.layers[li], (wl.Conv, wl.FC))
+                ps[li] = [t.detach() - (0.0 if stay and n == 0 else net.lr) * next(it) for n, t in enumerate(p)]
+    for a, b in zip(ts.params, ps):
+        for t, u in zip(a or (), b or ()):
+            assert rel_err(t.cpu().numpy(), u.detach().numpy()) <= TOL_F32
+
+
+@pytest.mark.gpu
+def test_bf16_chain_with_dropout_layer_norm_and_many_classes():
+    net = dropped(batch=70)
+    inputs = many_labels(net, True)
+    ts = TrainStep(net, wl.make_params(net), inputs, dtype=vcnn.BF16, fused_cost=True, seed=5, overlap=False)
+    graph = ts.capture()
+    for _ in range(2):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert bool(torch.isfinite(ts.loss))
+    # the last layer from the input that it stored, as the last step's weights were
+    li = len(net.layers) - 1
+    w = ts.params[li][0].double() + net.lr * ts.grads[li][0].double()
+    b = ts.params[li][1].double() + net.lr * ts.grads[li][1].double()
+    z = ts.acts[li].double() @ w.to(torch.bfloat16).double().t().contiguous() + b
+    want = F.cross_entropy(z, ts.labels.long(), ignore_index=-1)
+    # (the weights come back from a step of SGD with roundings of 2^-24, and may round to another bfloat16: 2^-8 of one product
+    # in each of few sums)
+    assert abs(float(ts.loss) - float(want)) <= 1e-3 * float(want)
+    for p, h in zip(ts.params, ts.params16):
+        if h is not None:
+            assert torch.equal(p[0].to(torch.bfloat16), h)

@@ -42,20 +42,43 @@ __device__ __forceinline__ uint4 philox(const DropoutKey& key, uint64_t block) {
 // Blocks of eight elements in a row.
 __host__ __device__ __forceinline__ uint32_t dropout_blocks(int cols) { return ((uint32_t)cols + 7) / 8; }
 
-// The bits of elements c .. c + N of a row (N 4 or 8, c a multiple of N), the row's first block being `first`.
-template <int N>
-__device__ __forceinline__ void dropout_bits(const DropoutKey& key, uint64_t first, int c, uint32_t (&bits)[N]) {
-  const uint4 r = philox(key, first + (uint32_t)(c >> 3));
+// The random words of a thread's groups of N elements (4 or 8) in a row, two elements a word: group k starts at element
+// (k * per_row + tid) * N (per_row even), the row's first block is `first`.  Groups of four: two neighbouring lanes share a block,
+// so of two groups each makes one block and hands the other lane its half.  All lanes of the wave take part.
+template <int N, int K>
+__device__ __forceinline__ void dropout_words(const DropoutKey& key, uint64_t first, int per_row, int tid, uint32_t (&words)[K][N / 2]) {
   if constexpr (N == 8) {
-    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) bits[2 * i] = w[i] & 0xffffu, bits[2 * i + 1] = w[i] >> 16;
+    for (int k = 0; k < K; ++k) {
+      const uint4 r = philox(key, first + (uint32_t)(k * per_row + tid));
+      words[k][0] = r.x, words[k][1] = r.y, words[k][2] = r.z, words[k][3] = r.w;
+    }
   } else {
-    const uint32_t w[2] = {c & 4 ? r.z : r.x, c & 4 ? r.w : r.y};
+    const bool odd = tid & 1;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) bits[2 * i] = w[i] & 0xffffu, bits[2 * i + 1] = w[i] >> 16;
+    for (int k = 0; k < K; k += 2) {
+      if (k + 1 < K) {
+        const uint4 r = philox(key, first + (uint32_t)(((k + (odd ? 1 : 0)) * per_row + tid) >> 1));
+        const uint32_t u = __shfl_xor(odd ? r.x : r.z, 1), v = __shfl_xor(odd ? r.y : r.w, 1);
+        words[k][0] = odd ? u : r.x, words[k][1] = odd ? v : r.y;
+        words[k + 1][0] = odd ? r.z : u, words[k + 1][1] = odd ? r.w : v;
+      } else {
+        const uint4 r = philox(key, first + (uint32_t)((k * per_row + tid) >> 1));
+        words[k][0] = odd ? r.z : r.x, words[k][1] = odd ? r.w : r.y;
+      }
+    }
   }
 }
+// Those of one group at element c (a multiple of N).
+template <int N>
+__device__ __forceinline__ void dropout_words(const DropoutKey& key, uint64_t first, int c, uint32_t (&words)[N / 2]) {
+  const uint4 r = philox(key, first + (uint32_t)(c >> 3));
+  if constexpr (N == 8) words[0] = r.x, words[1] = r.y, words[2] = r.z, words[3] = r.w;
+  else words[0] = c & 4 ? r.z : r.x, words[1] = c & 4 ? r.w : r.y;
+}
+// Element i's 16 bits of its group's words.
+template <int W>
+__device__ __forceinline__ uint32_t bits_of(const uint32_t (&words)[W], int i) { return i & 1 ? words[i / 2] >> 16 : words[i / 2] & 0xffffu; }
 
 // A kept element (one that is not is replaced, so that an infinity there leaves no NaN), and the residual with one rounding.
 __device__ __forceinline__ float dropped(float v, uint32_t bits, const Dropout& d) { return bits >= d.limit ? v * d.scale : 0.f; }

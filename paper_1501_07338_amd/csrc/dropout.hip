@@ -38,8 +38,8 @@ __global__ __launch_bounds__(kDropoutThreads) void dropout_kernel(DropoutArgs a)
         px[g] = load_group(x, c + g * N, a.cols);
         if (ADDED) pr[g] = load_group(res, c + g * N, a.cols);
       }
-    uint32_t bits[8];
-    dropout_bits(key, block, 0, bits);
+    uint32_t words[4];
+    dropout_words<8>(key, block, 0, words);
 #pragma unroll
     for (int g = 0; g < G; ++g) {
       if (g > 0 && c + g * N >= a.cols) break;
@@ -49,10 +49,10 @@ __global__ __launch_bounds__(kDropoutThreads) void dropout_kernel(DropoutArgs a)
         float w[N];
         unpack(pr[g], w);
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = dropped(v[i], bits[g * N + i], a.drop, w[i]);
+        for (int i = 0; i < N; ++i) v[i] = dropped(v[i], bits_of(words, g * N + i), a.drop, w[i]);
       } else {
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = dropped(v[i], bits[g * N + i], a.drop);
+        for (int i = 0; i < N; ++i) v[i] = dropped(v[i], bits_of(words, g * N + i), a.drop);
       }
       store_group(reinterpret_cast<T*>(a.y) + at, c + g * N, a.cols, pack(v));
     }

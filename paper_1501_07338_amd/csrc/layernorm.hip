@@ -97,19 +97,17 @@ __global__ __launch_bounds__(WAVE ? kWaveThreads : NV ? kKeptThreads : 1024, NV 
     T* const h = reinterpret_cast<T*>(a.h) + row * cols;
     T* const y = reinterpret_cast<T*>(a.y) + row * cols;
     // the group at c, dropped, the residual added, and the sum stored
-    auto take = [&](int c, const Loose16& gx, const Loose16& gr, float (&v)[N]) {
+    auto take = [&](int c, const Loose16& gx, const Loose16& gr, const uint32_t (&words)[N / 2], float (&v)[N]) {
       unpack(gx, v);
       if (!stored) return;
-      uint32_t bits[N];
-      if constexpr (DROP) dropout_bits(key, (uint64_t)row * blocks, c, bits);
       if (residual) {
         float w[N];
         unpack(gr, w);
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = DROP ? dropped(v[i], bits[i], drop, w[i]) : v[i] + w[i];
+        for (int i = 0; i < N; ++i) v[i] = DROP ? dropped(v[i], bits_of(words, i), drop, w[i]) : v[i] + w[i];
       } else {
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = DROP ? dropped(v[i], bits[i], drop) : v[i];
+        for (int i = 0; i < N; ++i) v[i] = DROP ? dropped(v[i], bits_of(words, i), drop) : v[i];
       }
       const Loose16 ph = pack(v);
       unpack(ph, v);
@@ -137,11 +135,13 @@ __global__ __launch_bounds__(WAVE ? kWaveThreads : NV ? kKeptThreads : 1024, NV 
     bool again = false;
     if constexpr (NV > 0) {
       float sum = 0.f, zero = 0.f;
+      uint32_t words[K][N / 2];
+      if constexpr (DROP) dropout_words<N, K>(key, (uint64_t)row * blocks, per_row, tid, words);
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
         const int c = (k * per_row + tid) * N;
         if (c < cols) {
-          take(c, px[k], pr[k], v[k]);
+          take(c, px[k], pr[k], words[k], v[k]);
 #pragma unroll
           for (int i = 0; i < N; ++i) sum += v[k][i];  // (zeros behind the row's end)
         }
@@ -171,7 +171,9 @@ __global__ __launch_bounds__(WAVE ? kWaveThreads : NV ? kKeptThreads : 1024, NV 
       for (int c = tid * N; c < cols; c += per_row * N) {
         px[0] = load_group(x, c, cols);
         if (residual) pr[0] = load_group(reinterpret_cast<const T*>(a.residual) + row * cols, c, cols);
-        take(c, px[0], pr[0], v[0]);
+        uint32_t words[N / 2];
+        if constexpr (DROP) dropout_words<N>(key, (uint64_t)row * blocks, c, words);
+        take(c, px[0], pr[0], words, v[0]);
         if (count == 0) first = v[0][0];
 #pragma unroll
         for (int i = 0; i < N; ++i) {
@@ -266,7 +268,7 @@ struct LayerNormBwdArgs {
   Dropout drop;
 };
 
-static constexpr int kLnBwdBlocks = 512;
+static constexpr int kLnBwdBlocks = 512;  // (256: 4096 x 4096 of bfloat16 42.5 and 4.5 us, not 38.5 and 7.1; 2999 x 5003 of float 76.7 and 7.8, not 64.0 and 10.4)
 
 template <typename T, bool DROP, int NV, bool WAVE>
 __global__ __launch_bounds__(WAVE ? kWaveThreads : NV ? kKeptThreads : 1024) void layernorm_bwd_kernel(LayerNormBwdArgs a) {
@@ -349,7 +351,7 @@ __global__ __launch_bounds__(WAVE ? kWaveThreads : NV ? kKeptThreads : 1024) voi
       mt = (float)(st / cols), mtz = (float)(stz / cols);
     }
     if (!a.dh && !a.dx) continue;
-    auto give = [&](int c, const Loose16& gh, const Loose16& gd, const Loose16& ga, const float (&g)[N]) {
+    auto give = [&](int c, const Loose16& gh, const Loose16& gd, const Loose16& ga, const float (&g)[N], const uint32_t (&words)[N / 2]) {
       float hv[N], d[N], o[N];
       unpack(gh, hv), unpack(gd, d);
 #pragma unroll
@@ -363,24 +365,29 @@ __global__ __launch_bounds__(WAVE ? kWaveThreads : NV ? kKeptThreads : 1024) voi
       if (a.dh) store_group(reinterpret_cast<T*>(a.dh) + row * cols, c, cols, pack(o));
       if constexpr (DROP) {
         if (!a.dx) return;
-        uint32_t bits[N];
-        dropout_bits(key, (uint64_t)row * blocks, c, bits);
 #pragma unroll
-        for (int i = 0; i < N; ++i) o[i] = dropped(o[i], bits[i], drop);
+        for (int i = 0; i < N; ++i) o[i] = dropped(o[i], bits_of(words, i), drop);
         store_group(reinterpret_cast<T*>(a.dx) + row * cols, c, cols, pack(o));
       }
     };
     if constexpr (NV > 0) {
+      constexpr bool SHARE = DROP && K <= 4;  // (the registers)
+      uint32_t words[K][N / 2];
+      if constexpr (SHARE) dropout_words<N, K>(key, (uint64_t)row * blocks, per_row, tid, words);
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
         const int c = (k * per_row + tid) * N;
-        if (c < cols) give(c, ph[k], pd[k], pa[k], gain[k]);
+        if (c >= cols) continue;
+        if constexpr (DROP && !SHARE) dropout_words<N>(key, (uint64_t)row * blocks, c, words[k]);
+        give(c, ph[k], pd[k], pa[k], gain[k], words[k]);
       }
     } else {
       for (int c = tid * N; c < cols; c += per_row * N) {
         if (above) pa[0] = load_group(above, c, cols);
         load_gain(a.gain, c, cols, gain[0]);
-        give(c, load_group(h, c, cols), load_group(dy, c, cols), pa[0], gain[0]);
+        uint32_t words[N / 2];
+        if constexpr (DROP) dropout_words<N>(key, (uint64_t)row * blocks, c, words);
+        give(c, load_group(h, c, cols), load_group(dy, c, cols), pa[0], gain[0], words);
       }
     }
   }

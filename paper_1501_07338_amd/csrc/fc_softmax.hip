@@ -5,7 +5,7 @@
 // The samples go through in parts.  A part's logits are made once (z, float), by a product whose tiles leave the largest logit of
 // each sample and its sum of exponentials beside them; these are joined; one pass turns z where it stands into d, a high
 // and a low bfloat16 term of the difference, and two products make dx and dw from it.  Without gradients z is not stored at all.
-//   d in two terms: dw is float, and one bfloat16 term alone would leave 2^-9 of each element in it (the two leave 2^-18).  dx is
+//   d in two terms: dw is float, and one bfloat16 term alone would leave up to 2^-8 of each element in it (the two leave 2^-16).  dx is
 //   bfloat16 itself and takes the high term alone.
 //   float: x, w and d in two half-precision terms each (22 bits), products high x high, high x low and low x high, three
 //   where the float instruction would take sixteen.  x and w are scaled by a power of two a row so that its largest element comes to
@@ -166,7 +166,7 @@ struct LossProduct {
   float* at_label;
   // EPI_DX, EPI_DW
   const LossMeta* meta;
-  float* partial;        // [splits][rows][cols] (EPI_DX, shared sums)
+  float* partial;        // [splits][rows][cols] (shared sums)
   void* out;             // [rows][cols]
   int add;               // EPI_DW: to what is there
   // float: by how much the rows of a and b (EPI_LOGITS), or that of b, were scaled beyond the least
@@ -286,7 +286,7 @@ __global__ __launch_bounds__(TILE::THREADS, TILE::WAVES_SIMD) void loss_product_
         if (n <= 0) continue;
         const int64_t at = (int64_t)b * a.cols + c;
         float v[4];
-        if (EPI == EPI_DX && a.partial) {
+        if (a.partial) {
 #pragma unroll
           for (int q = 0; q < 4; ++q) v[q] = F32 ? acc[i][j][q] * least * up : acc[i][j][q];
           store4(a.partial + (int64_t)blockIdx.y * a.rows * a.cols + at, v, n);
@@ -310,28 +310,30 @@ __global__ __launch_bounds__(TILE::THREADS, TILE::WAVES_SIMD) void loss_product_
   }
 }
 
-// ---- few samples, the cost alone ------------------------------------------------------------------------------------------
-// Bandwidth: w is read once, where it stands.  A wave takes 16 classes and up to 16 NB samples and reads its operands as the matrix
-// instruction wants them, straight into registers: lane l row l % 16, and of every 128 bytes of it the 16 from 16 (l / 16) on and the 16
-// that are 64 further.  (Which steps of the sum a lane holds does not matter as long as it is the same ones of both.)  The eight waves
-// of a block leave one maximum and sum of their 128 classes.
-static constexpr int kFewThreads = 512, kFewClasses = 16 * kFewThreads / 64, kFewRows = 64;
+// ---- few samples -----------------------------------------------------------------------------------------------------------
+// Bandwidth: w is read once, where it stands.  A wave takes 16 MA classes and up to 16 NB samples and reads its operands as the matrix
+// instruction wants them, straight into registers: lane l row l % 16, and of every 64 bytes of it the 16 from 16 (l / 16) on.  (Which
+// steps of the sum a lane holds does not matter as long as it is the same ones of both.)  The eight waves of a block leave one maximum
+// and sum of their classes.
+static constexpr int kFewThreads = 512, kFewWaves = kFewThreads / 64, kFewRows = 64;
+constexpr int few_tiles(int rows, int64_t classes) { return rows > 16 && classes >= 16 * 2 * kFewWaves * 64 ? 2 : 1; }  // MA
 
-template <typename T, int NB>
+template <typename T, int MA, int NB>
 __global__ __launch_bounds__(kFewThreads) void loss_few_kernel(LossProduct a, const T* xs, const T* ws, int in_f) {
-  constexpr int AHEAD = 4, N = 16 / sizeof(T), STEP = 4 * N;  // elements of a load, and of a row's four
-  __shared__ float2 parts[kFewThreads / 64][NB * 16];
+  constexpr int AHEAD = MA * NB == 1 ? 8 : 4, N = 16 / sizeof(T), STEP = 4 * N;  // elements of a load, and of a row's four
+  __shared__ float2 parts[kFewWaves][NB * 16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, at = (lane >> 4) * N;
-  const int c0 = blockIdx.x * kFewClasses + wave * 16;
-  const T* const w = ws + (int64_t)min(c0 + row, a.cols - 1) * in_f;
-  const T* x[NB];
-  f32x4 acc[NB];
+  const int c0 = (blockIdx.x * kFewWaves + wave) * 16 * MA;
+  const T *w[MA], *x[NB];
+  f32x4 acc[MA][NB];
+#pragma unroll
+  for (int m = 0; m < MA; ++m) w[m] = ws + (int64_t)min(c0 + m * 16 + row, a.cols - 1) * in_f;
 #pragma unroll
   for (int n = 0; n < NB; ++n) {
     x[n] = xs + (int64_t)min(n * 16 + row, a.rows - 1) * in_f;
-    acc[n] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int m = 0; m < MA; ++m) acc[m][n] = (f32x4){0.f, 0.f, 0.f, 0.f};
   }
-  auto whole_group = [](const T* p) { return *reinterpret_cast<const Loose16*>(p); };
   auto multiply = [](const Loose16& p, const Loose16& q, f32x4 c) {
     if constexpr (sizeof(T) == 2) {
       return mfma_bf16(make_uint4(p.w[0], p.w[1], p.w[2], p.w[3]), make_uint4(q.w[0], q.w[1], q.w[2], q.w[3]), c);
@@ -342,42 +344,58 @@ __global__ __launch_bounds__(kFewThreads) void loss_few_kernel(LossProduct a, co
     }
   };
   int k = 0;
-  for (; k + AHEAD * 2 * STEP <= in_f; k += AHEAD * 2 * STEP) {
-    Loose16 fw[2 * AHEAD];
+  for (; k + AHEAD * STEP <= in_f; k += AHEAD * STEP) {
+    Loose16 fw[AHEAD][MA], fx[AHEAD][NB];
 #pragma unroll
-    for (int u = 0; u < 2 * AHEAD; ++u) fw[u] = whole_group(w + k + u * STEP + at);
+    for (int u = 0; u < AHEAD; ++u) {
 #pragma unroll
-    for (int u = 0; u < 2 * AHEAD; ++u)
+      for (int m = 0; m < MA; ++m) fw[u][m] = *reinterpret_cast<const Loose16*>(w[m] + k + u * STEP + at);
 #pragma unroll
-      for (int n = 0; n < NB; ++n) acc[n] = multiply(fw[u], whole_group(x[n] + k + u * STEP + at), acc[n]);
+      for (int n = 0; n < NB; ++n) fx[u][n] = *reinterpret_cast<const Loose16*>(x[n] + k + u * STEP + at);
+    }
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+      for (int m = 0; m < MA; ++m)
+#pragma unroll
+        for (int n = 0; n < NB; ++n) acc[m][n] = multiply(fw[u][m], fx[u][n], acc[m][n]);
   }
   for (; k < in_f; k += STEP) {
-    Loose16 fw{{0, 0, 0, 0}};
-    if (k + at < in_f) fw = load_group(w, k + at, in_f);
+    Loose16 fx[NB];
+    const bool in = k + at < in_f;
 #pragma unroll
-    for (int n = 0; n < NB; ++n) {
-      Loose16 fx{{0, 0, 0, 0}};
-      if (k + at < in_f) fx = load_group(x[n], k + at, in_f);
-      acc[n] = multiply(fw, fx, acc[n]);
+    for (int n = 0; n < NB; ++n) fx[n] = in ? load_group(x[n], k + at, in_f) : Loose16{{0, 0, 0, 0}};
+#pragma unroll
+    for (int m = 0; m < MA; ++m) {
+      const Loose16 fw = in ? load_group(w[m], k + at, in_f) : Loose16{{0, 0, 0, 0}};
+#pragma unroll
+      for (int n = 0; n < NB; ++n) acc[m][n] = multiply(fw, fx[n], acc[m][n]);
     }
   }
-  const int c = c0 + 4 * (lane >> 4);
 #pragma unroll
   for (int n = 0; n < NB; ++n) {
     const int b = n * 16 + row, label = a.labels[min(b, a.rows - 1)];
     float most = -__builtin_inff(), sum = 0.f;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      if (a.bias) acc[n][q] += a.bias[min(c + q, a.cols - 1)];
-      if (c + q < a.cols) most = fmaxf(most, acc[n][q]);
-      if (b < a.rows && c + q == label && label < a.cols) a.at_label[b] = acc[n][q];
+    for (int m = 0; m < MA; ++m) {
+      const int c = c0 + m * 16 + 4 * (lane >> 4);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        if (a.bias) acc[m][n][q] += a.bias[min(c + q, a.cols - 1)];
+        if (c + q < a.cols) most = fmaxf(most, acc[m][n][q]);
+        if (b < a.rows && c + q == label && label < a.cols) a.at_label[b] = acc[m][n][q];
+      }
+      if (a.z && b < a.rows && c < a.cols)  // (rows of z have whole groups)
+        *reinterpret_cast<float4*>(a.z + b * a.z_pitch + c) = make_float4(acc[m][n][0], acc[m][n][1], acc[m][n][2], acc[m][n][3]);
     }
     most = fmaxf(most, __shfl_xor(most, 16));
     most = fmaxf(most, __shfl_xor(most, 32));
     const float about = most > -__builtin_inff() ? most : 0.f;  // (none is possible, or all are NaN)
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-      if (c + q < a.cols) sum += exp_of(acc[n][q] - about);
+    for (int m = 0; m < MA; ++m)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (c0 + m * 16 + 4 * (lane >> 4) + q < a.cols) sum += exp_of(acc[m][n][q] - about);
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
     if (lane < 16) parts[wave][b] = make_float2(most, sum);
@@ -386,25 +404,146 @@ __global__ __launch_bounds__(kFewThreads) void loss_few_kernel(LossProduct a, co
   if (threadIdx.x >= NB * 16 || threadIdx.x >= a.rows) return;
   float2 total = parts[0][threadIdx.x];
 #pragma unroll
-  for (int v = 1; v < kFewThreads / 64; ++v) join(total, parts[v][threadIdx.x]);
+  for (int v = 1; v < kFewWaves; ++v) join(total, parts[v][threadIdx.x]);
   a.stats[(int64_t)blockIdx.x * a.rows + threadIdx.x] = total;
 }
 
-// dx from the shares of its sums, always in the same order.
+// Up to 16 samples, the gradients: w is read once more and dw written, and d is made of z on the way, in float throughout.  A wave takes
+// 256 inputs (four a lane) and, four at a time, every fourth of its block's classes; lane l makes the d of sample l % 16 and class l / 16
+// of the four, and every lane takes it from there for its share of
+//     dx[b] += d[b] w,   dw = sum over b of d[b] x[b]
+// The blocks' shares of dx are joined by loss_join_kernel.
+static constexpr int kFewGrad = 16;
+struct LossFewGrad {
+  const void* x;
+  const void* w;
+  const float* z;
+  int64_t z_pitch;
+  const float2* softmax;
+  const int32_t* labels;
+  int ignore, rows, in_f, classes, per_block;  // (classes of a block, a multiple of 16)
+  float* partial;  // [blocks][rows][in_f] (nullable: no dx)
+  float* dw;       // nullable
+  float* dbias;    // nullable
+};
+template <typename T>
+__device__ __forceinline__ void load4(const T* row, int c, int cols, float (&v)[4]) {
+  if (c + 4 <= cols) {
+    if constexpr (sizeof(T) == 4) {
+      const Loose16 p = *reinterpret_cast<const Loose16*>(row + c);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(p.w[i]);
+    } else {
+      const Loose8 p = *reinterpret_cast<const Loose8*>(row + c);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) v[2 * i] = __uint_as_float(p.w[i] << 16), v[2 * i + 1] = __uint_as_float(p.w[i] & 0xffff0000u);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = c + i < cols ? ld(row + c + i) : 0.f;
+  }
+}
+
+template <typename T, int B>
+__global__ __launch_bounds__(kThreads) void loss_few_grad_kernel(LossFewGrad a) {
+  __shared__ float sums[kThreads / 64 - 1][B * 4][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i0 = blockIdx.x * 256 + lane * 4;
+  const int mine = min(lane & 15, a.rows - 1), label = a.labels[mine];
+  const bool real = (lane & 15) < a.rows, counts = real && label != a.ignore, bad = counts && (label < 0 || label >= a.classes);
+  const float2 about = a.softmax[mine];
+  const int count = __popcll(__ballot(counts && lane < 16));
+  const float inverse = count ? 1.f / (float)count : 0.f;
+  float x[B][4], dx[B][4];
+#pragma unroll
+  for (int b = 0; b < B; ++b) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[b][i] = dx[b][i] = 0.f;
+    // (what an ignored sample holds must not meet the zeros of d as a NaN)
+    if (b < a.rows && a.labels[b] != a.ignore) load4(reinterpret_cast<const T*>(a.x) + (int64_t)b * a.in_f, i0, a.in_f, x[b]);
+  }
+  const int v_end = min(a.classes, (int)(blockIdx.y + 1) * a.per_block);
+  for (int v0 = blockIdx.y * a.per_block + wave * 4; v0 < v_end; v0 += kThreads / 64 * 4) {
+    float w[4][4];
+    if (a.partial) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) load4(reinterpret_cast<const T*>(a.w) + (int64_t)min(v0 + j, a.classes - 1) * a.in_f, i0, a.in_f, w[j]);
+    }
+    const int v = v0 + (lane >> 4);
+    float d = 0.f;
+    if (counts && v < a.classes)
+      d = bad ? __builtin_nanf("") : exp_of(a.z[mine * a.z_pitch + v] - about.x) * about.y - (v == label ? 1.f : 0.f);
+    float out[4][4] = {};
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int b = 0; b < B; ++b) {
+        const float s = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(d), j * 16 + b));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (a.partial) dx[b][i] = fmaf(s, w[j][i], dx[b][i]);
+          out[j][i] = fmaf(s, x[b][i], out[j][i]);
+        }
+      }
+    if (a.dw) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (v0 + j >= a.classes || i0 >= a.in_f) continue;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) out[j][i] *= inverse;
+        store4(a.dw + (int64_t)(v0 + j) * a.in_f + i0, out[j], a.in_f - i0);
+      }
+    }
+    if (a.dbias && blockIdx.x == 0) {
+#pragma unroll
+      for (int n = 8; n > 0; n >>= 1) d += __shfl_xor(d, n);
+      if ((lane & 15) == 0 && v < a.classes) a.dbias[v] = d * inverse;
+    }
+  }
+  if (!a.partial) return;
+  if (wave > 0) {  // the waves' shares, in order
+#pragma unroll
+    for (int b = 0; b < B; ++b)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sums[wave - 1][b * 4 + i][lane] = dx[b][i];
+  }
+  __syncthreads();
+  if (wave > 0 || i0 >= a.in_f) return;
+#pragma unroll
+  for (int b = 0; b < B; ++b) {
+#pragma unroll
+    for (int n = 0; n < kThreads / 64 - 1; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) dx[b][i] += sums[n][b * 4 + i][lane];
+    if (b < a.rows) store4(a.partial + ((int64_t)blockIdx.y * a.rows + b) * a.in_f + i0, dx[b], a.in_f - i0);
+  }
+}
+
+// dx or dw from the shares of its sums, always in the same order (of few samples C is counted here).
 template <typename T>
 __global__ __launch_bounds__(kThreads) void loss_join_kernel(const float* partial, int splits, int64_t count, const LossMeta* meta,
-                                                             T* out) {
+                                                             const int32_t* labels, int ignore, int few, int add, T* out) {
   const int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * 4;
   if (i >= count) return;
-  const float inverse = meta->inverse;
+  float inverse;
+  if (few) {
+    int n = 0;
+    for (int b = 0; b < few; ++b) n += labels[b] != ignore;
+    inverse = n ? 1.f / (float)n : 0.f;
+  } else {
+    inverse = meta->inverse;
+  }
   const int n = (int)std::min<int64_t>(4, count - i);
   float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
   for (int s = 0; s < splits; ++s)
 #pragma unroll
     for (int q = 0; q < 4; ++q)
       if (q < n) v[q] += partial[s * count + i + q];
 #pragma unroll
-  for (int q = 0; q < 4; ++q) v[q] *= inverse;
+  for (int q = 0; q < 4; ++q) {
+    v[q] *= inverse;
+    if (add && q < n) v[q] += ld(out + i + q);
+  }
   store4(out + i, v, n);
 }
 
@@ -569,12 +708,61 @@ __global__ __launch_bounds__(1024) void loss_mean_kernel(const float* each, cons
 
 // ---- plan ----------------------------------------------------------------------------------------------------------------
 // One plane of each; d in two; both in two.  256 x 256 of the first and 256 x 128 of the others are what the registers of eight waves
-// and a ring in LDS that stays ahead of the memory allow.
-using TileLarge = ProductTile<256, 256, 8, 4, 1, 1, 4>;
-using TileSmall = ProductTile<128, 128, 4, 4, 1, 1, 4>;
-using TileTwo = ProductTile<256, 128, 8, 2, 1, 2, 5>;
-using TileTwoSmall = ProductTile<128, 128, 4, 4, 1, 2, 3>;
-using TileFloat = ProductTile<256, 128, 4, 4, 2, 2, 3>;
+// and a ring in LDS that stays ahead of the memory allow; the smaller ones spread few outputs over more of the chip.
+enum { TILE_LARGE = 0, TILE_SMALL = 1, TILE_FLAT = 2, TILE_LEAST = 3 };
+template <int TILE, int PLANES>  // planes of d: 1 or 2; 4: float
+struct TileOf;
+template <> struct TileOf<TILE_LARGE, 1> { using type = ProductTile<256, 256, 8, 4, 1, 1, 4>; };
+template <> struct TileOf<TILE_SMALL, 1> { using type = ProductTile<128, 128, 4, 4, 1, 1, 4>; };
+template <> struct TileOf<TILE_FLAT, 1> { using type = ProductTile<128, 64, 4, 2, 1, 1, 6>; };
+template <> struct TileOf<TILE_LEAST, 1> { using type = ProductTile<64, 64, 2, 2, 1, 1, 8>; };
+template <> struct TileOf<TILE_LARGE, 2> { using type = ProductTile<256, 128, 8, 2, 1, 2, 5>; };
+template <> struct TileOf<TILE_SMALL, 2> { using type = ProductTile<128, 128, 4, 4, 1, 2, 3>; };
+template <> struct TileOf<TILE_FLAT, 2> { using type = ProductTile<128, 64, 4, 2, 1, 2, 5>; };
+template <> struct TileOf<TILE_LEAST, 2> { using type = ProductTile<64, 64, 2, 2, 1, 2, 6>; };
+template <> struct TileOf<TILE_LARGE, 4> { using type = ProductTile<256, 128, 4, 4, 2, 2, 3>; };
+template <> struct TileOf<TILE_SMALL, 4> { using type = ProductTile<128, 64, 4, 2, 2, 2, 3>; };
+template <> struct TileOf<TILE_FLAT, 4> { using type = ProductTile<128, 64, 4, 2, 2, 2, 3>; };
+template <> struct TileOf<TILE_LEAST, 4> { using type = ProductTile<64, 64, 2, 2, 2, 2, 5>; };
+// f(TileOf<...>()) for a tile chosen at run time
+template <int PLANES, typename F>
+static auto with_tile(int tile, F f) {
+  switch (tile) {
+    case TILE_LARGE: return f(TileOf<TILE_LARGE, PLANES>());
+    case TILE_SMALL: return f(TileOf<TILE_SMALL, PLANES>());
+    case TILE_FLAT: return f(TileOf<TILE_FLAT, PLANES>());
+    default: return f(TileOf<TILE_LEAST, PLANES>());
+  }
+}
+struct TileSize {
+  int a, b, stat;  // outputs, and classes of one maximum
+};
+static TileSize tile_size(int planes, int tile) {
+  auto of = [](auto t) {
+    using TILE = typename decltype(t)::type;
+    return TileSize{TILE::BA, TILE::BB, 16 * TILE::TA};
+  };
+  return planes == 1 ? with_tile<1>(tile, of) : planes == 2 ? with_tile<2>(tile, of) : with_tile<4>(tile, of);
+}
+// The largest tile of which there are enough for the chip; where the sums can be shared by blocks, also fewer of the second one.
+static int tile_for(int planes, int64_t a, int64_t b, bool shared) {
+  auto tiles = [&](int tile) {
+    const TileSize t = tile_size(planes, tile);
+    return ceil_div(a, t.a) * ceil_div(b, t.b);
+  };
+  if (b <= 64) return a <= 64 || (!shared && tiles(TILE_FLAT) < 128) ? TILE_LEAST : TILE_FLAT;
+  if (tiles(TILE_LARGE) >= (planes == 4 ? 128 : 192)) return TILE_LARGE;
+  if (a <= 64) return TILE_LEAST;
+  return shared || tiles(TILE_SMALL) >= 192 ? TILE_SMALL : TILE_LEAST;
+}
+// By how many blocks a sum of `slabs` is shared: enough to fill the chip, at least `least` slabs each.
+static int shares_of(int planes, int tile, int64_t a, int64_t b, int slabs, int least) {
+  const TileSize t = tile_size(planes, tile);
+  const int64_t tiles = ceil_div(a, t.a) * ceil_div(b, t.b), room = tile == TILE_LARGE ? 256 : 512;
+  if (tiles * 2 > room) return 1;
+  const int want = (int)std::min<int64_t>(room / tiles, std::max(1, slabs / least));
+  return (int)ceil_div(slabs, ceil_div(slabs, want));
+}
 
 struct LossPlan {
   int part;            // samples at once
@@ -582,15 +770,13 @@ struct LossPlan {
   int groups;          // of eight inputs, of a row as it is relaid
   int64_t x_pitch;     // bytes of such a row
   int stat_tiles;      // of classes
-  bool f32, few, relay_w;
-  int splits, slabs_per_split;  // of dx
+  bool f32, few, few_grads, relay_w;
   int tile_z, tile_dx, tile_dw;
+  int splits_dx, splits_dw;  // (few_grads: blocks that share the classes)
   size_t x, w, down_x, down_w, stats, at_label, softmax, each, z, partial, shares, bytes;  // places in the workspace
 };
 
 static constexpr int kMostSamples = 1 << 20;  // of a part
-
-static int tile_of(int64_t a, int64_t b) { return ceil_div(a, 256) * ceil_div(b, 256) >= 192 ? 256 : 128; }
 
 static LossPlan loss_plan(bool f32, int part, int batch, int in_f, int classes, bool grads) {
   LossPlan p{};
@@ -598,18 +784,16 @@ static LossPlan loss_plan(bool f32, int part, int batch, int in_f, int classes, 
   p.classes_pitch = (int)ceil_div(classes, 64) * 64;
   p.groups = f32 ? (int)ceil_div(in_f, 64) * 8 : (int)ceil_div(in_f, 8);
   p.x_pitch = (int64_t)p.groups * (f32 ? 32 : 16);
-  p.few = !grads && part <= kFewRows;
+  p.few_grads = grads && part <= kFewGrad && batch <= kFewGrad;
+  p.few = p.few_grads || (!grads && part <= kFewRows);
   p.relay_w = !p.few && (f32 || in_f % 8 != 0);
-  p.tile_z = tile_of(classes, part), p.tile_dx = tile_of(in_f, part), p.tile_dw = tile_of(in_f, classes);
-  p.stat_tiles = (int)ceil_div(classes, p.few ? kFewClasses : 16 * (f32 ? TileFloat::TA : p.tile_z == 256 ? TileLarge::TA : TileSmall::TA));
-  const int slabs = (int)ceil_div(classes, 32);
-  p.splits = 1, p.slabs_per_split = slabs;
-  const int64_t tiles = f32 ? ceil_div(in_f, TileFloat::BA) * ceil_div(part, TileFloat::BB) : ceil_div(in_f, p.tile_dx) * ceil_div(part, p.tile_dx);
-  const int64_t room = f32 || p.tile_dx == 256 ? 256 : 512;
-  if (tiles * 2 <= room) {
-    const int want = (int)std::min<int64_t>(room / tiles, std::max(1, slabs / 16));
-    p.slabs_per_split = (int)ceil_div(slabs, want), p.splits = (int)ceil_div(slabs, p.slabs_per_split);
-  }
+  const int planes = f32 ? 4 : 1, planes_dw = f32 ? 4 : 2;
+  p.tile_z = tile_for(planes, classes, part, false), p.tile_dx = tile_for(planes, in_f, part, true);
+  p.tile_dw = tile_for(planes_dw, in_f, classes, true);
+  p.stat_tiles = (int)ceil_div(classes, p.few ? few_tiles(part, classes) * 16 * kFewWaves : tile_size(planes, p.tile_z).stat);
+  p.splits_dx = shares_of(planes, p.tile_dx, in_f, part, (int)ceil_div(classes, 32), 16);
+  p.splits_dw = shares_of(planes_dw, p.tile_dw, in_f, classes, (int)ceil_div(part, 32), 8);
+  if (p.few_grads) p.splits_dx = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(classes, 64), 1024 / ceil_div(in_f, 256))), p.splits_dw = 1;
   size_t at = 256;
   auto take = [&](size_t bytes) {
     const size_t here = at;
@@ -623,7 +807,8 @@ static LossPlan loss_plan(bool f32, int part, int batch, int in_f, int classes, 
   p.at_label = take((size_t)part * 4), p.softmax = take((size_t)part * 8), p.each = take((size_t)batch * 4);
   if (grads) {
     p.z = take((size_t)part * p.classes_pitch * 4);
-    p.partial = take(p.splits > 1 ? (size_t)p.splits * part * in_f * 4 : 0);
+    p.partial = take(std::max(p.splits_dx > 1 || p.few_grads ? (size_t)p.splits_dx * part * in_f * 4 : 0,
+                              p.splits_dw > 1 ? (size_t)p.splits_dw * classes * in_f * 4 : 0));
     p.shares = take((size_t)ceil_div(part, 64) * p.classes_pitch * 4);
   }
   p.bytes = at;
@@ -650,13 +835,18 @@ static vcnn_status launch_product(LossProduct a, int splits, hipStream_t st) {
   return check_launch("fc_softmax_loss product");
 }
 // A_ALONG, B_ALONG: how the operands lie.  Of d both planes are read for dw, and in float all planes of all.
-template <int EPI, bool A_ALONG, bool B_ALONG>
-static vcnn_status launch_product(bool f32, int tile, const LossProduct& a, int splits, hipStream_t st) {
-  if (f32) return launch_product<TileFloat, EPI, true, A_ALONG, B_ALONG, true>(a, splits, st);
-  using Large = std::conditional_t<EPI == EPI_DW, TileTwo, TileLarge>;
-  using Small = std::conditional_t<EPI == EPI_DW, TileTwoSmall, TileSmall>;
-  return tile == 256 ? launch_product<Large, EPI, false, A_ALONG, B_ALONG, EPI != EPI_LOGITS>(a, splits, st)
-                     : launch_product<Small, EPI, false, A_ALONG, B_ALONG, EPI != EPI_LOGITS>(a, splits, st);
+template <int EPI, bool F32, bool A_ALONG, bool B_ALONG>
+static vcnn_status launch_product(int tile, const LossProduct& a, int splits, hipStream_t st) {
+  return with_tile<F32 ? 4 : EPI == EPI_DW ? 2 : 1>(tile, [&](auto t) {
+    return launch_product<typename decltype(t)::type, EPI, F32, A_ALONG, B_ALONG, F32 || EPI != EPI_LOGITS>(a, splits, st);
+  });
+}
+template <typename T>
+static vcnn_status launch_join(const float* partial, int splits, int64_t count, const LossMeta* meta, const int32_t* labels, int ignore,
+                               int few, bool add, T* out, hipStream_t st) {
+  hipLaunchKernelGGL(loss_join_kernel<T>, dim3((unsigned)ceil_div(count, 4 * kThreads)), dim3(kThreads), 0, st, partial, splits, count,
+                     meta, labels, ignore, few, (int)add, out);
+  return check_launch("fc_softmax_loss join");
 }
 
 // x or w of T as the products read it.
@@ -692,7 +882,7 @@ static vcnn_status loss_products(LossPlan p, int batch, int in_f, int classes, c
   for (int64_t b0 = 0; b0 < batch; b0 += p.part) {
     const int rows = (int)std::min<int64_t>(p.part, batch - b0);
     const int32_t* const lab = labels + b0;
-    if (grads || (F32 && !p.few)) {
+    if (!p.few && (grads || F32)) {
       hipLaunchKernelGGL(loss_meta_kernel, dim3(1), dim3(1024), 0, st, labels, batch, ignore, b0 == 0, meta);
       if (vcnn_status s = check_launch("fc_softmax_loss count")) return s;
     }
@@ -711,16 +901,35 @@ static vcnn_status loss_products(LossPlan p, int batch, int in_f, int classes, c
     l.stats = (float2*)(ws + p.stats), l.at_label = (float*)(ws + p.at_label);
     l.meta = meta, l.down_a = down_w, l.down_b = down_x;
     const dim3 few_grid((unsigned)p.stat_tiles);
-    if (p.few && rows <= 16) hipLaunchKernelGGL((loss_few_kernel<T, 1>), few_grid, dim3(kFewThreads), 0, st, l, x + b0 * in_f, w, in_f);
-    else if (p.few && rows <= 32) hipLaunchKernelGGL((loss_few_kernel<T, 2>), few_grid, dim3(kFewThreads), 0, st, l, x + b0 * in_f, w, in_f);
-    else if (p.few) hipLaunchKernelGGL((loss_few_kernel<T, 4>), few_grid, dim3(kFewThreads), 0, st, l, x + b0 * in_f, w, in_f);
-    else if (vcnn_status s = launch_product<EPI_LOGITS, true, true>(F32, p.tile_z, l, 1, st)) return s;
+    auto launch_few = [&](auto kernel) { hipLaunchKernelGGL(kernel, few_grid, dim3(kFewThreads), 0, st, l, x + b0 * in_f, w, in_f); };
+    const bool pairs = few_tiles(p.part, classes) == 2;
+    if (!p.few) {
+      if (vcnn_status s = launch_product<EPI_LOGITS, F32, true, true>(p.tile_z, l, 1, st)) return s;
+    } else if (rows <= 16) {
+      pairs ? launch_few(loss_few_kernel<T, 2, 1>) : launch_few(loss_few_kernel<T, 1, 1>);
+    } else if (rows <= 32) {
+      pairs ? launch_few(loss_few_kernel<T, 2, 2>) : launch_few(loss_few_kernel<T, 1, 2>);
+    } else {
+      pairs ? launch_few(loss_few_kernel<T, 2, 4>) : launch_few(loss_few_kernel<T, 1, 4>);
+    }
     const LossRows r{l.stats, p.stat_tiles, rows, classes, lab, ignore, l.at_label, grads ? softmax : nullptr, each + b0,
                      batch <= kFewRows ? loss : nullptr};
     if (rows <= kFewRows) hipLaunchKernelGGL(loss_few_rows_kernel, dim3(1), dim3(1024), 0, st, r);
     else hipLaunchKernelGGL(loss_rows_kernel, dim3((unsigned)ceil_div(rows, 16)), dim3(kThreads), 0, st, r);
     if (vcnn_status s = check_launch("fc_softmax_loss rows")) return s;
     if (!grads) continue;
+    float* const partial = (float*)(ws + p.partial);
+    if (p.few_grads) {
+      const int per_block = (int)ceil_div(ceil_div(classes, p.splits_dx), 16) * 16;
+      const int blocks = (int)ceil_div(classes, per_block);
+      const LossFewGrad g{x, w, z, p.classes_pitch, softmax, lab, ignore, rows, in_f, classes, per_block, dx ? partial : nullptr, dw, dbias};
+      const dim3 grid((unsigned)ceil_div(in_f, 256), (unsigned)blocks);
+      if (rows <= 4) hipLaunchKernelGGL((loss_few_grad_kernel<T, 4>), grid, dim3(kThreads), 0, st, g);
+      else if (rows <= 8) hipLaunchKernelGGL((loss_few_grad_kernel<T, 8>), grid, dim3(kThreads), 0, st, g);
+      else hipLaunchKernelGGL((loss_few_grad_kernel<T, 16>), grid, dim3(kThreads), 0, st, g);
+      if (vcnn_status s = check_launch("fc_softmax_loss gradients")) return s;
+      return dx ? launch_join(partial, blocks, (int64_t)rows * in_f, meta, lab, ignore, rows, false, dx, st) : VCNN_OK;
+    }
     float* const shares = dbias ? (float*)(ws + p.shares) : nullptr;
     hipLaunchKernelGGL(loss_grad_kernel<F32>, dim3((unsigned)(p.classes_pitch / 64), (unsigned)ceil_div(rows, 64)), dim3(kThreads), 0, st, z,
                        p.classes_pitch, rows, classes, lab, ignore, softmax, down_x, down_w, shares, p.classes_pitch);
@@ -729,23 +938,24 @@ static vcnn_status loss_products(LossPlan p, int batch, int in_f, int classes, c
     if (dx) {
       LossProduct g{};
       g.p.a = {weights, p.x_pitch, p.groups}, g.p.b = {(const char*)z, z_pitch, rows};
-      g.p.k = classes, g.p.slabs_per_split = p.slabs_per_split;
+      g.p.k = classes, g.p.slabs_per_split = (int)ceil_div(ceil_div(classes, 32), p.splits_dx);
       g.rows = rows, g.cols = in_f, g.meta = meta, g.out = dx + b0 * in_f, g.down_b = down_x;
-      g.partial = p.splits > 1 ? (float*)(ws + p.partial) : nullptr;
-      if (vcnn_status s = launch_product<EPI_DX, false, true>(F32, p.tile_dx, g, p.splits, st)) return s;
-      if (p.splits > 1) {
-        const int64_t count = (int64_t)rows * in_f;
-        hipLaunchKernelGGL(loss_join_kernel<T>, dim3((unsigned)ceil_div(count, 4 * kThreads)), dim3(kThreads), 0, st, g.partial, p.splits,
-                           count, meta, (T*)g.out);
-        if (vcnn_status s = check_launch("fc_softmax_loss join")) return s;
-      }
+      g.partial = p.splits_dx > 1 ? partial : nullptr;
+      const int splits = (int)ceil_div(ceil_div(classes, 32), g.p.slabs_per_split);
+      if (vcnn_status s = launch_product<EPI_DX, F32, false, true>(p.tile_dx, g, splits, st)) return s;
+      if (g.partial)
+        if (vcnn_status s = launch_join(partial, splits, (int64_t)rows * in_f, meta, lab, ignore, 0, false, (T*)g.out, st)) return s;
     }
     if (dw) {
       LossProduct g{};
       g.p.a = {xs, p.x_pitch, p.groups}, g.p.b = {(const char*)z, z_pitch, p.classes_pitch / 8};
-      g.p.k = rows, g.p.slabs_per_split = (int)ceil_div(rows, 32);
+      g.p.k = rows, g.p.slabs_per_split = (int)ceil_div(ceil_div(rows, 32), p.splits_dw);
       g.rows = classes, g.cols = in_f, g.meta = meta, g.out = dw, g.add = b0 > 0, g.down_b = down_w;
-      if (vcnn_status s = launch_product<EPI_DW, false, false>(F32, p.tile_dw, g, 1, st)) return s;
+      g.partial = p.splits_dw > 1 ? partial : nullptr;
+      const int splits = (int)ceil_div(ceil_div(rows, 32), g.p.slabs_per_split);
+      if (vcnn_status s = launch_product<EPI_DW, F32, false, false>(p.tile_dw, g, splits, st)) return s;
+      if (g.partial)
+        if (vcnn_status s = launch_join(partial, splits, (int64_t)classes * in_f, meta, lab, ignore, 0, b0 > 0, dw, st)) return s;
     }
     if (dbias) {
       hipLaunchKernelGGL(loss_bias_kernel, dim3((unsigned)ceil_div(classes, kThreads)), dim3(kThreads), 0, st, shares, p.classes_pitch,
@@ -825,7 +1035,7 @@ static LossFloatPlan loss_float_plan(int batch, int in_f, int classes, bool grad
 
 // Small float layers by the float products, whole: d is made of finished logits there.
 static bool loss_is_small(int64_t batch, int64_t in_f, int64_t classes, bool grads) {
-  if (!grads && batch <= kFewRows) return false;
+  if (batch <= (grads ? kFewGrad : kFewRows)) return false;
   return batch * classes <= (int64_t)1 << 24 && batch * in_f * classes <= (int64_t)1 << 27;
 }
 

@@ -313,17 +313,28 @@ __global__ __launch_bounds__(TILE::THREADS, TILE::WAVES_SIMD) void loss_product_
 // ---- few samples -----------------------------------------------------------------------------------------------------------
 // Bandwidth: w is read once, where it stands.  A wave takes 16 MA classes and up to 16 NB samples and reads its operands as the matrix
 // instruction wants them, straight into registers: lane l row l % 16, and of every 64 bytes of it the 16 from 16 (l / 16) on.  (Which
-// steps of the sum a lane holds does not matter as long as it is the same ones of both.)  The eight waves of a block leave one maximum
-// and sum of their classes.
+// steps of the sum a lane holds does not matter as long as it is the same ones of both.)  Of few classes `sharing` waves share a sum.
+// The eight waves of a block leave one maximum and sum of their classes.
 static constexpr int kFewThreads = 512, kFewWaves = kFewThreads / 64, kFewRows = 64;
-constexpr int few_tiles(int rows, int64_t classes) { return rows > 16 && classes >= 16 * 2 * kFewWaves * 64 ? 2 : 1; }  // MA
+struct FewShape {
+  int tiles, sharing;  // MA; waves of one sum: enough blocks for the chip
+  int block_classes() const { return 16 * tiles * kFewWaves / sharing; }
+};
+static FewShape few_shape(int rows, int64_t classes) {
+  if (classes >= 16 * 2 * kFewWaves * 64) return {rows > 16 ? 2 : 1, 1};
+  FewShape s{1, 1};
+  while (s.sharing < kFewWaves && ceil_div(classes, s.block_classes()) < 256) s.sharing *= 2;
+  return s;
+}
 
 template <typename T, int MA, int NB>
-__global__ __launch_bounds__(kFewThreads) void loss_few_kernel(LossProduct a, const T* xs, const T* ws, int in_f) {
+__global__ __launch_bounds__(kFewThreads) void loss_few_kernel(LossProduct a, const T* xs, const T* ws, int in_f, int sharing) {
   constexpr int AHEAD = MA * NB == 1 ? 8 : 4, N = 16 / sizeof(T), STEP = 4 * N;  // elements of a load, and of a row's four
   __shared__ float2 parts[kFewWaves][NB * 16];
+  __shared__ float shares[MA == 1 ? kFewWaves : 1][NB * 4][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, at = (lane >> 4) * N;
-  const int c0 = (blockIdx.x * kFewWaves + wave) * 16 * MA;
+  const int group = wave / sharing, share = wave % sharing;
+  const int c0 = (blockIdx.x * (kFewWaves / sharing) + group) * 16 * MA;
   const T *w[MA], *x[NB];
   f32x4 acc[MA][NB];
 #pragma unroll
@@ -343,8 +354,8 @@ __global__ __launch_bounds__(kFewThreads) void loss_few_kernel(LossProduct a, co
       return c;
     }
   };
-  int k = 0;
-  for (; k + AHEAD * STEP <= in_f; k += AHEAD * STEP) {
+  const int whole = in_f / (AHEAD * STEP) * (AHEAD * STEP);
+  for (int k = share * AHEAD * STEP; k < whole; k += sharing * AHEAD * STEP) {
     Loose16 fw[AHEAD][MA], fx[AHEAD][NB];
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
@@ -360,7 +371,7 @@ __global__ __launch_bounds__(kFewThreads) void loss_few_kernel(LossProduct a, co
 #pragma unroll
         for (int n = 0; n < NB; ++n) acc[m][n] = multiply(fw[u][m], fx[u][n], acc[m][n]);
   }
-  for (; k < in_f; k += STEP) {
+  for (int k = whole + share * STEP; k < in_f; k += sharing * STEP) {
     Loose16 fx[NB];
     const bool in = k + at < in_f;
 #pragma unroll
@@ -372,6 +383,23 @@ __global__ __launch_bounds__(kFewThreads) void loss_few_kernel(LossProduct a, co
       for (int n = 0; n < NB; ++n) acc[m][n] = multiply(fw, fx[n], acc[m][n]);
     }
   }
+  if constexpr (MA == 1) {
+    if (sharing > 1) {  // the first wave of a sum adds the others' shares, in order
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) shares[wave][n * 4 + q][lane] = acc[0][n][q];
+      __syncthreads();
+      if (share == 0) {
+        for (int v = 1; v < sharing; ++v)
+#pragma unroll
+          for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) acc[0][n][q] += shares[wave + v][n * 4 + q][lane];
+      }
+    }
+  }
+  if (share == 0) {
 #pragma unroll
   for (int n = 0; n < NB; ++n) {
     const int b = n * 16 + row, label = a.labels[min(b, a.rows - 1)];
@@ -398,13 +426,13 @@ __global__ __launch_bounds__(kFewThreads) void loss_few_kernel(LossProduct a, co
         if (c0 + m * 16 + 4 * (lane >> 4) + q < a.cols) sum += exp_of(acc[m][n][q] - about);
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
-    if (lane < 16) parts[wave][b] = make_float2(most, sum);
+    if (lane < 16) parts[group][b] = make_float2(most, sum);
+  }
   }
   __syncthreads();
   if (threadIdx.x >= NB * 16 || threadIdx.x >= a.rows) return;
   float2 total = parts[0][threadIdx.x];
-#pragma unroll
-  for (int v = 1; v < kFewWaves; ++v) join(total, parts[v][threadIdx.x]);
+  for (int v = 1; v < kFewWaves / sharing; ++v) join(total, parts[v][threadIdx.x]);
   a.stats[(int64_t)blockIdx.x * a.rows + threadIdx.x] = total;
 }
 
@@ -518,27 +546,45 @@ __global__ __launch_bounds__(kThreads) void loss_few_grad_kernel(LossFewGrad a) 
   }
 }
 
-// dx or dw from the shares of its sums, always in the same order (of few samples C is counted here).
-template <typename T>
+// dx or dw from the shares of its sums: PARTS threads for each four outputs take every PARTS-th share and are added in pairs, always
+// the same ones.  (Of few samples C is counted here.)
+template <typename T, int PARTS>
 __global__ __launch_bounds__(kThreads) void loss_join_kernel(const float* partial, int splits, int64_t count, const LossMeta* meta,
                                                              const int32_t* labels, int ignore, int few, int add, T* out) {
-  const int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * 4;
-  if (i >= count) return;
-  float inverse;
-  if (few) {
-    int n = 0;
-    for (int b = 0; b < few; ++b) n += labels[b] != ignore;
-    inverse = n ? 1.f / (float)n : 0.f;
-  } else {
-    inverse = meta->inverse;
-  }
-  const int n = (int)std::min<int64_t>(4, count - i);
+  constexpr int WIDE = kThreads / PARTS;
+  __shared__ float sums[PARTS > 1 ? PARTS : 1][4][WIDE];
+  const int in = threadIdx.x % WIDE, part = threadIdx.x / WIDE;
+  const int64_t i = ((int64_t)blockIdx.x * WIDE + in) * 4;
+  const int n = (int)std::max<int64_t>(0, std::min<int64_t>(4, count - i));
   float v[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-  for (int s = 0; s < splits; ++s)
+  for (int s = part; s < splits; s += PARTS)
 #pragma unroll
     for (int q = 0; q < 4; ++q)
       if (q < n) v[q] += partial[s * count + i + q];
+  if constexpr (PARTS > 1) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) sums[part][q][in] = v[q];
+#pragma unroll
+    for (int h = PARTS / 2; h > 0; h /= 2) {
+      __syncthreads();
+      if (part < h) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) sums[part][q][in] += sums[part + h][q][in];
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[q] = sums[0][q][in];  // (read by those that wrote it)
+  }
+  if (part > 0 || n <= 0) return;
+  float inverse;
+  if (few) {
+    int c = 0;
+    for (int b = 0; b < few; ++b) c += labels[b] != ignore;
+    inverse = c ? 1.f / (float)c : 0.f;
+  } else {
+    inverse = meta->inverse;
+  }
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     v[q] *= inverse;
@@ -790,10 +836,10 @@ static LossPlan loss_plan(bool f32, int part, int batch, int in_f, int classes, 
   const int planes = f32 ? 4 : 1, planes_dw = f32 ? 4 : 2;
   p.tile_z = tile_for(planes, classes, part, false), p.tile_dx = tile_for(planes, in_f, part, true);
   p.tile_dw = tile_for(planes_dw, in_f, classes, true);
-  p.stat_tiles = (int)ceil_div(classes, p.few ? few_tiles(part, classes) * 16 * kFewWaves : tile_size(planes, p.tile_z).stat);
+  p.stat_tiles = (int)ceil_div(classes, p.few ? few_shape(part, classes).block_classes() : tile_size(planes, p.tile_z).stat);
   p.splits_dx = shares_of(planes, p.tile_dx, in_f, part, (int)ceil_div(classes, 32), 16);
   p.splits_dw = shares_of(planes_dw, p.tile_dw, in_f, classes, (int)ceil_div(part, 32), 8);
-  if (p.few_grads) p.splits_dx = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(classes, 64), 1024 / ceil_div(in_f, 256))), p.splits_dw = 1;
+  if (p.few_grads) p.splits_dx = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(classes, 16), 1024 / ceil_div(in_f, 256))), p.splits_dw = 1;
   size_t at = 256;
   auto take = [&](size_t bytes) {
     const size_t here = at;
@@ -844,8 +890,12 @@ static vcnn_status launch_product(int tile, const LossProduct& a, int splits, hi
 template <typename T>
 static vcnn_status launch_join(const float* partial, int splits, int64_t count, const LossMeta* meta, const int32_t* labels, int ignore,
                                int few, bool add, T* out, hipStream_t st) {
-  hipLaunchKernelGGL(loss_join_kernel<T>, dim3((unsigned)ceil_div(count, 4 * kThreads)), dim3(kThreads), 0, st, partial, splits, count,
-                     meta, labels, ignore, few, (int)add, out);
+  auto launch = [&](auto kernel, int wide) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(count, 4 * wide)), dim3(kThreads), 0, st, partial, splits, count, meta, labels,
+                       ignore, few, (int)add, out);
+  };
+  if (splits >= 16) launch(loss_join_kernel<T, 16>, kThreads / 16);  // (4 x 2048 outputs of 128 shares 65 us with one thread, 5 with these)
+  else launch(loss_join_kernel<T, 1>, kThreads);
   return check_launch("fc_softmax_loss join");
 }
 
@@ -878,6 +928,8 @@ static vcnn_status loss_products(LossPlan p, int batch, int in_f, int classes, c
   float* const down_x = F32 ? (float*)(ws + p.down_x) : nullptr;
   float* const down_w = F32 ? (float*)(ws + p.down_w) : nullptr;
   char* const xs = ws + p.x;
+  // one block does for all rows and their mean where there is little to add up
+  const bool mean_with_rows = batch <= kFewRows && (int64_t)batch * p.stat_tiles <= 8192;
   const char* weights = (const char*)w;
   for (int64_t b0 = 0; b0 < batch; b0 += p.part) {
     const int rows = (int)std::min<int64_t>(p.part, batch - b0);
@@ -900,9 +952,10 @@ static vcnn_status loss_products(LossPlan p, int batch, int in_f, int classes, c
     l.rows = rows, l.cols = classes, l.z = z, l.z_pitch = p.classes_pitch, l.bias = bias, l.labels = lab;
     l.stats = (float2*)(ws + p.stats), l.at_label = (float*)(ws + p.at_label);
     l.meta = meta, l.down_a = down_w, l.down_b = down_x;
+    const FewShape few = few_shape(p.part, classes);
     const dim3 few_grid((unsigned)p.stat_tiles);
-    auto launch_few = [&](auto kernel) { hipLaunchKernelGGL(kernel, few_grid, dim3(kFewThreads), 0, st, l, x + b0 * in_f, w, in_f); };
-    const bool pairs = few_tiles(p.part, classes) == 2;
+    auto launch_few = [&](auto kernel) { hipLaunchKernelGGL(kernel, few_grid, dim3(kFewThreads), 0, st, l, x + b0 * in_f, w, in_f, few.sharing); };
+    const bool pairs = few.tiles == 2;
     if (!p.few) {
       if (vcnn_status s = launch_product<EPI_LOGITS, F32, true, true>(p.tile_z, l, 1, st)) return s;
     } else if (rows <= 16) {
@@ -913,8 +966,8 @@ static vcnn_status loss_products(LossPlan p, int batch, int in_f, int classes, c
       pairs ? launch_few(loss_few_kernel<T, 2, 4>) : launch_few(loss_few_kernel<T, 1, 4>);
     }
     const LossRows r{l.stats, p.stat_tiles, rows, classes, lab, ignore, l.at_label, grads ? softmax : nullptr, each + b0,
-                     batch <= kFewRows ? loss : nullptr};
-    if (rows <= kFewRows) hipLaunchKernelGGL(loss_few_rows_kernel, dim3(1), dim3(1024), 0, st, r);
+                     mean_with_rows ? loss : nullptr};
+    if (mean_with_rows) hipLaunchKernelGGL(loss_few_rows_kernel, dim3(1), dim3(1024), 0, st, r);
     else hipLaunchKernelGGL(loss_rows_kernel, dim3((unsigned)ceil_div(rows, 16)), dim3(kThreads), 0, st, r);
     if (vcnn_status s = check_launch("fc_softmax_loss rows")) return s;
     if (!grads) continue;
@@ -928,7 +981,9 @@ static vcnn_status loss_products(LossPlan p, int batch, int in_f, int classes, c
       else if (rows <= 8) hipLaunchKernelGGL((loss_few_grad_kernel<T, 8>), grid, dim3(kThreads), 0, st, g);
       else hipLaunchKernelGGL((loss_few_grad_kernel<T, 16>), grid, dim3(kThreads), 0, st, g);
       if (vcnn_status s = check_launch("fc_softmax_loss gradients")) return s;
-      return dx ? launch_join(partial, blocks, (int64_t)rows * in_f, meta, lab, ignore, rows, false, dx, st) : VCNN_OK;
+      if (dx)
+        if (vcnn_status s = launch_join(partial, blocks, (int64_t)rows * in_f, meta, lab, ignore, rows, false, dx, st)) return s;
+      continue;
     }
     float* const shares = dbias ? (float*)(ws + p.shares) : nullptr;
     hipLaunchKernelGGL(loss_grad_kernel<F32>, dim3((unsigned)(p.classes_pitch / 64), (unsigned)ceil_div(rows, 64)), dim3(kThreads), 0, st, z,
@@ -963,7 +1018,7 @@ static vcnn_status loss_products(LossPlan p, int batch, int in_f, int classes, c
       if (vcnn_status s = check_launch("fc_softmax_loss bias")) return s;
     }
   }
-  if (batch <= kFewRows) return VCNN_OK;
+  if (mean_with_rows) return VCNN_OK;
   hipLaunchKernelGGL(loss_mean_kernel, dim3(1), dim3(1024), 0, st, each, labels, ignore, batch, loss);
   return check_launch("fc_softmax_loss mean");
 }

@@ -790,16 +790,16 @@ static TileSize tile_size(int planes, int tile) {
   };
   return planes == 1 ? with_tile<1>(tile, of) : planes == 2 ? with_tile<2>(tile, of) : with_tile<4>(tile, of);
 }
-// The largest tile of which there are enough for the chip; where the sums can be shared by blocks, also fewer of the second one.
-static int tile_for(int planes, int64_t a, int64_t b, bool shared) {
-  auto tiles = [&](int tile) {
+// The largest tile of which there are enough for the chip, also by sharing a sum among up to `sharing` blocks.
+static int tile_for(int planes, int64_t a, int64_t b, int64_t sharing) {
+  auto blocks = [&](int tile) {
     const TileSize t = tile_size(planes, tile);
-    return ceil_div(a, t.a) * ceil_div(b, t.b);
+    return ceil_div(a, t.a) * ceil_div(b, t.b) * sharing;
   };
-  if (b <= 64) return a <= 64 || (!shared && tiles(TILE_FLAT) < 128) ? TILE_LEAST : TILE_FLAT;
-  if (tiles(TILE_LARGE) >= (planes == 4 ? 128 : 192)) return TILE_LARGE;
+  if (b <= 64) return a <= 64 || blocks(TILE_FLAT) < 128 ? TILE_LEAST : TILE_FLAT;
+  if (a > 128 && b > 128 && blocks(TILE_LARGE) >= (planes == 4 ? 128 : 192)) return TILE_LARGE;
   if (a <= 64) return TILE_LEAST;
-  return shared || tiles(TILE_SMALL) >= 192 ? TILE_SMALL : TILE_LEAST;
+  return blocks(TILE_SMALL) >= 192 || (sharing > 1 && b > 128) ? TILE_SMALL : TILE_LEAST;
 }
 // By how many blocks a sum of `slabs` is shared: enough to fill the chip, at least `least` slabs each.
 static int shares_of(int planes, int tile, int64_t a, int64_t b, int slabs, int least) {
@@ -834,11 +834,12 @@ static LossPlan loss_plan(bool f32, int part, int batch, int in_f, int classes, 
   p.few = p.few_grads || (!grads && part <= kFewRows);
   p.relay_w = !p.few && (f32 || in_f % 8 != 0);
   const int planes = f32 ? 4 : 1, planes_dw = f32 ? 4 : 2;
-  p.tile_z = tile_for(planes, classes, part, false), p.tile_dx = tile_for(planes, in_f, part, true);
-  p.tile_dw = tile_for(planes_dw, in_f, classes, true);
+  const int slabs_dx = (int)ceil_div(classes, 32), slabs_dw = (int)ceil_div(part, 32);
+  p.tile_z = tile_for(planes, classes, part, 1), p.tile_dx = tile_for(planes, in_f, part, std::max(1, slabs_dx / 16));
+  p.tile_dw = tile_for(planes_dw, in_f, classes, std::max(1, slabs_dw / 8));
   p.stat_tiles = (int)ceil_div(classes, p.few ? few_shape(part, classes).block_classes() : tile_size(planes, p.tile_z).stat);
-  p.splits_dx = shares_of(planes, p.tile_dx, in_f, part, (int)ceil_div(classes, 32), 16);
-  p.splits_dw = shares_of(planes_dw, p.tile_dw, in_f, classes, (int)ceil_div(part, 32), 8);
+  p.splits_dx = shares_of(planes, p.tile_dx, in_f, part, slabs_dx, 16);
+  p.splits_dw = shares_of(planes_dw, p.tile_dw, in_f, classes, slabs_dw, 8);
   if (p.few_grads) p.splits_dx = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(classes, 16), 1024 / ceil_div(in_f, 256))), p.splits_dw = 1;
   size_t at = 256;
   auto take = [&](size_t bytes) {

@@ -119,10 +119,10 @@ __device__ __forceinline__ void product_tile_of(const ProductArgs& p, int* ta, i
   *ta = in / wide, *tb = group * 8 + in % wide;
 }
 
-// Slabs of 32 steps go to a ring by direct loads, RING - 1 slabs ahead; a wave reads the second half of a step's a-tiles while it
-// multiplies the first, and the first of the next step while it multiplies the second, so that neither the loads nor the barrier
-// (one a slab) leave the matrix cores without operands.  acc[i][j]: lane l has a = 16 i + 4 (l / 16) + q, b = 16 j + l % 16 of the
-// wave's part.
+// Slabs of 32 steps go to a ring by direct loads.  A wave reads the second half of a step's a-tiles while it multiplies the first, and
+// the first of the next step while it multiplies the second.  The one barrier of a step stands between the two: there the next slab is
+// in LDS for every wave, and every wave has read this one, whose place then takes the slab RING steps on; so a slab has RING - 1 steps
+// to arrive.  acc[i][j]: lane l has a = 16 i + 4 (l / 16) + q, b = 16 j + l % 16 of the wave's part.
 template <typename TILE, bool F16, bool A_ALONG, bool A_PLANES, bool B_ALONG, bool B_PLANES>
 __device__ __forceinline__ void slab_product(const ProductArgs& p, int a0, int b0, uint4* smem,
                                              f32x4 (&acc)[TILE::TA][TILE::TB]) {
@@ -169,8 +169,8 @@ __device__ __forceinline__ void slab_product(const ProductArgs& p, int a0, int b
 #pragma unroll
     for (int j = 0; j < TB; ++j) to[j] = WayB::fragment(buf, rb + j * 16, lane);
   };
-  // The products of half h: term t of a with `with`.  Loads of slab s, every L / (2 PAIRS) such products one, stand among them: a
-  // load waits its turn behind those of the other waves, and the matrix cores are not to wait with it.
+  // The products of half h: term t of a with `with`.  Of slab s every L / (2 PAIRS) loads belong to one such turn and stand among its
+  // products: a load waits its turn behind those of the other waves, and the matrix cores are not to wait with it.
   constexpr int PAIRS = PA == 2 && PB == 2 ? 3 : PA * PB;
   auto multiply = [&](int h, int t, const uint4 (&with)[TB], int s, int slot, int turn, auto is_whole) {
     const int l0 = L * turn / (2 * PAIRS), l1 = L * (turn + 1) / (2 * PAIRS), every = H * TB / (l1 > l0 ? l1 - l0 : 1);
@@ -188,12 +188,11 @@ __device__ __forceinline__ void slab_product(const ProductArgs& p, int a0, int b
     __builtin_amdgcn_sched_barrier(0);
   };
   constexpr auto all_but = [](int n) { return 0x0F70 | (n & 15) | n >> 4 << 14; };  // vmcnt(n)
-  static_assert((R - 2) * L < 64, "the counts fit");
+  constexpr int HALF = L * PAIRS / (2 * PAIRS);  // loads of a slab that are issued in a step's second half, R steps ahead
+  static_assert((R - 1) * L + HALF < 64, "the counts fit");
 #pragma unroll
-  for (int s = 0; s < R - 1; ++s)
-#pragma unroll
-    for (int i = 0; i < L; ++i) stage(s, s, i, std::false_type());
-  __builtin_amdgcn_s_waitcnt(all_but((R - 2) * L));
+  for (int n = 0; n < (R - 1) * L + HALF; ++n) stage(n / L, n / L, n % L, std::false_type());
+  __builtin_amdgcn_s_waitcnt(all_but((R - 2) * L + HALF));
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
   read_b(0, fb[0], 0), read_a(0, 0);
@@ -201,26 +200,27 @@ __device__ __forceinline__ void slab_product(const ProductArgs& p, int a0, int b
   int here = 0;  // the slab's place
   auto step = [&](int s, int n, auto is_whole) {
     const int next = here + 1 == R ? 0 : here + 1, last = here == 0 ? R - 1 : here - 1;
-    // slab s + 1 is there, for everyone; slab s - 1 has been read by everyone
-    __builtin_amdgcn_s_waitcnt(all_but((R - 3) * L));
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    int turn = 0;
+    int turn = PAIRS;
     if constexpr (PB == 2) read_b(here, fl, 1);
     read_a(here, 1);
     __builtin_amdgcn_sched_barrier(0);
     multiply(0, 0, fb[n], s + R - 1, last, turn++, is_whole);
     if constexpr (PA == 2) multiply(0, 1, fb[n], s + R - 1, last, turn++, is_whole);
     if constexpr (PB == 2) multiply(0, 0, fl, s + R - 1, last, turn++, is_whole);
+    // slab s + 1 is there, for everyone; slab s has been read by everyone (vmcnt and lgkmcnt(0))
+    __builtin_amdgcn_s_waitcnt(all_but((R - 2) * L) & ~0x0F00);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    turn = 0;
     read_b(next, fb[n ^ 1], 0), read_a(next, 0);
     __builtin_amdgcn_sched_barrier(0);
-    if constexpr (PB == 2) multiply(1, 0, fl, s + R - 1, last, turn++, is_whole);
-    if constexpr (PA == 2) multiply(1, 1, fb[n], s + R - 1, last, turn++, is_whole);
-    multiply(1, 0, fb[n], s + R - 1, last, turn++, is_whole);
+    if constexpr (PB == 2) multiply(1, 0, fl, s + R, here, turn++, is_whole);
+    if constexpr (PA == 2) multiply(1, 1, fb[n], s + R, here, turn++, is_whole);
+    multiply(1, 0, fb[n], s + R, here, turn++, is_whole);
     here = next;
   };
   int s = 0;
-  for (; s + R < whole; s += 2) {
+  for (; s + R + 1 < whole; s += 2) {
     step(s, 0, std::true_type());
     step(s + 1, 1, std::true_type());
   }

@@ -169,3 +169,35 @@ def test_a_captured_step_drops_other_elements_each_time():
         torch.cuda.synchronize()
         assert torch.equal(y.cpu(), factors(rows, cols, 0.4, 3, n, 1).float()) and torch.equal(y, dx)
         assert rng.tolist() == [3, n + 1]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,cols", [(70001, 40009), (3, 1 << 30)])
+def test_more_than_2_31_elements(rows, cols):
+    """Rows behind 2^32 bytes: their elements, and those of layer norm's passes, by samples of rows."""
+    from test_gpu_norm import EPS
+    free, _ = torch.cuda.mem_get_info()
+    if free < 5 * rows * cols * 2:
+        pytest.skip("needs the memory")
+    x = torch.empty(rows, cols, dtype=torch.bfloat16, device=DEV)
+    x.fill_(1.0)
+    x[rows - 1, cols - 9:] = 3.0
+    y, p, rng = torch.empty_like(x), 0.25, generator()
+    vcnn.dropout_fwd(vcnn.BF16, rows, cols, p, rng, 3, x, None, y)
+    h, z = torch.empty_like(x), torch.empty_like(x)
+    gain, mean = torch.ones(cols, device=DEV), torch.empty(rows, device=DEV)
+    vcnn.layernorm_fwd(vcnn.BF16, rows, cols, EPS, p, rng, 3, x, None, gain, None, h, z, mean, None)
+    blocks, width = -(-cols // 8), min(cols, 4096) // 8 * 8
+    for r, c0 in ((0, 0), (rows - 1, 0), (rows - 1, (cols - width) // 8 * 8), (rows // 2, cols // 16 * 8)):
+        n = np.arange(width // 8, dtype=np.uint64) + np.uint64(r * blocks + c0 // 8)
+        ctr = np.stack([n & np.uint64(0xffffffff), n >> np.uint64(32), np.full_like(n, 7), np.full_like(n, 3)], 1)
+        words = philox(ctr, (0x123456789abcdef & 0xffffffff, 0x123456789abcdef >> 32))
+        kept = torch.from_numpy(np.stack([words & 0xffff, words >> 16], 2).reshape(-1) >= 16384)[:cols - c0]
+        got = y[r, c0:c0 + width].cpu()
+        want = torch.where(kept, x[r, c0:c0 + width].cpu().float() * (65536 / 49152), 0.0).bfloat16()
+        assert torch.equal(got, want) and torch.equal(h[r, c0:c0 + width].cpu(), want)
+        hr = h[r].double()
+        m, s = hr.mean(), (hr.var(unbiased=False) + EPS).rsqrt()
+        assert abs(float(mean[r]) - float(m)) <= 1e-6 * float(m)
+        want = (hr[c0:c0 + width] - m) * s
+        assert bool(((z[r, c0:c0 + width].double() - want).abs() <= want.abs() * 2.0 ** -8 + 1e-5).all())

@@ -224,10 +224,10 @@ def test_gradients_against_differences(batch, in_f, classes):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("batch,in_f,classes", [(200, 136, 1100), (300, 520, 1100), (12, 100, 700), (128, 50, 10)])
 @pytest.mark.parametrize("dtype", [vcnn.F32, vcnn.BF16])
-def test_captured_call(dtype):
+def test_captured_call(batch, in_f, classes, dtype):
     """Replayed on new inputs, with eager calls on a workspace of their own between the replays."""
-    batch, in_f, classes = 200, 136, 1100
     x, w, b, labels = (dev(t) for t in inputs(batch, in_f, classes, dtype, seed=8))
     nbytes = vcnn.fc_softmax_loss_workspace_bytes(dtype, batch, in_f, classes, True)
 
@@ -256,6 +256,62 @@ def test_captured_call(dtype):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(o[k], eager[k]) for k in ("loss", "each", "dx", "dw", "db"))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("scale", [1e-30, 1e-20, 1e15, 1e30])
+@pytest.mark.parametrize("batch", [12, 300])
+def test_float_operands_of_any_magnitude(batch, scale):
+    """x and w far from one, their products ordinary; some rows of either much smaller than the others, one class of zeros."""
+    in_f, classes = 520, 1100
+    x, w, b, labels = inputs(batch, in_f, classes, vcnn.F32, seed=9)
+    x, w = x * scale, w / scale
+    x[1::3] *= 2.0 ** -6
+    w[2::5] *= 2.0 ** -6
+    w[7] = 0.0
+    out, bounds, gradients = plain(x, w, b, labels)
+    got = run(vcnn.F32, x, w, b, labels)
+    check(vcnn.F32, got, out, bounds, gradients)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [vcnn.F32, vcnn.BF16])
+def test_one_sample_apart_does_not_move_the_others(dtype):
+    """A sample of 2^20 times the others' magnitude, in the products that scale all of x together: the others' costs stay within
+    what 2^-39 of the largest element leaves in their logits."""
+    batch, in_f, classes = 300, 520, 1100
+    x, w, b, labels = inputs(batch, in_f, classes, dtype, ignored=0.0, seed=10)
+    x[5] = (x[5].float() * 2.0 ** 20).to(x.dtype)
+    out, bounds, _ = plain(x, w, b, labels)
+    got = run(dtype, x, w, b, labels, want="each")["each"].double()
+    lost = 2 * 2.0 ** -39 * float(x.float().abs().max()) * w.float().abs().sum(1).max().double() * (dtype == vcnn.F32)
+    others = torch.arange(batch) != 5
+    assert bool(((got - out["each"].cpu()).abs() <= 1.01 * bounds["each"].cpu() + lost)[others].all())
+
+
+@pytest.mark.gpu
+def test_weights_of_more_than_2_31_elements():
+    """Rows behind 2^32 bytes, read where they stand by the kernels for few samples and by those for many."""
+    in_f, classes = 20480, 110000
+    free, _ = torch.cuda.mem_get_info()
+    if free < 24 << 30:
+        pytest.skip("needs 24 GiB")
+    g = torch.Generator(device=DEV).manual_seed(11)
+    w = torch.empty(classes, in_f, dtype=torch.bfloat16, device=DEV)
+    for at in range(0, classes, 10000):
+        w[at:at + 10000] = torch.randn(min(10000, classes - at), in_f, device=DEV, generator=g).bfloat16() / 64
+    for batch in (3, 70):
+        labels = torch.randint(0, classes, (batch,), dtype=torch.int32, device=DEV, generator=g)
+        labels[0] = classes - 1
+        x = (torch.randn(batch, in_f, device=DEV, generator=g) + 20 * w[labels.long()].float()).bfloat16()
+        z = torch.cat([x.float() @ w[at:at + 10000].float().t().contiguous() for at in range(0, classes, 10000)], 1).double()
+        want = torch.logsumexp(z, 1) - z.gather(1, labels.long()[:, None])[:, 0]
+        loss, each = torch.empty((), device=DEV), torch.empty(batch, device=DEV)
+        ws = torch.empty(vcnn.fc_softmax_loss_workspace_bytes(vcnn.BF16, batch, in_f, classes, False), dtype=torch.uint8, device=DEV)
+        vcnn.fc_softmax_loss(vcnn.BF16, batch, in_f, classes, x, w, None, labels, IGNORE, loss, each, None, None, None, ws)
+        # both sides' sums: at most in_f roundings of the sum of magnitudes each, here some 20 * in_f / 64 / 64 + 2 |x| |w|
+        most = 2 * 2 * (in_f / 16) * U * float((x.float().abs() @ w[:1000].float().abs().t()).max()) * 2
+        assert float((each.double() - want).abs().max()) <= most
 
 
 def test_refusals_need_no_gpu():

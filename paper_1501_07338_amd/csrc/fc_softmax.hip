@@ -320,17 +320,20 @@ struct FewShape {
   int tiles, sharing;  // MA; waves of one sum: enough blocks for the chip
   int block_classes() const { return 16 * tiles * kFewWaves / sharing; }
 };
+// Pairs of tiles where both are many (they halve the samples' way from the caches).  Sums are shared until there are blocks for the
+// chip, and no further: bfloat16, 8 samples 8192 -> 20000 100, 102, 83, 93 us with one, two, four, eight waves a sum (157 blocks
+// with one), 4 of 2048 -> 50000 49.8, 51.4, 52.7, 104 (391).
 static FewShape few_shape(int rows, int64_t classes) {
-  if (classes >= 16 * 2 * kFewWaves * 64) return {rows > 16 ? 2 : 1, 1};
+  if (rows > 16 && classes >= 16 * 2 * kFewWaves * 256) return {2, 1};
   FewShape s{1, 1};
-  while (s.sharing < kFewWaves && ceil_div(classes, s.block_classes()) < 256) s.sharing *= 2;
+  while (s.sharing < kFewWaves && ceil_div(classes, s.block_classes()) < 384) s.sharing *= 2;
   return s;
 }
 
 template <typename T, int MA, int NB>
 __global__ __launch_bounds__(kFewThreads) void loss_few_kernel(LossProduct a, const T* xs, const T* ws, int in_f, int sharing) {
-  constexpr bool TURNS = sizeof(T) == 2 && MA * NB > 1;
-  constexpr int AHEAD = TURNS ? 2 : MA * NB == 1 ? 8 : 4, N = 16 / sizeof(T), STEP = 4 * N;  // elements of a load, and of a row's four
+  constexpr bool TURNS = sizeof(T) == 2;
+  constexpr int AHEAD = (MA * NB == 1 ? 8 : 4) / (TURNS ? 2 : 1), N = 16 / sizeof(T), STEP = 4 * N;  // elements of a load, and of a row's four
   __shared__ float2 parts[kFewWaves][NB * 16];
   __shared__ float shares[MA == 1 ? kFewWaves : 1][NB * 4][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, at = (lane >> 4) * N;

@@ -5,13 +5,16 @@
 // The samples go through in parts.  A part's logits are made once (z, float), by a product whose tiles leave the largest logit of
 // each sample and its sum of exponentials beside them; these are joined; one pass turns z where it stands into d, a high
 // and a low bfloat16 term of the difference, and two products make dx and dw from it.  Without gradients z is not stored at all.
+// (Making the logits a second time instead would take a quarter more products; a float stored, read and replaced by its two terms
+// takes a third of that at 4096 inputs, and bounds the pass: 4096 x 65536 in 434 us, 4.9 TB/s.)
 //   d in two terms: dw is float, and one bfloat16 term alone would leave up to 2^-8 of each element in it (the two leave 2^-16).  dx is
 //   bfloat16 itself and takes the high term alone.
 //   float: x, w and d in two half-precision terms each (22 bits), products high x high, high x low and low x high, three
-//   where the float instruction would take sixteen.  x and w are scaled by a power of two a row so that its largest element comes to
-//   2^14 .. 2^15, but by at most 2^8 more than the row with the largest element of all, and d by 2^14 and the inverse of what its
-//   sample's and its class's rows were scaled by beyond that.  What falls below 2^-24 in half precision is lost: 2^-39 of a row's
-//   largest element, and 2^-39 of 1 in an element of d, 2^-23 at the worst (where a float keeps 2^-24 of p - 1).
+//   where the float instruction would take sixteen (1001 x 1100 -> 30011 with gradients 0.76 ms, by the float products 3.46).  x and w
+//   are scaled by a power of two a row so that its largest element comes to 2^14 .. 2^15, but by at most 2^8 more than the row with the
+//   largest element of all, and d by 2^14 and the inverse of what its sample's and its class's rows were scaled by beyond that.  What
+//   falls below 2^-24 in half precision is lost: 2^-39 of a row's largest element, and 2^-39 of 1 in an element of d, 2^-23 at the
+//   worst (where a float keeps 2^-24 of p - 1).
 #include <algorithm>
 
 #include "rows.h"
@@ -315,6 +318,7 @@ __global__ __launch_bounds__(TILE::THREADS, TILE::WAVES_SIMD) void loss_product_
 // instruction wants them, straight into registers: lane l row l % 16, and of every 64 bytes of it the 16 from 16 (l / 16) on.  (Which
 // steps of the sum a lane holds does not matter as long as it is the same ones of both.)  Of few classes `sharing` waves share a sum.
 // The eight waves of a block leave one maximum and sum of their classes.
+// 1 sample 4096 -> 65536 in bfloat16 109 us (4.9 TB/s, half of w from the last-level cache), in float 215.
 static constexpr int kFewThreads = 512, kFewWaves = kFewThreads / 64, kFewRows = 64;
 struct FewShape {
   int tiles, sharing;  // MA; waves of one sum: enough blocks for the chip
@@ -467,7 +471,7 @@ __global__ __launch_bounds__(kFewThreads) void loss_few_kernel(LossProduct a, co
 // 256 inputs (four a lane) and, four at a time, every fourth of its block's classes; lane l makes the d of sample l % 16 and class l / 16
 // of the four, and every lane takes it from there for its share of
 //     dx[b] += d[b] w,   dw = sum over b of d[b] x[b]
-// The blocks' shares of dx are joined by loss_join_kernel.
+// The blocks' shares of dx are joined by loss_join_kernel.  4 samples 2048 -> 50000 in bfloat16: 157 us for 614 MB.
 static constexpr int kFewGrad = 16;
 struct LossFewGrad {
   const void* x;

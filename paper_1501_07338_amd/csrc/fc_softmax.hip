@@ -1056,10 +1056,11 @@ static vcnn_status loss_products(LossPlan p, int batch, int in_f, int classes, c
 }
 
 // ---- small float layers --------------------------------------------------------------------------------------------------
-// A block a sample: z to d / C where it stands, what the sample costs, and its x, zeros if it does not count (whatever it holds must not
+// A block a sample (which counts those that count by itself without meta): z to d / C where it stands, what the sample costs, and its x, zeros if it does not count (whatever it holds must not
 // meet the zeros of d as a NaN).
 __global__ __launch_bounds__(kThreads) void loss_float_kernel(float* z, int classes, const int32_t* labels, int ignore,
-                                                              int batch, int grads, float* each, const float* x, float* x_to, int in_f) {
+                                                              int batch, int grads, const LossMeta* meta, float* each, const float* x,
+                                                              float* x_to, int in_f) {
   __shared__ float parts[kThreads / 64];
   __shared__ int counts[kThreads / 64];
   const int b = blockIdx.x, label = labels[b];
@@ -1072,7 +1073,7 @@ __global__ __launch_bounds__(kThreads) void loss_float_kernel(float* z, int clas
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
   int n = 0;
-  if (grads) {
+  if (grads && !meta) {
     for (int i = threadIdx.x; i < batch; i += kThreads) n += labels[i] != ignore;
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) n += __shfl_xor(n, d);
@@ -1095,7 +1096,7 @@ __global__ __launch_bounds__(kThreads) void loss_float_kernel(float* z, int clas
   if (threadIdx.x == 0) each[b] = !counted ? 0.f : good ? lse - row[label] : __builtin_nanf("");
   if (!grads) return;
   __syncthreads();
-  const float inverse = n ? 1.f / (float)n : 0.f;
+  const float inverse = meta ? meta->inverse : n ? 1.f / (float)n : 0.f;
   for (int c = threadIdx.x; c < classes; c += kThreads) {
     const float d = (expf(row[c] - lse) - (c == label ? 1.f : 0.f)) * inverse;
     row[c] = !counted ? 0.f : good ? d : __builtin_nanf("");
@@ -1107,7 +1108,7 @@ struct LossFloatPlan {
 };
 static LossFloatPlan loss_float_plan(int batch, int in_f, int classes, bool grads) {
   LossFloatPlan p{};
-  size_t at = 0;
+  size_t at = 256;  // (LossMeta)
   auto take = [&](size_t bytes) {
     const size_t here = at;
     at += (bytes + 255) & ~(size_t)255;
@@ -1135,8 +1136,10 @@ static vcnn_status loss_float(int batch, int in_f, int classes, const float* x, 
   float* const each = sample_loss ? sample_loss : (float*)(ws + p.each);
   float* const z = (float*)(ws + p.z);
   if (vcnn_status s = vcnn_fc_fwd(VCNN_F32, batch, in_f, classes, VCNN_ACT_NONE, x, w, bias, z, st)) return s;
-  hipLaunchKernelGGL(loss_float_kernel, dim3((unsigned)batch), dim3(kThreads), 0, st, z, classes, labels, ignore, batch, (int)grads, each,
-                     x, dw ? (float*)(ws + p.x) : nullptr, in_f);
+  LossMeta* const meta = grads && batch > 1024 ? (LossMeta*)ws : nullptr;
+  if (meta) hipLaunchKernelGGL(loss_meta_kernel, dim3(1), dim3(1024), 0, st, labels, batch, ignore, 1, meta);
+  hipLaunchKernelGGL(loss_float_kernel, dim3((unsigned)batch), dim3(kThreads), 0, st, z, classes, labels, ignore, batch, (int)grads, meta,
+                     each, x, dw ? (float*)(ws + p.x) : nullptr, in_f);
   if (vcnn_status s = check_launch("fc_softmax_loss rows")) return s;
   if (dw) x = (const float*)(ws + p.x);
   if (grads)

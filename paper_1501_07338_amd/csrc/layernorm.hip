@@ -5,8 +5,8 @@
 //
 // All of it is bandwidth (and, with dropout, the generator's products).  A row is read once and kept in registers over its sums,
 // divided over threads as in rows.h; rows of more than 16384 elements are read twice.  bfloat16, with a residual: 8192 x 5120 forward
-// 61.6 us (5.4 TB/s, the residual stream in part from the last-level cache; a large copy 5.1); with dropout, 4096 x 4096 forward 27.3
-// (4.9 TB/s) and backward 38.8 and 7.2 us for the two sums; float 2999 x 5003 forward 55.5, backward 63.6 and 10.5.
+// 61.6 us (5.4 TB/s, the residual stream in part from the last-level cache; a large copy 5.1); with dropout, 4096 x 4096 forward 26.7
+// (5.0 TB/s) and backward 38.2 and 4.8 us for the two sums; float 2999 x 5003 forward 54.9, backward 61.9 and 8.1.
 // Groups of eight elements in float too (a block of random words each, 32 bytes a lane) were slower: forward 64, backward 97 us.
 #include "dropout.h"
 #include "rows.h"
@@ -14,6 +14,23 @@
 namespace vcnn {
 
 // ---- sums over a row's threads -------------------------------------------------------------------------------------------
+// As wave_sum, the same pairs, but through the registers: four exchanges within sixteen lanes (by a lane, by two, mirrored in eight
+// and in sixteen, where the sums already are alike), two between them.
+template <int CONTROL>
+__device__ __forceinline__ float moved(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CONTROL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float quick_sum(float v) {
+  v += moved<0xB1>(v);   // quad_perm 1 0 3 2
+  v += moved<0x4E>(v);   // quad_perm 2 3 0 1
+  v += moved<0x141>(v);  // row_half_mirror
+  v += moved<0x140>(v);  // row_mirror
+  v += __shfl_xor(v, 16);
+  v += __shfl_xor(v, 32);
+  return v;
+}
+__device__ __forceinline__ double quick_sum(double v) { return wave_sum(v); }
+
 template <typename S>
 struct PairSums {  // one slot per wave; two sets, taken in turn
   S a[2][kMaxWaves], b[2][kMaxWaves];
@@ -22,13 +39,26 @@ struct PairSums {  // one slot per wave; two sets, taken in turn
 // every wave's reading of it.
 template <bool WAVE, typename S>
 __device__ __forceinline__ void pair_reduce(PairSums<S>& s, int& turn, S& x, S& y) {
-  x = wave_sum(x), y = wave_sum(y);
+  x = quick_sum(x), y = quick_sum(y);
   if constexpr (!WAVE) {
     const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
     if ((threadIdx.x & 63) == 0) s.a[turn][wave] = x, s.b[turn][wave] = y;
     __syncthreads();
     x = 0, y = 0;
     for (int w = 0; w < waves; ++w) x += s.a[turn][w], y += s.b[turn][w];
+    turn ^= 1;
+  }
+}
+
+template <bool WAVE, typename S>
+__device__ __forceinline__ void row_sum(PairSums<S>& s, int& turn, S& x) {
+  x = quick_sum(x);
+  if constexpr (!WAVE) {
+    const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    if ((threadIdx.x & 63) == 0) s.a[turn][wave] = x;
+    __syncthreads();
+    x = 0;
+    for (int w = 0; w < waves; ++w) x += s.a[turn][w];
     turn ^= 1;
   }
 }
@@ -137,7 +167,7 @@ __global__ __launch_bounds__(WAVE ? kWaveThreads : NV ? kKeptThreads : 1024, NV 
     float m0, shift, rstd;
     bool again = false;
     if constexpr (NV > 0) {
-      float sum = 0.f, zero = 0.f;
+      float sum = 0.f;
       uint32_t words[K][N / 2];
       if constexpr (DROP) dropout_words<N, K>(key, (uint64_t)row * blocks, per_row, tid, words);
 #pragma unroll
@@ -150,7 +180,7 @@ __global__ __launch_bounds__(WAVE ? kWaveThreads : NV ? kKeptThreads : 1024, NV 
         }
       }
       if (row + stride < a.rows) fetch(row + stride);
-      pair_reduce<WAVE>(sums, turn, sum, zero);
+      row_sum<WAVE>(sums, turn, sum);
       m0 = sum / (float)cols;
       float off = 0.f, squares = 0.f;
       each([&](int, int c, const float (&u)[N]) {
@@ -185,12 +215,11 @@ __global__ __launch_bounds__(WAVE ? kWaveThreads : NV ? kKeptThreads : 1024, NV 
           sum += d, squares += d * d, ++count;
         }
       }
-      double total = sum + count * first, zero = 0.;
-      pair_reduce<WAVE>(wide_sums, wide_turn, total, zero);
+      double total = sum + count * first;
+      row_sum<WAVE>(wide_sums, wide_turn, total);
       const double mean = total / cols, off = first - mean;  // (v - mean = d + off)
       squares += 2. * off * sum + count * off * off;
-      zero = 0.;
-      pair_reduce<WAVE>(wide_sums, wide_turn, squares, zero);
+      row_sum<WAVE>(wide_sums, wide_turn, squares);
       m0 = (float)mean, shift = (float)(mean - m0);
       const float variance = (float)(fmax(squares, 0.) / cols) + a.eps;
       rstd = 1.f / sqrtf(variance);
@@ -198,12 +227,12 @@ __global__ __launch_bounds__(WAVE ? kWaveThreads : NV ? kKeptThreads : 1024, NV 
     }
     double wide_mean = 0., wide_rstd = 0.;
     if (again) {
-      double total = 0., zero = 0.;
+      double total = 0.;
       each([&](int, int c, const float (&u)[N]) {
 #pragma unroll
         for (int i = 0; i < N; ++i) total += (double)u[i];  // (zeros behind the row's end)
       });
-      pair_reduce<WAVE>(wide_sums, wide_turn, total, zero);
+      row_sum<WAVE>(wide_sums, wide_turn, total);
       wide_mean = total / cols;
       double squares = 0.;
       each([&](int, int c, const float (&u)[N]) {
@@ -213,8 +242,7 @@ __global__ __launch_bounds__(WAVE ? kWaveThreads : NV ? kKeptThreads : 1024, NV 
           squares += d * d;
         }
       });
-      zero = 0.;
-      pair_reduce<WAVE>(wide_sums, wide_turn, squares, zero);
+      row_sum<WAVE>(wide_sums, wide_turn, squares);
       wide_rstd = 1. / sqrt(squares / cols + (double)a.eps);
       m0 = (float)wide_mean, shift = 0.f, rstd = (float)wide_rstd;
     }
@@ -271,7 +299,7 @@ struct LayerNormBwdArgs {
   Dropout drop;
 };
 
-static constexpr int kLnBwdBlocks = 512;  // (256: 4096 x 4096 of bfloat16 42.5 and 4.5 us, not 38.5 and 7.1; 2999 x 5003 of float 76.7 and 7.8, not 64.0 and 10.4)
+static constexpr int kLnBwdBlocks = 512;  // (256: 4096 x 4096 of bfloat16 42.5 us, not 38.5; 2999 x 5003 of float 76.7, not 64.0)
 
 template <typename T, bool DROP, int NV, bool WAVE>
 __global__ __launch_bounds__(WAVE ? kWaveThreads : NV ? kKeptThreads : 1024) void layernorm_bwd_kernel(LayerNormBwdArgs a) {
@@ -429,18 +457,19 @@ __global__ __launch_bounds__(WAVE ? kWaveThreads : NV ? kKeptThreads : 1024) voi
   }
 }
 
-// dg and db from the blocks' shares: 64 threads a column take every 64th, and their sums are added in pairs, always the same ones.
+// dg and db from the blocks' shares: 32 threads a column take every 32nd, and their sums are added in pairs, always the same ones.
+static constexpr int kAffineColumns = 32, kAffineParts = 1024 / kAffineColumns;
 __global__ __launch_bounds__(1024) void affine_grad_kernel(const float* partial, float* dg, float* db, int blocks, int cols) {
-  __shared__ float sums[64][17];
-  const int in = threadIdx.x & 15, part = threadIdx.x >> 4;
-  const int64_t col = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 16 + in;  // of the 2 cols
+  __shared__ float sums[kAffineParts][kAffineColumns + 1];
+  const int in = threadIdx.x % kAffineColumns, part = threadIdx.x / kAffineColumns;
+  const int64_t col = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kAffineColumns + in;  // of the 2 cols
   float s = 0.f;
   if (col < 2 * (int64_t)cols) {
-#pragma unroll 8
-    for (int b = part; b < blocks; b += 64) s += partial[(int64_t)b * 2 * cols + col];
+#pragma unroll 16
+    for (int b = part; b < blocks; b += kAffineParts) s += partial[(int64_t)b * 2 * cols + col];
   }
   sums[part][in] = s;
-  for (int n = 32; n > 0; n >>= 1) {
+  for (int n = kAffineParts / 2; n > 0; n >>= 1) {
     __syncthreads();
     if (part < n) sums[part][in] += sums[part + n][in];
   }
@@ -478,7 +507,7 @@ vcnn_status launch_layernorm_bwd(int dtype, int rows, int cols, const Dropout& d
     blocks = drop.rng ? launch_layernorm_bwd_typed<float, true>(a, st) : launch_layernorm_bwd_typed<float, false>(a, st);
   if (vcnn_status s = check_launch("layernorm_bwd")) return s;
   if (!a.partial) return VCNN_OK;
-  const unsigned groups = (unsigned)ceil_div(2 * (int64_t)cols, 16), wide = std::min(groups, 1u << 16);
+  const unsigned groups = (unsigned)ceil_div(2 * (int64_t)cols, kAffineColumns), wide = std::min(groups, 1u << 16);
   hipLaunchKernelGGL(affine_grad_kernel, dim3(wide, (unsigned)ceil_div(groups, wide)), dim3(1024), 0, st, partial, dgain, dbias,
                      blocks, cols);
   return check_launch("layernorm_bwd gain and bias");

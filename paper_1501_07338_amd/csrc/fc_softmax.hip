@@ -1056,49 +1056,100 @@ static vcnn_status loss_products(LossPlan p, int batch, int in_f, int classes, c
 }
 
 // ---- small float layers --------------------------------------------------------------------------------------------------
-// A block a sample (which counts those that count by itself without meta): z to d / C where it stands, what the sample costs, and its x, zeros if it does not count (whatever it holds must not
-// meet the zeros of d as a NaN).
-__global__ __launch_bounds__(kThreads) void loss_float_kernel(float* z, int classes, const int32_t* labels, int ignore,
-                                                              int batch, int grads, const LossMeta* meta, float* each, const float* x,
-                                                              float* x_to, int in_f) {
+struct LossFloat {
+  float* z;              // [batch][classes]; d / C afterwards (grads)
+  int classes, batch, ignore, grads, in_f, sample_blocks;
+  const int32_t* labels;
+  const LossMeta* meta;  // null: every sample's threads count those that count
+  float* each;
+  const float* x;
+  float* x_to;           // nullable: x with zeros for the samples that do not count (whatever they hold must not meet the zeros of d
+                         // as a NaN), by the blocks behind the samples'
+};
+// What each sample costs, and z to d / C where it stands.  KEPT: a wave a sample of at most 512 classes, in registers; else a block.
+static constexpr int kKeptClasses = 512;
+template <bool KEPT>
+__global__ __launch_bounds__(kThreads) void loss_float_kernel(LossFloat a) {
   __shared__ float parts[kThreads / 64];
   __shared__ int counts[kThreads / 64];
-  const int b = blockIdx.x, label = labels[b];
-  float* const row = z + (int64_t)b * classes;
-  const bool counted = label != ignore, good = label >= 0 && label < classes;
-  if (x_to)
-    for (int64_t i = (int64_t)b * in_f + threadIdx.x; i < (int64_t)(b + 1) * in_f; i += kThreads) x_to[i] = counted ? x[i] : 0.f;
-  float most = -__builtin_inff();
-  for (int c = threadIdx.x; c < classes; c += kThreads) most = fmaxf(most, row[c]);
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, classes = a.classes;
+  if ((int)blockIdx.x >= a.sample_blocks) {
+    const int blocks = gridDim.x - a.sample_blocks;
+    for (int64_t row = (int64_t)(blockIdx.x - a.sample_blocks) * (kThreads / 64) + wave; row < a.batch; row += (int64_t)blocks * (kThreads / 64)) {
+      const bool counted = a.labels[row] != a.ignore;
+#pragma unroll 4
+      for (int c = lane * 4; c < a.in_f; c += 256) {
+        Loose16 v{{0, 0, 0, 0}};
+        if (counted) v = load_group(a.x + row * a.in_f, c, a.in_f);
+        store_group(a.x_to + row * a.in_f, c, a.in_f, v);
+      }
+    }
+    return;
+  }
+  const int b = KEPT ? blockIdx.x * (kThreads / 64) + wave : blockIdx.x;
+  if (b >= a.batch) return;  // (KEPT: waves are on their own)
+  const int label = a.labels[b];
+  const bool counted = label != a.ignore, good = label >= 0 && label < classes;
+  float* const row = a.z + (int64_t)b * classes;
   int n = 0;
-  if (grads && !meta) {
-    for (int i = threadIdx.x; i < batch; i += kThreads) n += labels[i] != ignore;
+  if (a.grads && !a.meta) {
+    for (int i = KEPT ? lane : threadIdx.x; i < a.batch; i += KEPT ? 64 : kThreads) n += a.labels[i] != a.ignore;
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) n += __shfl_xor(n, d);
   }
-  if ((threadIdx.x & 63) == 0) parts[threadIdx.x >> 6] = most, counts[threadIdx.x >> 6] = n;
+  float most = -__builtin_inff(), sum = 0.f;
+  if constexpr (KEPT) {
+    constexpr int K = kKeptClasses / 64;
+    float v[K], at = 0.f;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int c = k * 64 + lane;
+      v[k] = c < classes ? row[c] : -__builtin_inff();
+      most = fmaxf(most, v[k]);
+      if (k == label >> 6) at = v[k];
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
+    at = __shfl(at, label & 63);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      v[k] = k * 64 + lane < classes ? expf(v[k] - most) : 0.f;
+      sum += v[k];
+    }
+    sum = wave_sum(sum);
+    if (lane == 0) a.each[b] = !counted ? 0.f : good ? (most + logf(sum)) - at : __builtin_nanf("");
+    if (!a.grads) return;
+    const float inverse = a.meta ? a.meta->inverse : n ? 1.f / (float)n : 0.f, share = 1.f / sum;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int c = k * 64 + lane;
+      const float d = (v[k] * share - (c == label ? 1.f : 0.f)) * inverse;
+      if (c < classes) row[c] = !counted ? 0.f : good ? d : __builtin_nanf("");
+    }
+    return;
+  }
+  for (int c = threadIdx.x; c < classes; c += kThreads) most = fmaxf(most, row[c]);
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
+  if (lane == 0) parts[wave] = most, counts[wave] = n;
   __syncthreads();
   n = 0;
 #pragma unroll
   for (int w = 0; w < kThreads / 64; ++w) most = fmaxf(most, parts[w]), n += counts[w];
   __syncthreads();
-  float sum = 0.f;
   for (int c = threadIdx.x; c < classes; c += kThreads) sum += expf(row[c] - most);
   sum = wave_sum(sum);
-  if ((threadIdx.x & 63) == 0) parts[threadIdx.x >> 6] = sum;
+  if (lane == 0) parts[wave] = sum;
   __syncthreads();
   sum = 0.f;
 #pragma unroll
   for (int w = 0; w < kThreads / 64; ++w) sum += parts[w];
-  const float lse = most + logf(sum);
-  if (threadIdx.x == 0) each[b] = !counted ? 0.f : good ? lse - row[label] : __builtin_nanf("");
-  if (!grads) return;
+  if (threadIdx.x == 0) a.each[b] = !counted ? 0.f : good ? (most + logf(sum)) - row[label] : __builtin_nanf("");
+  if (!a.grads) return;
   __syncthreads();
-  const float inverse = meta ? meta->inverse : n ? 1.f / (float)n : 0.f;
+  const float inverse = a.meta ? a.meta->inverse : n ? 1.f / (float)n : 0.f, share = 1.f / sum;
   for (int c = threadIdx.x; c < classes; c += kThreads) {
-    const float d = (expf(row[c] - lse) - (c == label ? 1.f : 0.f)) * inverse;
+    const float d = (expf(row[c] - most) * share - (c == label ? 1.f : 0.f)) * inverse;
     row[c] = !counted ? 0.f : good ? d : __builtin_nanf("");
   }
 }
@@ -1138,8 +1189,12 @@ static vcnn_status loss_float(int batch, int in_f, int classes, const float* x, 
   if (vcnn_status s = vcnn_fc_fwd(VCNN_F32, batch, in_f, classes, VCNN_ACT_NONE, x, w, bias, z, st)) return s;
   LossMeta* const meta = grads && batch > 1024 ? (LossMeta*)ws : nullptr;
   if (meta) hipLaunchKernelGGL(loss_meta_kernel, dim3(1), dim3(1024), 0, st, labels, batch, ignore, 1, meta);
-  hipLaunchKernelGGL(loss_float_kernel, dim3((unsigned)batch), dim3(kThreads), 0, st, z, classes, labels, ignore, batch, (int)grads, meta,
-                     each, x, dw ? (float*)(ws + p.x) : nullptr, in_f);
+  const bool kept = classes <= kKeptClasses;
+  const int sample_blocks = kept ? (int)ceil_div(batch, kThreads / 64) : batch;
+  const LossFloat a{z, classes, batch, ignore, (int)grads, in_f, sample_blocks, labels, meta, each, x, dw ? (float*)(ws + p.x) : nullptr};
+  const unsigned blocks = sample_blocks + (dw ? (unsigned)std::min<int64_t>(ceil_div(batch, kThreads / 64), 2048) : 0);
+  if (kept) hipLaunchKernelGGL(loss_float_kernel<true>, dim3(blocks), dim3(kThreads), 0, st, a);
+  else hipLaunchKernelGGL(loss_float_kernel<false>, dim3(blocks), dim3(kThreads), 0, st, a);
   if (vcnn_status s = check_launch("fc_softmax_loss rows")) return s;
   if (dw) x = (const float*)(ws + p.x);
   if (grads)

@@ -2,13 +2,13 @@
 //     z = x w^T + bias,   lse_r = log sum exp z_r,   loss = 1/C sum over the C samples that count of lse_r - z_r[label]
 //     d = softmax(z) - onehot(label) (0 for samples that do not count),   dx = d w / C,   dw = d^T x / C,   dbias = sum_r d_r / C
 //
-// The samples go through in parts.  A part's logits are made once (z, float), by a product whose tiles leave the largest logit of
-// each sample and its sum of exponentials beside them; these are joined; one pass turns z where it stands into d, a high
-// and a low bfloat16 term of the difference, and two products make dx and dw from it.  Without gradients z is not stored at all.
-// (Making the logits a second time instead would take a quarter more products; a float stored, read and replaced by its two terms
-// takes a third of that at 4096 inputs, and bounds the pass: 4096 x 65536 in 434 us, 4.9 TB/s.)
-//   d in two terms: dw is float, and one bfloat16 term alone would leave up to 2^-8 of each element in it (the two leave 2^-16).  dx is
-//   bfloat16 itself and takes the high term alone.
+// The samples go through in parts. A part's logits are made once (z, float), by a product whose tiles leave the largest logit of
+// each sample and its sum of exponentials beside them; these are joined; one pass turns z where it stands into d, in two or three
+// bfloat16 terms, and two products make dx and dw from it. Without gradients z is not stored at all. (Making the logits a second
+// time instead would take a quarter more products; a float stored, read and replaced by its two terms takes a third of that at 4096
+// inputs, and bounds the pass: 4096 x 65536 in 434 us, 4.9 TB/s.)
+//   d in terms: dw is float, and one bfloat16 term alone would leave up to 2^-8 of each element in it (kTwoTerms: two 2^-16, three
+//   2^-24). dx is bfloat16 itself and takes the first term alone.
 //   float: x, w and d in two half-precision terms each (22 bits), products high x high, high x low and low x high, three
 //   where the float instruction would take sixteen (1001 x 1100 -> 30011 with gradients 0.76 ms, by the float products 3.46).  x and w
 //   are scaled by a power of two a row so that its largest element comes to 2^14 .. 2^15, but by at most 2^8 more than the row with the
@@ -161,8 +161,9 @@ struct LossProduct {
   ProductArgs p;
   int rows, cols;        // of the result
   // EPI_LOGITS: a classes, b samples
-  float* z;              // [rows][z_pitch] (nullable)
+  float* z;              // [rows][z_pitch] (nullable), z_group floats from 64 classes to the next
   int64_t z_pitch;
+  int z_group;
   const float* bias;     // nullable
   const int32_t* labels;
   float2* stats;         // [16 TA of classes][rows]: the largest logit, the sum of exponentials about it
@@ -200,13 +201,13 @@ __device__ __forceinline__ void store4(T* at, const float (&v)[4], int n) {
   }
 }
 
-template <typename TILE, int EPI, bool F32, bool A_ALONG, bool B_ALONG, bool B_PLANES>
+template <typename TILE, int EPI, bool F32, bool A_ALONG, bool B_ALONG, int B_PLANES>
 __global__ __launch_bounds__(TILE::THREADS, TILE::WAVES_SIMD) void loss_product_kernel(LossProduct a) {
   extern __shared__ uint4 smem16[];
   int ta, tb;
   product_tile_of(a.p, &ta, &tb);
   f32x4 acc[TILE::TA][TILE::TB];
-  slab_product<TILE, F32, A_ALONG, F32, B_ALONG, B_PLANES>(a.p, ta * TILE::BA, tb * TILE::BB, smem16, acc);
+  slab_product<TILE, F32, A_ALONG, F32 ? 2 : 1, B_ALONG, B_PLANES>(a.p, ta * TILE::BA, tb * TILE::BB, smem16, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int a0 = ta * TILE::BA + (wave % TILE::WA) * 16 * TILE::TA, b0 = tb * TILE::BB + (wave / TILE::WA) * 16 * TILE::TB;
   const int ca = a0 + 4 * (lane >> 4);  // + 16 i + q
@@ -271,7 +272,7 @@ __global__ __launch_bounds__(TILE::THREADS, TILE::WAVES_SIMD) void loss_product_
       for (int i = 0; i < TILE::TA; ++i) {
         const int c = ca + 16 * i, at = label - c;
         const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
-        if (a.z && c < a.cols) *reinterpret_cast<float4*>(z + c) = make_float4(v[0], v[1], v[2], v[3]);  // (rows have whole groups)
+        if (a.z && c < a.cols) *reinterpret_cast<float4*>(z + (c >> 6) * a.z_group + (c & 63)) = make_float4(v[0], v[1], v[2], v[3]);  // (rows have whole groups)
         if (at >= 0 && at < 4 && label < a.cols) a.at_label[b] = at == 0 ? v[0] : at == 1 ? v[1] : at == 2 ? v[2] : v[3];
       }
     }
@@ -687,9 +688,10 @@ __global__ __launch_bounds__(1024) void loss_few_rows_kernel(LossRows a) {
   if (lane == 0) *a.loss = n ? s / (float)n : 0.f;
 }
 
-// z to d where it stands: 64 floats of a row become 64 high and 64 low terms (the sixteen lanes that read them are of one wave, which
-// has them all before it writes); behind the last class zeros.  Each block leaves its samples' share of dbias.
-template <bool F32>
+// z to d where it stands: 64 floats of a row become 64 high and 64 low terms, and 64 lower ones, for which z leaves room (the sixteen
+// lanes that read them are of one wave, which has them all before it writes); behind the last class zeros.  Each block leaves its
+// samples' share of dbias.
+template <bool F32, int TERMS>
 __global__ __launch_bounds__(kThreads) void loss_grad_kernel(float* z, int64_t pitch, int rows, int classes, const int32_t* labels,
                                                              int ignore, const float2* softmax, const float* down_x, const float* down_w,
                                                              float* shares, int64_t share_pitch) {
@@ -707,10 +709,10 @@ __global__ __launch_bounds__(kThreads) void loss_grad_kernel(float* z, int64_t p
     const int label = labels[b];
     const bool counts = label != ignore, bad = counts && (label < 0 || label >= classes);
     const float2 about = softmax[b];
-    char* const row = reinterpret_cast<char*>(z + b * pitch);
-    const float4 v = *reinterpret_cast<const float4*>(row + c * 4);
+    char* const row = reinterpret_cast<char*>(z + b * pitch) + (int64_t)blockIdx.x * (TERMS * 128);
+    const float4 v = *reinterpret_cast<const float4*>(row + in * 16);
     float d[4] = {v.x, v.y, v.z, v.w};
-    uint2 h, r;
+    uint2 h, r, u;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       d[q] = exp_of(d[q] - about.x) * about.y - (c + q == label ? 1.f : 0.f);
@@ -729,18 +731,23 @@ __global__ __launch_bounds__(kThreads) void loss_grad_kernel(float* z, int64_t p
       }
       h = __builtin_bit_cast(uint2, hi), r = __builtin_bit_cast(uint2, lo);
     } else {
-      bf16x2 hi[2], lo[2];
+      uint32_t term[3][2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        hi[i] = __builtin_convertvector((f32x2){d[2 * i], d[2 * i + 1]}, bf16x2);
-        lo[i] = __builtin_convertvector((f32x2){d[2 * i] - (float)hi[i][0], d[2 * i + 1] - (float)hi[i][1]}, bf16x2);
+        float rest[2] = {d[2 * i], d[2 * i + 1]};
+#pragma unroll
+        for (int t = 0; t < TERMS; ++t) {
+          const bf16x2 to = __builtin_convertvector((f32x2){rest[0], rest[1]}, bf16x2);
+          term[t][i] = __builtin_bit_cast(uint32_t, to);
+          rest[0] -= (float)to[0], rest[1] -= (float)to[1];
+        }
       }
-      h = make_uint2(__builtin_bit_cast(uint32_t, hi[0]), __builtin_bit_cast(uint32_t, hi[1]));
-      r = make_uint2(__builtin_bit_cast(uint32_t, lo[0]), __builtin_bit_cast(uint32_t, lo[1]));
+      h = make_uint2(term[0][0], term[0][1]), r = make_uint2(term[1][0], term[1][1]);
+      if constexpr (TERMS == 3) u = make_uint2(term[2][0], term[2][1]);
     }
-    char* const to = row + (int64_t)blockIdx.x * 256 + in * 8;
-    *reinterpret_cast<uint2*>(to) = h;
-    *reinterpret_cast<uint2*>(to + 128) = r;
+    *reinterpret_cast<uint2*>(row + in * 8) = h;
+    *reinterpret_cast<uint2*>(row + 128 + in * 8) = r;
+    if constexpr (TERMS == 3) *reinterpret_cast<uint2*>(row + 256 + in * 8) = u;
   }
   if (!shares) return;
 #pragma unroll
@@ -784,10 +791,10 @@ __global__ __launch_bounds__(1024) void loss_mean_kernel(const float* each, cons
 }
 
 // ---- plan ----------------------------------------------------------------------------------------------------------------
-// One plane of each; d in two; both in two.  256 x 256 of the first and 256 x 128 of the others are what the registers of eight waves
+// One plane of each; d in two or three; both in two.  256 x 256 of the first and 256 x 128 of the others are what the registers of eight waves
 // and a ring in LDS that stays ahead of the memory allow; the smaller ones spread few outputs over more of the chip.
 enum { TILE_LARGE = 0, TILE_SMALL = 1, TILE_FLAT = 2, TILE_LEAST = 3 };
-template <int TILE, int PLANES>  // planes of d: 1 or 2; 4: float
+template <int TILE, int PLANES>  // planes of d: 1, 2 or 3; 4: float
 struct TileOf;
 template <> struct TileOf<TILE_LARGE, 1> { using type = ProductTile<256, 256, 8, 4, 1, 1, 4>; };
 template <> struct TileOf<TILE_SMALL, 1> { using type = ProductTile<128, 128, 4, 4, 1, 1, 4>; };
@@ -797,6 +804,10 @@ template <> struct TileOf<TILE_LARGE, 2> { using type = ProductTile<256, 128, 8,
 template <> struct TileOf<TILE_SMALL, 2> { using type = ProductTile<128, 128, 4, 4, 1, 2, 3>; };
 template <> struct TileOf<TILE_FLAT, 2> { using type = ProductTile<128, 64, 4, 2, 1, 2, 5>; };
 template <> struct TileOf<TILE_LEAST, 2> { using type = ProductTile<64, 64, 2, 2, 1, 2, 6>; };
+template <> struct TileOf<TILE_LARGE, 3> { using type = ProductTile<256, 128, 8, 2, 1, 3, 4>; };
+template <> struct TileOf<TILE_SMALL, 3> { using type = ProductTile<128, 64, 4, 2, 1, 3, 4>; };
+template <> struct TileOf<TILE_FLAT, 3> { using type = ProductTile<128, 64, 4, 2, 1, 3, 4>; };
+template <> struct TileOf<TILE_LEAST, 3> { using type = ProductTile<64, 64, 2, 2, 1, 3, 5>; };
 template <> struct TileOf<TILE_LARGE, 4> { using type = ProductTile<256, 128, 4, 4, 2, 2, 3>; };
 template <> struct TileOf<TILE_SMALL, 4> { using type = ProductTile<128, 64, 4, 2, 2, 2, 3>; };
 template <> struct TileOf<TILE_FLAT, 4> { using type = ProductTile<128, 64, 4, 2, 2, 2, 3>; };
@@ -819,7 +830,7 @@ static TileSize tile_size(int planes, int tile) {
     using TILE = typename decltype(t)::type;
     return TileSize{TILE::BA, TILE::BB, 16 * TILE::TA};
   };
-  return planes == 1 ? with_tile<1>(tile, of) : planes == 2 ? with_tile<2>(tile, of) : with_tile<4>(tile, of);
+  return planes == 1 ? with_tile<1>(tile, of) : planes == 2 ? with_tile<2>(tile, of) : planes == 3 ? with_tile<3>(tile, of) : with_tile<4>(tile, of);
 }
 // The largest tile of which there are enough for the chip, also by sharing a sum among up to `sharing` blocks.
 static int tile_for(int planes, int64_t a, int64_t b, int64_t sharing) {
@@ -844,6 +855,7 @@ static int shares_of(int planes, int tile, int64_t a, int64_t b, int slabs, int 
 struct LossPlan {
   int part;            // samples at once
   int classes_pitch;   // elements of a row of z
+  int terms;           // of d
   int groups;          // of eight inputs, of a row as it is relaid
   int64_t x_pitch;     // bytes of such a row
   int stat_tiles;      // of classes
@@ -855,6 +867,12 @@ struct LossPlan {
 
 static constexpr int kMostSamples = 1 << 20;  // of a part
 
+// Two bfloat16 terms of d leave 2^-16 of an element, 1.7e-6 of a dw as measured, and three 2^-24. What sums of n floats lose grows
+// with the root of n: in the same product of floats 5e-7 over 40 samples, 6e-7 over 700, 1.0e-6 over 3000, 1.6e-6 over 4096. So d
+// has two terms from 4096 samples on and three below, which leave 4e-7 over 40 and 700, 6e-7 over 3000. Time with three, with two:
+// 40 x 2048 -> 8192 65, 63 us; 700 x 1024 -> 16384 206, 186; 1024 x 8192 -> 32768 2.36, 2.05 ms; 2048 x 4096 -> 65536 4.70, 4.06.
+static constexpr int kTwoTerms = 4096;
+
 static LossPlan loss_plan(bool f32, int part, int batch, int in_f, int classes, bool grads) {
   LossPlan p{};
   p.f32 = f32, p.part = part;
@@ -864,7 +882,8 @@ static LossPlan loss_plan(bool f32, int part, int batch, int in_f, int classes, 
   p.few_grads = grads && part <= kFewGrad && batch <= kFewGrad;
   p.few = p.few_grads || (!grads && part <= kFewRows);
   p.relay_w = !p.few && (f32 || in_f % 8 != 0);
-  const int planes = f32 ? 4 : 1, planes_dw = f32 ? 4 : 2;
+  p.terms = f32 || p.few || batch >= kTwoTerms ? 2 : 3;
+  const int planes = f32 ? 4 : 1, planes_dw = f32 ? 4 : p.terms;
   const int slabs_dx = (int)ceil_div(classes, 32), slabs_dw = (int)ceil_div(part, 32);
   p.tile_z = tile_for(planes, classes, part, 1), p.tile_dx = tile_for(planes, in_f, part, std::max(1, slabs_dx / 16));
   p.tile_dw = tile_for(planes_dw, in_f, classes, std::max(1, slabs_dw / 8));
@@ -884,7 +903,7 @@ static LossPlan loss_plan(bool f32, int part, int batch, int in_f, int classes, 
   p.stats = take((size_t)p.stat_tiles * part * 8);
   p.at_label = take((size_t)part * 4), p.softmax = take((size_t)part * 8), p.each = take((size_t)batch * 4);
   if (grads) {
-    p.z = take((size_t)part * p.classes_pitch * 4);
+    p.z = take((size_t)part * p.classes_pitch * 2 * p.terms);
     p.partial = take(std::max(p.splits_dx > 1 || p.few_grads ? (size_t)p.splits_dx * part * in_f * 4 : 0,
                               p.splits_dw > 1 ? (size_t)p.splits_dw * classes * in_f * 4 : 0));
     p.shares = take((size_t)ceil_div(part, 64) * p.classes_pitch * 4);
@@ -896,7 +915,7 @@ static LossPlan loss_plan(bool f32, int part, int batch, int in_f, int classes, 
 // The samples in equal parts of whole tiles, the fewest that keep a part's logits (without gradients: its statistics) within `most`.
 static LossPlan loss_plan_within(bool f32, size_t most, int batch, int in_f, int classes, bool grads) {
   const LossPlan one = loss_plan(f32, 64, batch, in_f, classes, grads);
-  const size_t row = grads ? (size_t)one.classes_pitch * 4 : (size_t)one.x_pitch + (size_t)one.stat_tiles * 8;
+  const size_t row = grads ? (size_t)one.classes_pitch * 2 * one.terms : (size_t)one.x_pitch + (size_t)one.stat_tiles * 8;
   const int64_t fit = std::max<int64_t>(64, std::min<int64_t>((int64_t)(most / row), kMostSamples) / 64 * 64), parts = ceil_div(batch, fit);
   int64_t part = ceil_div(batch, parts);
   if (parts > 1) part = std::min(fit, ceil_div(part, part > 256 ? 256 : 64) * (part > 256 ? 256 : 64));
@@ -904,7 +923,7 @@ static LossPlan loss_plan_within(bool f32, size_t most, int batch, int in_f, int
 }
 static constexpr size_t kMostLogits = (size_t)1 << 30;  // bytes of a part's
 
-template <typename TILE, int EPI, bool F32, bool A_ALONG, bool B_ALONG, bool B_PLANES>
+template <typename TILE, int EPI, bool F32, bool A_ALONG, bool B_ALONG, int B_PLANES>
 static vcnn_status launch_product(LossProduct a, int splits, hipStream_t st) {
   a.p.tiles_a = (int)ceil_div(a.cols, TILE::BA), a.p.tiles_b = (int)ceil_div(a.rows, TILE::BB);
   const auto kernel = loss_product_kernel<TILE, EPI, F32, A_ALONG, B_ALONG, B_PLANES>;
@@ -912,11 +931,11 @@ static vcnn_status launch_product(LossProduct a, int splits, hipStream_t st) {
   hipLaunchKernelGGL(kernel, dim3((unsigned)(a.p.tiles_a * a.p.tiles_b), (unsigned)splits), dim3(TILE::THREADS), TILE::LDS, st, a);
   return check_launch("fc_softmax_loss product");
 }
-// A_ALONG, B_ALONG: how the operands lie.  Of d both planes are read for dw, and in float all planes of all.
-template <int EPI, bool F32, bool A_ALONG, bool B_ALONG>
+// A_ALONG, B_ALONG: how the operands lie.  Of d, in TERMS planes, all are read for dw, and in float all planes of all.
+template <int EPI, bool F32, bool A_ALONG, bool B_ALONG, int TERMS>
 static vcnn_status launch_product(int tile, const LossProduct& a, int splits, hipStream_t st) {
-  return with_tile<F32 ? 4 : EPI == EPI_DW ? 2 : 1>(tile, [&](auto t) {
-    return launch_product<typename decltype(t)::type, EPI, F32, A_ALONG, B_ALONG, F32 || EPI != EPI_LOGITS>(a, splits, st);
+  return with_tile<F32 ? 4 : EPI == EPI_DW ? TERMS : 1>(tile, [&](auto t) {
+    return launch_product<typename decltype(t)::type, EPI, F32, A_ALONG, B_ALONG, TERMS>(a, splits, st);
   });
 }
 template <typename T>
@@ -960,6 +979,7 @@ static vcnn_status loss_products(LossPlan p, int batch, int in_f, int classes, c
   float* const down_x = F32 ? (float*)(ws + p.down_x) : nullptr;
   float* const down_w = F32 ? (float*)(ws + p.down_w) : nullptr;
   char* const xs = ws + p.x;
+  const int64_t z_pitch = (int64_t)p.classes_pitch / 2 * p.terms;  // floats
   // one block does for all rows and their mean where there is little to add up
   const bool mean_with_rows = batch <= kFewRows && (int64_t)batch * p.stat_tiles <= 8192;
   const char* weights = (const char*)w;
@@ -981,7 +1001,7 @@ static vcnn_status loss_products(LossPlan p, int batch, int in_f, int classes, c
     LossProduct l{};
     l.p.a = {weights, p.x_pitch, classes}, l.p.b = {as_it_is ? (const char*)(x + b0 * in_f) : xs, p.x_pitch, rows};
     l.p.k = F32 ? in_f : p.groups * 8, l.p.slabs_per_split = (int)ceil_div(l.p.k, 32);
-    l.rows = rows, l.cols = classes, l.z = z, l.z_pitch = p.classes_pitch, l.bias = bias, l.labels = lab;
+    l.rows = rows, l.cols = classes, l.z = z, l.z_pitch = z_pitch, l.z_group = 32 * p.terms, l.bias = bias, l.labels = lab;
     l.stats = (float2*)(ws + p.stats), l.at_label = (float*)(ws + p.at_label);
     l.meta = meta, l.down_a = down_w, l.down_b = down_x;
     const FewShape few = few_shape(p.part, classes);
@@ -989,7 +1009,7 @@ static vcnn_status loss_products(LossPlan p, int batch, int in_f, int classes, c
     auto launch_few = [&](auto kernel) { hipLaunchKernelGGL(kernel, few_grid, dim3(kFewThreads), 0, st, l, x + b0 * in_f, w, in_f, few.sharing); };
     const bool pairs = few.tiles == 2;
     if (!p.few) {
-      if (vcnn_status s = launch_product<EPI_LOGITS, F32, true, true>(p.tile_z, l, 1, st)) return s;
+      if (vcnn_status s = launch_product<EPI_LOGITS, F32, true, true, F32 ? 2 : 1>(p.tile_z, l, 1, st)) return s;
     } else if (rows <= 16) {
       pairs ? launch_few(loss_few_kernel<T, 2, 1>) : launch_few(loss_few_kernel<T, 1, 1>);
     } else if (rows <= 32) {
@@ -1018,29 +1038,41 @@ static vcnn_status loss_products(LossPlan p, int batch, int in_f, int classes, c
       continue;
     }
     float* const shares = dbias ? (float*)(ws + p.shares) : nullptr;
-    hipLaunchKernelGGL(loss_grad_kernel<F32>, dim3((unsigned)(p.classes_pitch / 64), (unsigned)ceil_div(rows, 64)), dim3(kThreads), 0, st, z,
-                       p.classes_pitch, rows, classes, lab, ignore, softmax, down_x, down_w, shares, p.classes_pitch);
+    auto with_terms = [&](auto f) {
+      if constexpr (!F32)
+        if (p.terms == 3) return f(std::integral_constant<int, 3>());
+      return f(std::integral_constant<int, 2>());
+    };
+    with_terms([&](auto terms) {
+      hipLaunchKernelGGL((loss_grad_kernel<F32, decltype(terms)::value>), dim3((unsigned)(p.classes_pitch / 64), (unsigned)ceil_div(rows, 64)),
+                         dim3(kThreads), 0, st, z, z_pitch, rows, classes, lab, ignore, softmax, down_x, down_w, shares, p.classes_pitch);
+    });
     if (vcnn_status s = check_launch("fc_softmax_loss gradient")) return s;
-    const int64_t z_pitch = (int64_t)p.classes_pitch * 4;
     if (dx) {
       LossProduct g{};
-      g.p.a = {weights, p.x_pitch, p.groups}, g.p.b = {(const char*)z, z_pitch, rows};
+      g.p.a = {weights, p.x_pitch, p.groups}, g.p.b = {(const char*)z, z_pitch * 4, rows};
       g.p.k = classes, g.p.slabs_per_split = (int)ceil_div(ceil_div(classes, 32), p.splits_dx);
       g.rows = rows, g.cols = in_f, g.meta = meta, g.out = dx + b0 * in_f, g.down_b = down_x;
       g.partial = p.splits_dx > 1 ? partial : nullptr;
       const int splits = (int)ceil_div(ceil_div(classes, 32), g.p.slabs_per_split);
-      if (vcnn_status s = launch_product<EPI_DX, F32, false, true>(p.tile_dx, g, splits, st)) return s;
+      if (vcnn_status s = with_terms([&](auto terms) {
+            return launch_product<EPI_DX, F32, false, true, decltype(terms)::value>(p.tile_dx, g, splits, st);
+          }))
+        return s;
       if (g.partial)
         if (vcnn_status s = launch_join(partial, splits, (int64_t)rows * in_f, meta, lab, ignore, 0, false, (T*)g.out, st)) return s;
     }
     if (dw) {
       LossProduct g{};
-      g.p.a = {xs, p.x_pitch, p.groups}, g.p.b = {(const char*)z, z_pitch, p.classes_pitch / 8};
+      g.p.a = {xs, p.x_pitch, p.groups}, g.p.b = {(const char*)z, z_pitch * 4, p.classes_pitch / 8};
       g.p.k = rows, g.p.slabs_per_split = (int)ceil_div(ceil_div(rows, 32), p.splits_dw);
       g.rows = classes, g.cols = in_f, g.meta = meta, g.out = dw, g.add = b0 > 0, g.down_b = down_w;
       g.partial = p.splits_dw > 1 ? partial : nullptr;
       const int splits = (int)ceil_div(ceil_div(rows, 32), g.p.slabs_per_split);
-      if (vcnn_status s = launch_product<EPI_DW, F32, false, false>(p.tile_dw, g, splits, st)) return s;
+      if (vcnn_status s = with_terms([&](auto terms) {
+            return launch_product<EPI_DW, F32, false, false, decltype(terms)::value>(p.tile_dw, g, splits, st);
+          }))
+        return s;
       if (g.partial)
         if (vcnn_status s = launch_join(partial, splits, (int64_t)classes * in_f, meta, lab, ignore, 0, b0 > 0, dw, st)) return s;
     }

@@ -2,8 +2,8 @@
 //     out[b][a] = sum over k of  A(a, k) B(b, k)
 // Each operand lies in memory as rows that run along k, or as rows of k that run along a (or b): the second kind is turned round
 // on its way from LDS to the registers (ds_read_b64_tr_b16: sixteen lanes read four rows of sixteen elements, and each gets a
-// column of four), so that no transposed copy is ever written.  An operand may come in planes, a high and a low term in turn
-// for every 64 elements; the products high x high, low x high and high x low are then made of one slab into the same sums.
+// column of four), so that no transposed copy is ever written.  An operand may come in planes, a high and a low term (or three)
+// in turn for every 64 elements; the products high x high, low x high and high x low are then made of one slab into the same sums.
 //
 // What bounds it.  On operands of zeros a step of 256 x 256 x 32 takes 1820 clocks of which the matrix cores are busy 1031, without
 // its loads 1440: a CU's loads to LDS wait for one another, 16 rows of 64 bytes each (rows of 1 KB: 1620).  On operands as they come
@@ -33,8 +33,8 @@ struct ProductArgs {
   int slabs_per_split;  // of ceil(k / 32)
 };
 
-// BA x BB outputs by waves of 16 TA x 16 TB, from PA and PB planes of the operands: high x high, and the products of a low term
-// with the other's high one.  RING slabs in LDS.
+// BA x BB outputs by waves of 16 TA x 16 TB, from PA and PB planes of the operands: high x high, and the products of the lower
+// terms with the other's high one.  RING slabs in LDS.
 template <int BA_, int BB_, int TA_, int TB_, int PA_, int PB_, int RING_>
 struct ProductTile {
   static constexpr int BA = BA_, BB = BB_, TA = TA_, TB = TB_, PA = PA_, PB = PB_, RING = RING_;
@@ -57,7 +57,8 @@ typedef __attribute__((address_space(3))) short4_t* LdsShort4;
 //   rows along k: word c (of four) of row r at place 4 r + (c ^ swizzle(r)): sixteen lanes of a read meet all banks (as in int8.hip)
 //   rows of k:    word c (of R / 8) of step k at place R / 8 * k + (c ^ turn(k)): a read of half a wave takes two neighbouring
 //                 words of eight steps 8 g + 0 .. 3 and 8 (g + 1) + 0 .. 3, which turn() sends to different banks
-template <bool ALONG, bool PLANES, int R, int THREADS>
+// PLANES: how many there are of it in memory.
+template <bool ALONG, int PLANES, int R, int THREADS>
 struct Way {
   static constexpr int L = R * 4 / THREADS, WPR = R / 8;
   static_assert(R >= 64 || ALONG, "the banks");
@@ -86,7 +87,7 @@ struct Way {
 #pragma unroll
       for (int i = 0; i < L; ++i) {
         const int p = i * THREADS + tid, k = p / WPR, c = min(r0 / 8 + ((p % WPR) ^ turn(k)), o.count - 1);
-        offset[i] = (uint32_t)k * (uint32_t)pitch + (uint32_t)(PLANES ? (c >> 3) * 256 + (c & 7) * 16 : c * 16);
+        offset[i] = (uint32_t)k * (uint32_t)pitch + (uint32_t)((c >> 3) * (PLANES * 128) + (c & 7) * 16);
         step[i] = k;
       }
     }
@@ -94,7 +95,7 @@ struct Way {
   // Word i of a plane of slab s (32 steps from 32 s on) to `to` (wave-uniform).
   __device__ __forceinline__ const char* from(int s, int plane) const {
     int64_t at;
-    if constexpr (ALONG) at = PLANES ? (int64_t)(s >> 1) * 256 + (s & 1) * 64 + plane * 128 : (int64_t)s * 64;
+    if constexpr (ALONG) at = (int64_t)(s >> 1) * (PLANES * 128) + (s & 1) * 64 + plane * 128;
     else at = (int64_t)s * 32 * pitch + plane * 128;
     return base + at;
   }
@@ -131,7 +132,7 @@ __device__ __forceinline__ void product_tile_of(const ProductArgs& p, int* ta, i
 // the first of the next step while it multiplies the second.  The one barrier of a step stands between the two: there the next slab is
 // in LDS for every wave, and every wave has read this one, whose place then takes the slab RING steps on; so a slab has RING - 1 steps
 // to arrive.  acc[i][j]: lane l has a = 16 i + 4 (l / 16) + q, b = 16 j + l % 16 of the wave's part.
-template <typename TILE, bool F16, bool A_ALONG, bool A_PLANES, bool B_ALONG, bool B_PLANES>
+template <typename TILE, bool F16, bool A_ALONG, int A_PLANES, bool B_ALONG, int B_PLANES>
 __device__ __forceinline__ void slab_product(const ProductArgs& p, int a0, int b0, uint4* smem,
                                              f32x4 (&acc)[TILE::TA][TILE::TB]) {
   constexpr int TA = TILE::TA, TB = TILE::TB, PA = TILE::PA, PB = TILE::PB, LA = TILE::LA, LB = TILE::LB, L = TILE::LOADS;
@@ -163,8 +164,8 @@ __device__ __forceinline__ void slab_product(const ProductArgs& p, int a0, int b
     for (int j = 0; j < TB; ++j) acc[i][j] = (f32x4){0.f, 0.f, 0.f, 0.f};
   const int ra = (wave % TILE::WA) * 16 * TA, rb = (wave / TILE::WA) * 16 * TB;
   constexpr int H = TA / 2;
-  // fa: [half][term]; fb: the high terms of this step and the next, and the low ones of this step
-  uint4 fa[2][PA][H], fb[2][TB], fl[TB];
+  // fa: [half][term]; fb: the high terms of this step and the next, and the lower ones of this step
+  uint4 fa[2][PA][H], fb[2][TB], fl[2][TB];
   auto read_a = [&](int slot, int h) {
     const uint4* const buf = smem + slot * TILE::WORDS;
 #pragma unroll
@@ -209,12 +210,14 @@ __device__ __forceinline__ void slab_product(const ProductArgs& p, int a0, int b
   auto step = [&](int s, int n, auto is_whole) {
     const int next = here + 1 == R ? 0 : here + 1, last = here == 0 ? R - 1 : here - 1;
     int turn = PAIRS;
-    if constexpr (PB == 2) read_b(here, fl, 1);
+    if constexpr (PB >= 2) read_b(here, fl[0], 1);
+    if constexpr (PB == 3) read_b(here, fl[1], 2);
     read_a(here, 1);
     __builtin_amdgcn_sched_barrier(0);
     multiply(0, 0, fb[n], s + R - 1, last, turn++, is_whole);
     if constexpr (PA == 2) multiply(0, 1, fb[n], s + R - 1, last, turn++, is_whole);
-    if constexpr (PB == 2) multiply(0, 0, fl, s + R - 1, last, turn++, is_whole);
+    if constexpr (PB >= 2) multiply(0, 0, fl[0], s + R - 1, last, turn++, is_whole);
+    if constexpr (PB == 3) multiply(0, 0, fl[1], s + R - 1, last, turn++, is_whole);
     // slab s + 1 is there, for everyone; slab s has been read by everyone (vmcnt and lgkmcnt(0))
     __builtin_amdgcn_s_waitcnt(all_but((R - 2) * L) & ~0x0F00);
     __builtin_amdgcn_s_barrier();
@@ -222,7 +225,8 @@ __device__ __forceinline__ void slab_product(const ProductArgs& p, int a0, int b
     turn = 0;
     read_b(next, fb[n ^ 1], 0), read_a(next, 0);
     __builtin_amdgcn_sched_barrier(0);
-    if constexpr (PB == 2) multiply(1, 0, fl, s + R, here, turn++, is_whole);
+    if constexpr (PB == 3) multiply(1, 0, fl[1], s + R, here, turn++, is_whole);
+    if constexpr (PB >= 2) multiply(1, 0, fl[0], s + R, here, turn++, is_whole);
     if constexpr (PA == 2) multiply(1, 1, fb[n], s + R, here, turn++, is_whole);
     multiply(1, 0, fb[n], s + R, here, turn++, is_whole);
     here = next;

@@ -1,7 +1,7 @@
 // Dropout of the rows of a matrix, with the residual's addition behind it, and the step of its generator (dropout.h):
 //     y = residual + (kept ? x / (1 - p) : 0),   dx = kept ? dy / (1 - p) : 0
 // A thread makes the bits of a block of eight elements of one row and loads and stores them as groups of 16 bytes (two in float)
-// wherever the row starts.  Bandwidth: bfloat16, 8192 x 5120, with a residual 55.8 us (4.5 TB/s; a large copy 5.1), without 31.5
+// wherever the row starts.  Bandwidth: bfloat16, 8192 x 5120, with a residual 51.4 us (4.9 TB/s; a large copy 5.1), without 31.5
 // (read from the last-level cache in part); the generator's products are hidden behind the loads of other waves.
 #include "dropout.h"
 

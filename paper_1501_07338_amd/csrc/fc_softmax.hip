@@ -319,7 +319,7 @@ __global__ __launch_bounds__(TILE::THREADS, TILE::WAVES_SIMD) void loss_product_
 // instruction wants them, straight into registers: lane l row l % 16, and of every 64 bytes of it the 16 from 16 (l / 16) on.  (Which
 // steps of the sum a lane holds does not matter as long as it is the same ones of both.)  Of few classes `sharing` waves share a sum.
 // The eight waves of a block leave one maximum and sum of their classes.
-// 1 sample 4096 -> 65536 in bfloat16 109 us (4.9 TB/s, half of w from the last-level cache), in float 215.
+// 1 sample 4096 -> 65536 in bfloat16 102 us (5.2 TB/s, half of w from the last-level cache), in float 215.
 static constexpr int kFewThreads = 512, kFewWaves = kFewThreads / 64, kFewRows = 64;
 struct FewShape {
   int tiles, sharing;  // MA; waves of one sum: enough blocks for the chip

@@ -32,48 +32,92 @@ struct LossMeta {     // at the head of the workspace
 };
 
 // ---- operands ----------------------------------------------------------------------------------------------------------
-// How many samples count (before the first part), and no largest magnitude yet (x before each).
-__global__ __launch_bounds__(1024) void loss_meta_kernel(const int32_t* labels, int batch, int ignore, int first, LossMeta* meta) {
-  __shared__ int counts[16];
-  if (threadIdx.x == 0) meta->most[0] = 0;
-  if (!first) return;
+// How many samples count, by a block.
+template <int THREADS>
+__device__ __forceinline__ void count_samples(const int32_t* labels, int batch, int ignore, LossMeta* meta) {
+  __shared__ int counts[THREADS / 64];
   int n = 0;
-  for (int b = threadIdx.x; b < batch; b += 1024) n += labels[b] != ignore;
+#pragma unroll 4
+  for (int64_t b = threadIdx.x * 4; b < batch; b += THREADS * 4) {
+    if (b + 4 <= batch) {
+      const Loose16 v = *reinterpret_cast<const Loose16*>(labels + b);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) n += (int)v.w[i] != ignore;
+    } else {
+      for (int64_t i = b; i < batch; ++i) n += labels[i] != ignore;
+    }
+  }
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) n += __shfl_xor(n, d);
   if ((threadIdx.x & 63) == 0) counts[threadIdx.x >> 6] = n;
   __syncthreads();
   if (threadIdx.x > 0) return;
   n = 0;
-  for (int w = 0; w < 16; ++w) n += counts[w];
-  meta->inverse = n ? 1.f / (float)n : 0.f, meta->most[1] = 0;
+  for (int w = 0; w < THREADS / 64; ++w) n += counts[w];
+  meta->inverse = n ? 1.f / (float)n : 0.f;
 }
 
-// Rows re-laid with a length of whole groups of eight, the rows of samples that do not count as zeros (whatever they hold must
-// not meet the zeros of d as a NaN).
-template <typename T>
-__global__ __launch_bounds__(kThreads) void relay_rows_kernel(const T* x, T* to, int64_t rows, int cols, int groups,
-                                                              const int32_t* labels, int ignore) {
-  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < rows * groups; i += (int64_t)gridDim.x * kThreads) {
-    const int64_t row = i / groups;
-    const int c = (int)(i - row * groups) * 8;
+// Float: how many samples count (before the first part), and no largest magnitude yet (x before each).
+__global__ __launch_bounds__(1024) void loss_meta_kernel(const int32_t* labels, int batch, int ignore, int first, LossMeta* meta) {
+  if (threadIdx.x == 0) meta->most[0] = 0;
+  if (!first) return;
+  if (threadIdx.x == 0) meta->most[1] = 0;
+  count_samples<1024>(labels, batch, ignore, meta);
+}
+
+// What is re-laid in one launch: a part's x, and w before the first.
+struct Relay {
+  const void* x;
+  const void* w;
+  char* xs;
+  char* ws;
+  int64_t rows, all;      // of x, and of both
+  int cols, groups;       // of eight
+  const int32_t* labels;  // nullable: of x
+  int ignore;
+  float* down_x;          // float
+  float* down_w;
+  LossMeta* meta;
+  const int32_t* count;   // bfloat16: the first block counts the `batch` labels here (nullable)
+  int batch;
+  __device__ __forceinline__ bool counts(int64_t row) const { return !labels || row >= rows || labels[row] != ignore; }
+};
+
+// Rows with a length of whole groups of eight, those of samples that do not count as zeros (whatever they hold must not meet the zeros
+// of d as a NaN).
+__global__ __launch_bounds__(kThreads) void relay_rows_kernel(Relay a) {
+  int block = blockIdx.x;
+  if (a.count) {
+    if (block == 0) {
+      count_samples<kThreads>(a.count, a.batch, a.ignore, a.meta);
+      return;
+    }
+    --block;
+  }
+  const int64_t blocks = gridDim.x - (a.count ? 1 : 0);
+  for (int64_t i = (int64_t)block * kThreads + threadIdx.x; i < a.all * a.groups; i += blocks * kThreads) {
+    const int64_t row = i / a.groups, first = row < a.rows ? 0 : a.rows;
+    const int c = (int)(i - row * a.groups) * 8;
+    const bf16* const from = static_cast<const bf16*>(row < a.rows ? a.x : a.w);
     Loose16 v{{0, 0, 0, 0}};
-    if (!labels || labels[row] != ignore) v = load_group(x + row * cols, c, cols);
-    *reinterpret_cast<uint4*>(to + i * 8) = make_uint4(v.w[0], v.w[1], v.w[2], v.w[3]);
+    if (a.counts(row)) v = load_group(from + (row - first) * a.cols, c, a.cols);
+    *reinterpret_cast<uint4*>((row < a.rows ? a.xs : a.ws) + (i - first * a.groups) * 16) = make_uint4(v.w[0], v.w[1], v.w[2], v.w[3]);
   }
 }
 
 // Float: the largest finite magnitude of each row (a wave a row) and of all.  Rows of samples that do not count are not looked at.
-__global__ __launch_bounds__(kThreads) void row_most_kernel(const float* x, int64_t rows, int cols, const int32_t* labels, int ignore,
-                                                            uint32_t* row_most, uint32_t* most) {
+__global__ __launch_bounds__(kThreads) void row_most_kernel(Relay a) {
   const int lane = threadIdx.x & 63;
-  uint32_t all = 0;
-  for (int64_t row = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6); row < rows; row += (int64_t)gridDim.x * (kThreads / 64)) {
+  uint32_t all[2] = {0, 0};
+  for (int64_t at = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6); at < a.all; at += (int64_t)gridDim.x * (kThreads / 64)) {
+    const bool of_w = at >= a.rows;
+    const int64_t row = of_w ? at - a.rows : at;
+    const float* const from = static_cast<const float*>(of_w ? a.w : a.x) + row * a.cols;
     uint32_t m = 0;
-    if (!labels || labels[row] != ignore) {
+    if (a.counts(at)) {
 #pragma unroll 4
-      for (int c = lane * 4; c < cols; c += 256) {
-        const Loose16 v = load_group(x + row * cols, c, cols);
+      for (int c = lane * 4; c < a.cols; c += 256) {
+        const Loose16 v = load_group(from, c, a.cols);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const uint32_t bits = v.w[i] & 0x7fffffffu;
@@ -82,17 +126,19 @@ __global__ __launch_bounds__(kThreads) void row_most_kernel(const float* x, int6
       }
     }
     m = wave_max(m);
-    if (lane == 0) row_most[row] = m;
-    all = max(all, m);
+    if (lane == 0) reinterpret_cast<uint32_t*>(of_w ? a.down_w : a.down_x)[row] = m;
+    all[0] = max(all[0], of_w ? 0u : m), all[1] = max(all[1], of_w ? m : 0u);
   }
   // one of a block, and only if it is larger than what is known (2000 of one place take 60 us); whatever the order, the same
-  __shared__ uint32_t tops[kThreads / 64];
-  if (lane == 0) tops[threadIdx.x >> 6] = all;
+  __shared__ uint32_t tops[2][kThreads / 64];
+  if (lane == 0) tops[0][threadIdx.x >> 6] = all[0], tops[1][threadIdx.x >> 6] = all[1];
   __syncthreads();
-  if (threadIdx.x > 0) return;
+  if (threadIdx.x > 1) return;
+  uint32_t top = 0;
 #pragma unroll
-  for (int w = 1; w < kThreads / 64; ++w) all = max(all, tops[w]);
-  if (all > __atomic_load_n(most, __ATOMIC_RELAXED)) atomicMax(most, all);
+  for (int w = 0; w < kThreads / 64; ++w) top = max(top, tops[threadIdx.x][w]);
+  uint32_t* const most = &a.meta->most[threadIdx.x];
+  if (top > __atomic_load_n(most, __ATOMIC_RELAXED)) atomicMax(most, top);
 }
 
 // The power of two that brings the largest of all, `bits`, to 2^14 .. 2^15 (at most 2^110, so that it and its inverse are floats).
@@ -108,24 +154,29 @@ __device__ __forceinline__ void split_f16(float v, _Float16* hi, _Float16* lo) {
 
 // Rows in two terms: 64 high ones, 64 low ones in turn, zeros behind the row's end; row_most becomes the 2^-(0 .. 8) by which a row
 // is scaled more than the least.
-__global__ __launch_bounds__(kThreads) void relay_planes_kernel(const float* x, char* to, int64_t rows, int cols, int groups,
-                                                                const int32_t* labels, int ignore, float* down, const uint32_t* most) {
-  const uint32_t top = *most;
-  const int least = least_power(top), lane = threadIdx.x & 63;
-  for (int64_t row = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6); row < rows; row += (int64_t)gridDim.x * (kThreads / 64)) {
-    const uint32_t bits = __builtin_amdgcn_readfirstlane(__float_as_uint(down[row]));  // (every lane has read it before lane 0 writes)
+__global__ __launch_bounds__(kThreads) void relay_planes_kernel(Relay a) {
+  const int lane = threadIdx.x & 63;
+  for (int64_t at = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6); at < a.all; at += (int64_t)gridDim.x * (kThreads / 64)) {
+    const bool of_w = at >= a.rows;
+    const int64_t row = of_w ? at - a.rows : at;
+    const float* const from = static_cast<const float*>(of_w ? a.w : a.x) + row * a.cols;
+    char* const to = (of_w ? a.ws : a.xs) + row * (a.groups >> 3) * 256;
+    float* const down = (of_w ? a.down_w : a.down_x) + row;
+    const uint32_t top = a.meta->most[of_w];
+    const int least = least_power(top);
+    const uint32_t bits = __builtin_amdgcn_readfirstlane(__float_as_uint(*down));  // (every lane has read it before lane 0 writes)
     const int more = bits ? min(8, (int)max(1u, top >> 23) - (int)max(1u, bits >> 23)) : 8;
-    if (lane == 0) down[row] = power2(-more);
+    if (lane == 0) *down = power2(-more);
     const float scale = power2(least + more);
-    const bool counts = !labels || labels[row] != ignore;
-    for (int g = lane; g < groups; g += 64) {
+    const bool counts = a.counts(at);
+    for (int g = lane; g < a.groups; g += 64) {
       const int c = g * 8;
       float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
       if (counts) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
-          if (c + 4 * h < cols) {
-            const Loose16 q = load_group(x + row * cols, c + 4 * h, cols);
+          if (c + 4 * h < a.cols) {
+            const Loose16 q = load_group(from, c + 4 * h, a.cols);
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[4 * h + i] = __uint_as_float(q.w[i]) * scale;
           }
@@ -137,9 +188,9 @@ __global__ __launch_bounds__(kThreads) void relay_planes_kernel(const float* x, 
         split_f16(v[i], &a, &b);
         hi[i] = a, lo[i] = b;
       }
-      char* const at = to + (row * (groups >> 3) + (g >> 3)) * 256 + (g & 7) * 16;
-      *reinterpret_cast<f16x8*>(at) = hi;
-      *reinterpret_cast<f16x8*>(at + 128) = lo;
+      char* const place = to + (g >> 3) * 256 + (g & 7) * 16;
+      *reinterpret_cast<f16x8*>(place) = hi;
+      *reinterpret_cast<f16x8*>(place + 128) = lo;
     }
   }
 }
@@ -761,24 +812,34 @@ __global__ __launch_bounds__(kThreads) void loss_grad_kernel(float* z, int64_t p
   }
 }
 
-__global__ __launch_bounds__(kThreads) void loss_bias_kernel(const float* shares, int64_t share_pitch, int parts, int classes,
-                                                             const LossMeta* meta, int add, float* dbias) {
-  const int c = blockIdx.x * kThreads + threadIdx.x;
-  if (c >= classes) return;
-  float s = 0.f;
+// The mean of what the samples cost, in a fixed order, by the first block; dbias by the others.
+struct LossEnd {
+  const float* each;
+  const int32_t* labels;
+  int ignore, batch;
+  float* loss;          // nullable: no mean
+  const float* shares;  // of dbias, `parts` of them
+  int64_t share_pitch;
+  int parts, classes, add;
+  const LossMeta* meta;
+  float* dbias;
+};
+__global__ __launch_bounds__(1024) void loss_end_kernel(LossEnd a) {
+  if (blockIdx.x > 0 || !a.loss) {
+    const int64_t c = (int64_t)(blockIdx.x - (a.loss ? 1 : 0)) * 1024 + threadIdx.x;
+    if (c >= a.classes) return;
+    float s = 0.f;
 #pragma unroll 8
-  for (int p = 0; p < parts; ++p) s += shares[p * share_pitch + c];
-  s *= meta->inverse;
-  dbias[c] = add ? dbias[c] + s : s;
-}
-
-// The mean of what the samples cost, in a fixed order.
-__global__ __launch_bounds__(1024) void loss_mean_kernel(const float* each, const int32_t* labels, int ignore, int batch, float* loss) {
+    for (int p = 0; p < a.parts; ++p) s += a.shares[p * a.share_pitch + c];
+    s *= a.meta->inverse;
+    a.dbias[c] = a.add ? a.dbias[c] + s : s;
+    return;
+  }
   __shared__ float sums[16];
   __shared__ int counts[16];
   float s = 0.f;
   int n = 0;
-  for (int b = threadIdx.x; b < batch; b += 1024) s += each[b], n += labels[b] != ignore;
+  for (int b = threadIdx.x; b < a.batch; b += 1024) s += a.each[b], n += a.labels[b] != a.ignore;
   s = wave_sum(s);
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) n += __shfl_xor(n, d);
@@ -787,7 +848,12 @@ __global__ __launch_bounds__(1024) void loss_mean_kernel(const float* each, cons
   if (threadIdx.x > 0) return;
   s = 0.f, n = 0;
   for (int w = 0; w < 16; ++w) s += sums[w], n += counts[w];
-  *loss = n ? s / (float)n : 0.f;
+  *a.loss = n ? s / (float)n : 0.f;
+}
+static vcnn_status launch_end(const LossEnd& a, hipStream_t st) {
+  const unsigned blocks = (a.loss ? 1 : 0) + (a.dbias ? (unsigned)ceil_div(a.classes, 1024) : 0);
+  if (blocks > 0) hipLaunchKernelGGL(loss_end_kernel, dim3(blocks), dim3(1024), 0, st, a);
+  return check_launch("fc_softmax_loss mean");
 }
 
 // ---- plan ----------------------------------------------------------------------------------------------------------------
@@ -950,18 +1016,16 @@ static vcnn_status launch_join(const float* partial, int splits, int64_t count, 
   return check_launch("fc_softmax_loss join");
 }
 
-// x or w of T as the products read it.
-static vcnn_status relay(const bf16* x, char* to, const LossPlan& p, int64_t rows, int cols, const int32_t* labels, int ignore, float*,
-                         const uint32_t*, hipStream_t st) {
-  hipLaunchKernelGGL(relay_rows_kernel<bf16>, dim3((unsigned)std::min<int64_t>(ceil_div(rows * p.groups, kThreads), 256 * 16)),
-                     dim3(kThreads), 0, st, x, (bf16*)to, rows, cols, p.groups, labels, ignore);
-  return check_launch("fc_softmax_loss relay");
-}
-static vcnn_status relay(const float* x, char* to, const LossPlan& p, int64_t rows, int cols, const int32_t* labels, int ignore,
-                         float* down, uint32_t* most, hipStream_t st) {
-  const dim3 grid((unsigned)std::min<int64_t>(ceil_div(rows, kThreads / 64), 256 * 8));
-  hipLaunchKernelGGL(row_most_kernel, grid, dim3(kThreads), 0, st, x, rows, cols, labels, ignore, (uint32_t*)down, most);
-  hipLaunchKernelGGL(relay_planes_kernel, grid, dim3(kThreads), 0, st, x, to, rows, cols, p.groups, labels, ignore, down, most);
+// As the products read them, in bfloat16 or float.
+static vcnn_status launch_relay(bool f32, const Relay& a, hipStream_t st) {
+  if (f32) {
+    const dim3 grid((unsigned)std::min<int64_t>(ceil_div(a.all, kThreads / 64), 256 * 8));
+    hipLaunchKernelGGL(row_most_kernel, grid, dim3(kThreads), 0, st, a);
+    hipLaunchKernelGGL(relay_planes_kernel, grid, dim3(kThreads), 0, st, a);
+  } else {
+    const int64_t blocks = std::min<int64_t>(ceil_div(a.all * a.groups, kThreads), 256 * 16);
+    hipLaunchKernelGGL(relay_rows_kernel, dim3((unsigned)(blocks + (a.count ? 1 : 0))), dim3(kThreads), 0, st, a);
+  }
   return check_launch("fc_softmax_loss relay");
 }
 
@@ -982,24 +1046,29 @@ static vcnn_status loss_products(LossPlan p, int batch, int in_f, int classes, c
   const int64_t z_pitch = (int64_t)p.classes_pitch / 2 * p.terms;  // floats
   // one block does for all rows and their mean where there is little to add up
   const bool mean_with_rows = batch <= kFewRows && (int64_t)batch * p.stat_tiles <= 8192;
+  LossEnd end{each, labels, ignore, batch, mean_with_rows ? nullptr : loss};
   const char* weights = (const char*)w;
   for (int64_t b0 = 0; b0 < batch; b0 += p.part) {
     const int rows = (int)std::min<int64_t>(p.part, batch - b0);
     const int32_t* const lab = labels + b0;
-    if (!p.few && (grads || F32)) {
+    const T* const xp = x + b0 * in_f;
+    // (the cost alone reads x where it stands if its rows have whole groups)
+    const bool as_it_is = !F32 && !grads && in_f % 8 == 0 && (reinterpret_cast<uintptr_t>(x) & 15) == 0;
+    const bool relay_w = b0 == 0 && p.relay_w;
+    if (relay_w) weights = ws + p.w;
+    if (F32 && !p.few) {
       hipLaunchKernelGGL(loss_meta_kernel, dim3(1), dim3(1024), 0, st, labels, batch, ignore, b0 == 0, meta);
       if (vcnn_status s = check_launch("fc_softmax_loss count")) return s;
     }
-    if (b0 == 0 && p.relay_w) {
-      weights = ws + p.w;
-      if (vcnn_status s = relay(w, ws + p.w, p, classes, in_f, nullptr, 0, down_w, &meta->most[1], st)) return s;
+    if (!p.few && (!as_it_is || relay_w)) {
+      Relay r{};
+      r.x = xp, r.w = w, r.xs = xs, r.ws = ws + p.w, r.rows = as_it_is ? 0 : rows, r.all = r.rows + (relay_w ? classes : 0);
+      r.cols = in_f, r.groups = p.groups, r.labels = grads || F32 ? lab : nullptr, r.ignore = ignore;
+      r.down_x = down_x, r.down_w = down_w, r.meta = meta, r.count = !F32 && grads && b0 == 0 ? labels : nullptr, r.batch = batch;
+      if (vcnn_status s = launch_relay(F32, r, st)) return s;
     }
-    // (the cost alone reads x where it stands if its rows have whole groups)
-    const bool as_it_is = !F32 && !grads && in_f % 8 == 0 && (reinterpret_cast<uintptr_t>(x) & 15) == 0;
-    if (!as_it_is && !p.few)
-      if (vcnn_status s = relay(x + b0 * in_f, xs, p, rows, in_f, grads || F32 ? lab : nullptr, ignore, down_x, &meta->most[0], st)) return s;
     LossProduct l{};
-    l.p.a = {weights, p.x_pitch, classes}, l.p.b = {as_it_is ? (const char*)(x + b0 * in_f) : xs, p.x_pitch, rows};
+    l.p.a = {weights, p.x_pitch, classes}, l.p.b = {as_it_is ? (const char*)xp : xs, p.x_pitch, rows};
     l.p.k = F32 ? in_f : p.groups * 8, l.p.slabs_per_split = (int)ceil_div(l.p.k, 32);
     l.rows = rows, l.cols = classes, l.z = z, l.z_pitch = z_pitch, l.z_group = 32 * p.terms, l.bias = bias, l.labels = lab;
     l.stats = (float2*)(ws + p.stats), l.at_label = (float*)(ws + p.at_label);
@@ -1076,15 +1145,15 @@ static vcnn_status loss_products(LossPlan p, int batch, int in_f, int classes, c
       if (g.partial)
         if (vcnn_status s = launch_join(partial, splits, (int64_t)classes * in_f, meta, lab, ignore, 0, b0 > 0, dw, st)) return s;
     }
-    if (dbias) {
-      hipLaunchKernelGGL(loss_bias_kernel, dim3((unsigned)ceil_div(classes, kThreads)), dim3(kThreads), 0, st, shares, p.classes_pitch,
-                         (int)ceil_div(rows, 64), classes, meta, b0 > 0, dbias);
-      if (vcnn_status s = check_launch("fc_softmax_loss bias")) return s;
+    end.shares = shares, end.share_pitch = p.classes_pitch, end.parts = (int)ceil_div(rows, 64), end.classes = classes, end.add = b0 > 0;
+    end.meta = meta, end.dbias = dbias;
+    if (b0 + rows < batch) {
+      LossEnd one = end;
+      one.loss = nullptr;
+      if (vcnn_status s = launch_end(one, st)) return s;
     }
   }
-  if (mean_with_rows) return VCNN_OK;
-  hipLaunchKernelGGL(loss_mean_kernel, dim3(1), dim3(1024), 0, st, each, labels, ignore, batch, loss);
-  return check_launch("fc_softmax_loss mean");
+  return launch_end(end, st);
 }
 
 // ---- small float layers --------------------------------------------------------------------------------------------------
@@ -1231,8 +1300,7 @@ static vcnn_status loss_float(int batch, int in_f, int classes, const float* x, 
   if (dw) x = (const float*)(ws + p.x);
   if (grads)
     if (vcnn_status s = vcnn_fc_bwd(VCNN_F32, batch, in_f, classes, x, w, z, dw, dbias, dx, st)) return s;
-  hipLaunchKernelGGL(loss_mean_kernel, dim3(1), dim3(1024), 0, st, each, labels, ignore, batch, loss);
-  return check_launch("fc_softmax_loss mean");
+  return launch_end({each, labels, ignore, batch, loss}, st);
 }
 
 // ---- entry ---------------------------------------------------------------------------------------------------------------

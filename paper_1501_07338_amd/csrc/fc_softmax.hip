@@ -939,13 +939,21 @@ static constexpr int kMostSamples = 1 << 20;  // of a part
 // 40 x 2048 -> 8192 65, 63 us; 700 x 1024 -> 16384 206, 186; 1024 x 8192 -> 32768 2.36, 2.05 ms; 2048 x 4096 -> 65536 4.70, 4.06.
 static constexpr int kTwoTerms = 4096;
 
+// Whether the gradients of so few samples are made in float while w is read: always in float, in bfloat16 where the matrix cores, which
+// read w once more and take more launches, are slower.  Sixteen multiplications a weight and four samples bound it beyond (in
+// bfloat16, this way and by products: 4 x 4096 -> 32768 303, 322 us, 6 400, 323, 16 481, 328; 8 x 1024 -> 9000 43, 48, 12 61, 48;
+// 16 x 490 -> 1260 29, 32).
+static bool few_gradients(bool f32, int64_t batch, int64_t in_f, int64_t classes) {
+  return batch <= kFewGrad && (f32 || batch <= 4 || batch * in_f * classes <= (int64_t)1 << 26);
+}
+
 static LossPlan loss_plan(bool f32, int part, int batch, int in_f, int classes, bool grads) {
   LossPlan p{};
   p.f32 = f32, p.part = part;
   p.classes_pitch = (int)ceil_div(classes, 64) * 64;
   p.groups = f32 ? (int)ceil_div(in_f, 64) * 8 : (int)ceil_div(in_f, 8);
   p.x_pitch = (int64_t)p.groups * (f32 ? 32 : 16);
-  p.few_grads = grads && part <= kFewGrad && batch <= kFewGrad;
+  p.few_grads = grads && part <= kFewGrad && few_gradients(f32, batch, in_f, classes);
   p.few = p.few_grads || (!grads && part <= kFewRows);
   p.relay_w = !p.few && (f32 || in_f % 8 != 0);
   p.terms = f32 || p.few || batch >= kTwoTerms ? 2 : 3;

@@ -15,7 +15,8 @@ IGNORE = -100
 SHAPES = [(1, 1, 1), (1, 8, 10), (3, 7, 5), (5, 64, 10), (128, 500, 10), (64, 100, 1000), (130, 129, 257), (257, 64, 300),
           (300, 1032, 520), (70, 33, 4099), (513, 256, 2049), (17, 96, 20000), (700, 200, 16400), (16, 300, 5000), (9, 1030, 777),
           (2, 5, 70000), (40, 72, 17000), (64, 260, 130), (2500, 40, 300), (2100, 100, 90), (33, 2000, 65), (600, 500, 5000), (100, 3, 70)]
-LARGE = [(2048, 6144, 300), (200, 2050, 6200), (1025, 40, 33000), (5000, 3, 9000), (200000, 5, 9), (70000, 130, 12)]
+LARGE = [(2048, 6144, 300), (200, 2050, 6200), (1025, 40, 33000), (5000, 3, 9000), (200000, 5, 9), (70000, 130, 12),
+         (5, 1000, 14000), (16, 703, 6100), (9, 1024, 7500)]
 
 
 def inputs(batch, in_f, classes, dtype, ignored=0.2, seed=1):

@@ -6,12 +6,13 @@
 // in turn for every 64 elements; the products high x high, low x high and high x low are then made of one slab into the same sums.
 //
 // What bounds it.  On operands of zeros a step of 256 x 256 x 32 takes 1820 clocks of which the matrix cores are busy 1031, without
-// its loads 1440: a CU's loads to LDS wait for one another, 16 rows of 64 bytes each (rows of 1 KB: 1620).  On operands as they come
-// the clock falls to 1.6 .. 1.9 GHz instead, and of all that only 4 % are left: 4096 x 4096 x 65536, called in turn, 1.88 ms (1.17
-// PFLOP/s; the library's product 1.46 ms), with d along the sum 1.66 ms (1.32), its two terms 3.49 ms (1.26).  No bank conflicts.  Measured and
-// not taken: 256 x 128 in two blocks a CU 2.31 ms, not 1.90 (the loads); 128 x 128 a wave, four waves, 2.59 (the sums do not fit
-// beside the operands); five slabs, a higher priority of the products, and LDS reads among them: no difference; planes in turn
-// for every 32 elements, so that a load takes both: float 220, 210, 250 us, not 227, 203, 238, and the pass that writes them 490, not 434.
+// its loads 1440: a CU's loads to LDS wait for one another, 16 rows of 64 bytes each (rows of 1 KB: 1620).  On operands as they
+// come the clock falls to 1.6 .. 1.9 GHz instead, and of all that only 4 % are left: 4096 x 4096 x 65536, called in turn, 1.88 ms
+// (1.17 PFLOP/s; the library's product 1.46 ms), with d along the sum 1.66 ms (1.32), its two terms 3.49 ms (1.26).  No bank
+// conflicts.  Measured and not taken: 256 x 128 in two blocks a CU 2.31 ms, not 1.90 (the loads); 128 x 128 a wave, four waves,
+// 2.59 (the sums do not fit beside the operands); five slabs, a higher priority of the products, and LDS reads among them: no
+// difference; planes in turn for every 32 elements, so that a load takes both: float 220, 210, 250 us, not 227, 203, 238, and the
+// pass that writes them 490, not 434.
 #pragma once
 #include <type_traits>
 
